@@ -23,6 +23,8 @@ DEVICE_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC",
 HOST_CXX = os.environ.get("CXX_HOST", "g++")
 HOST_SOURCES = ["ckpt_runtime.cpp", "ckpt_snapshot.cpp", "ckpt_check.cpp", "ckpt_bounce.cpp", "ckpt_file.cpp",
                 "ckpt_h2h.cpp", "ckpt_peer.cpp", "ckpt_recover.cpp", "ckpt_noalloc.cpp"]
+OPS_SOURCES = ["ckpt_ops.cpp"]  # the training-step operators: with their kernels only, apart from the runtime
+KERNEL_SOURCES = ["ckpt_kernels.hip", "loss_kernels.hip", "optim_kernels.hip"]
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-pthread", "-Wall", "-Wextra", "-D__HIP_PLATFORM_AMD__",
               "-I", "/opt/rocm/include"]
 
@@ -68,16 +70,18 @@ def build(verbose=False):
     Python module beside it (always rebuilds)."""
     obj_dir = os.path.join(PKG, "_build")
     os.makedirs(obj_dir, exist_ok=True)
-    k_obj = os.path.join(obj_dir, "ckpt_kernels.o")
     inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
-    _run([HIPCC] + DEVICE_FLAGS + inc + ["-c", os.path.join(CSRC, "ckpt_kernels.hip"), "-o", k_obj], verbose)
-    host_objs = []
-    for src in HOST_SOURCES:
+    objs = []
+    for src in KERNEL_SOURCES:
+        o = os.path.join(obj_dir, src.replace(".hip", ".o"))
+        _run([HIPCC] + DEVICE_FLAGS + inc + ["-c", os.path.join(CSRC, src), "-o", o], verbose)
+        objs.append(o)
+    for src in HOST_SOURCES + OPS_SOURCES:
         o = os.path.join(obj_dir, src.replace(".cpp", ".o"))
         _run([HOST_CXX] + HOST_FLAGS + inc + ["-c", os.path.join(CSRC, src), "-o", o], verbose)
-        host_objs.append(o)
+        objs.append(o)
     tmp = LIB + ".tmp"
-    _run([HIPCC, "--offload-arch=" + ARCH, "-shared", "-fPIC", k_obj] + host_objs + ["-o", tmp, "-L/opt/rocm/lib",
+    _run([HIPCC, "--offload-arch=" + ARCH, "-shared", "-fPIC"] + objs + ["-o", tmp, "-L/opt/rocm/lib",
           "-lhsa-runtime64", "-lpthread"], verbose)
     os.replace(tmp, LIB)
     build_py_ext(verbose)

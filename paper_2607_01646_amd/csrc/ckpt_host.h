@@ -570,6 +570,21 @@ ckpt_status dma(ckpt_ctx* c, void* dst, hsa_agent_t dst_agent, const void* src, 
                 uint32_t n_dep = 1);
 // Text of this thread's last failed ckpt_pack_noalloc ("" if none).
 const char* noalloc_error();
+// For the entry points without a context (ckpt_noalloc.cpp): set and clear
+// that text; check that [p, p + n) is memory of `device` inside one allocation;
+// make `device` current until the guard goes.
+ckpt_status fail_free(ckpt_status code, const char* fmt, ...);
+void clear_free_error();
+ckpt_status check_range(const void* p, uint64_t n, int device, const char* what);
+struct DeviceGuard {
+    int prev = -1;
+    bool set = false;
+    ~DeviceGuard()
+    {
+        if (set) (void)hipSetDevice(prev);
+    }
+};
+ckpt_status enter_device(int32_t device, DeviceGuard& dg);
 
 // Snapshot records (ckpt_runtime.cpp)
 ckpt_status get_res(ckpt_ctx* c, RecRes** out);

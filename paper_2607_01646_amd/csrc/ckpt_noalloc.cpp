@@ -15,6 +15,8 @@ namespace {
 
 thread_local char t_err[384];
 
+} // namespace
+
 ckpt_status fail_free(ckpt_status code, const char* fmt, ...)
 {
     va_list ap;
@@ -24,7 +26,7 @@ ckpt_status fail_free(ckpt_status code, const char* fmt, ...)
     return code;
 }
 
-uint64_t align_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
+void clear_free_error() { t_err[0] = 0; }
 
 // [p, p + n) must be memory of `device` inside one allocation: the kernels
 // read or write every byte of it.  `what` names it in the error text.
@@ -53,15 +55,22 @@ ckpt_status check_range(const void* p, uint64_t n, int device, const char* what)
     return CKPT_OK;
 }
 
-// Restores the caller's current device on every return path.
-struct DeviceGuard {
-    int prev = -1;
-    bool set = false;
-    ~DeviceGuard()
-    {
-        if (set) (void)hipSetDevice(prev);
+ckpt_status enter_device(int32_t device, DeviceGuard& dg)
+{
+    int ndev = 0;
+    if (hipGetDeviceCount(&ndev) != hipSuccess || device < 0 || device >= ndev)
+        return fail_free(CKPT_EINVAL, "no device %d", device);
+    if (hipGetDevice(&dg.prev) != hipSuccess) return fail_free(CKPT_EHIP, "hipGetDevice failed");
+    if (dg.prev != device) {
+        if (hipSetDevice(device) != hipSuccess) return fail_free(CKPT_EHIP, "hipSetDevice(%d) failed", device);
+        dg.set = true;
     }
-};
+    return CKPT_OK;
+}
+
+namespace {
+
+uint64_t align_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 
 } // namespace
 
@@ -110,14 +119,7 @@ extern "C" ckpt_status ckpt_pack_noalloc(const ckpt_tensor* t, uint32_t n, uint6
         return fail_free(CKPT_EINVAL, "%llu sums for %llu chunks", (unsigned long long)sums_cap, (unsigned long long)nc);
 
     DeviceGuard dg;
-    int ndev = 0;
-    if (hipGetDeviceCount(&ndev) != hipSuccess || device < 0 || device >= ndev)
-        return fail_free(CKPT_EINVAL, "no device %d", device);
-    if (hipGetDevice(&dg.prev) != hipSuccess) return fail_free(CKPT_EHIP, "hipGetDevice failed");
-    if (dg.prev != device) {
-        if (hipSetDevice(device) != hipSuccess) return fail_free(CKPT_EHIP, "hipSetDevice(%d) failed", device);
-        dg.set = true;
-    }
+    if (ckpt_status st = enter_device(device, dg)) return st;
     for (uint32_t i = 0; i < n; ++i) {
         if (!t[i].nbytes) continue;
         char what[32];

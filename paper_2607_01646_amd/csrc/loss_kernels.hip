@@ -1,0 +1,699 @@
+// loss_kernels.hip -- gfx950 kernels of the vocabulary head's losses.
+//
+// Three products on the matrix cores, with what comes before and after them:
+//   logits    l = hidden weight^T           statistics of each row, the logits of a piece
+//   d_hidden  = d_logits weight             contraction over the words
+//   d_weight  = d_logits^T hidden           contraction over the tokens
+// each 2 tokens * vocab * dim operations, and the row kernel that turns a
+// piece's logits into their gradient.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "ops_internal.h"
+
+namespace ckpt {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef u16x4 u16x4_any __attribute__((aligned(2)));
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kInf = __builtin_inff();
+
+__device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ inline uint16_t bf16_of(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// An fp32 value as the sum of 3 bf16: each takes the next 8 bits of the
+// significand, cut off, not rounded, so the rests are exact and all 24 bits are
+// kept.  A value that is not finite is its first plane alone.
+__device__ inline void split3(float x, uint16_t (&p)[3])
+{
+    const uint32_t a = __float_as_uint(x) & 0xFFFF0000u;
+    p[0] = (uint16_t)(a >> 16);
+    if ((a & 0x7F800000u) == 0x7F800000u) {
+        if ((__float_as_uint(x) & 0x007FFFFFu) != 0) p[0] |= 0x40; // a NaN whose payload was cut off stays one
+        p[1] = p[2] = 0;
+        return;
+    }
+    const float r = x - __uint_as_float(a);
+    const uint32_t b = __float_as_uint(r) & 0xFFFF0000u;
+    p[1] = (uint16_t)(b >> 16);
+    p[2] = (uint16_t)(__float_as_uint(r - __uint_as_float(b)) >> 16);
+}
+
+// ---- tiles of an operand in LDS ----
+//
+// A tile is B rows by BK values of k, in 16-byte chunks that the loads write
+// straight to LDS, one wave 64 consecutive chunks at a time; which chunk of
+// global memory goes to a slot is chosen so that the reads below meet every
+// bank once.
+template <int B, int BK, bool ACROSS>
+struct Tile {
+    static constexpr int kElems = B * BK, kChunks = kElems / 8;
+
+    // k contiguous: rows of BK; a chunk moves by its row, which spreads the 16 rows that a quarter of a wave reads.
+    static __device__ inline uint32_t turn(uint32_t row)
+    {
+        constexpr uint32_t slots = BK / 8;
+        return (row / (16 / slots)) & (slots - 1);
+    }
+    // k across rows: BK rows of B; pairs of chunks (16 values) move by k, which spreads the 4 rows and 2 pairs
+    // that half a wave reads.
+    static __device__ inline uint32_t turn_pair(uint32_t k)
+    {
+        return B >= 128 ? (k & 3) << 1 : B == 64 ? (k & 2) : 0;
+    }
+
+    template <int THREADS>
+    static __device__ inline void load(const Operand& o, const uint16_t* base, uint32_t row0, uint32_t k0,
+                                       uint16_t* lds)
+    {
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int i = 0; i < (kChunks + THREADS - 1) / THREADS; ++i) {
+            const uint32_t s = i * THREADS + threadIdx.x;
+            if (kChunks % THREADS != 0 && i * THREADS + wave * 64 >= kChunks) break;
+            const uint16_t* src;
+            if constexpr (!ACROSS) {
+                const uint32_t r = s / (BK / 8), c = (s % (BK / 8)) ^ turn(r);
+                src = base + (uint64_t)min(row0 + r, o.rows - 1) * o.ld + k0 + c * 8;
+            } else {
+                const uint32_t k = s / (B / 8), at = s % (B / 8), c = ((at >> 1) ^ turn_pair(k)) << 1 | (at & 1);
+                src = base + (uint64_t)min(k0 + k, o.rows - 1) * o.ld + min(row0 + c * 8, o.cols - 8);
+            }
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                             (__attribute__((address_space(3))) void*)(lds + (i * THREADS + wave * 64) * 8),
+                                             16, 0, 0);
+        }
+    }
+
+    // The lane's 8 values of rows [r0, r0 + 32), k [16 step, 16 step + 16): row lane % 32, k 8 (lane / 32) + 0..7.
+    static __device__ inline bf16x8 read(const uint16_t* lds, uint32_t r0, uint32_t step)
+    {
+        const uint32_t lane = threadIdx.x & 63;
+        if constexpr (!ACROSS) {
+            const uint32_t r = r0 + (lane & 31), c = step * 2 + (lane >> 5);
+            return *(const bf16x8*)(lds + (r * (BK / 8) + (c ^ turn(r))) * 8);
+        } else {
+            // Transposing reads: 16 lanes name 4 rows of 16 values and each receives a column of them.
+            typedef __attribute__((address_space(3))) i16x4* Ptr;
+            i16x4 h[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t k = step * 16 + 8 * (lane >> 5) + 4 * u + ((lane >> 2) & 3);
+                const uint32_t pair = (r0 >> 4) + ((lane >> 4) & 1), half = (lane >> 1) & 1;
+                h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (Ptr)(lds + (k * (B / 8) + ((pair ^ turn_pair(k)) << 1 | half)) * 8 + (lane & 1) * 4));
+            }
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+// ---- epilogues ----
+//
+// acc[tp][tq] holds out[q][p] of 32 x 32 tiles: q = q0 + 32 tq + lane % 32 and, for register i,
+// p = p0 + 32 tp + 8 (i / 4) + 4 (lane / 32) + i % 4: every lane has runs of 4 consecutive p of one q.
+
+template <int TP, int TQ>
+__device__ inline void finish(const LogitsOut& o, f32x16 (&acc)[TP][TQ], uint32_t p0, uint32_t q0, uint32_t)
+{
+    static_assert(TP * 32 == kPartWords, "a wave's words are one part");
+    const uint32_t lane = threadIdx.x & 63, up = 4 * (lane >> 5);
+#pragma unroll
+    for (int tq = 0; tq < TQ; ++tq) {
+        const uint32_t q = q0 + 32 * tq + (lane & 31);
+        const bool here = q < o.tokens;
+        float top = -kInf;
+#pragma unroll
+        for (int tp = 0; tp < TP; ++tp)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t p = p0 + 32 * tp + 8 * (i >> 2) + up + (i & 3);
+                const float x = acc[tp][tq][i];
+                top = p < o.vocab ? fmaxf(top, x) : top; // fmaxf passes a NaN by; the sum below does not
+            }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float low = top == -kInf ? 0.0f : top;
+        float sum = 0, sum_t = 0;
+#pragma unroll
+        for (int tp = 0; tp < TP; ++tp)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t p = p0 + 32 * tp + 8 * (i >> 2) + up + (i & 3);
+                const float x = acc[tp][tq][i] - low;
+                sum += p < o.vocab ? exp_of(x) : 0.0f;
+                if (o.part_t) sum_t += p < o.vocab ? exp_of(x * o.inv_t) : 0.0f;
+            }
+        sum += __shfl_xor(sum, 32);
+        if (o.part_t) sum_t += __shfl_xor(sum_t, 32);
+        if (here && lane < 32 && p0 < o.vocab) {
+            const uint64_t at = (uint64_t)(p0 / kPartWords) * o.tokens + q;
+            o.part[at] = make_float2(top, sum);
+            if (o.part_t) o.part_t[at] = sum_t;
+        }
+        if (o.target && here) {
+            const int64_t t = o.target[q] - p0;
+            if (t >= 0 && t < TP * 32) {
+#pragma unroll
+                for (int tp = 0; tp < TP; ++tp)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if ((uint32_t)t == 32u * tp + 8 * (i >> 2) + up + (i & 3) && p0 + t < o.vocab)
+                            o.target_logit[q] = acc[tp][tq][i];
+            }
+        }
+        if (o.logits && here) {
+            float* row = o.logits + (uint64_t)q * o.ld;
+#pragma unroll
+            for (int tp = 0; tp < TP; ++tp)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const uint32_t p = p0 + 32 * tp + 8 * (i >> 2) + up;
+                    if (p < o.vocab) // ld covers whole runs
+                        *(f32x4*)(row + p) = {acc[tp][tq][i], acc[tp][tq][i + 1], acc[tp][tq][i + 2], acc[tp][tq][i + 3]};
+                }
+        }
+    }
+}
+
+struct GradEnd {
+    GradOut o;
+    uint32_t p, q;
+};
+
+template <int TP, int TQ>
+__device__ inline void finish(const GradEnd& e, f32x16 (&acc)[TP][TQ], uint32_t p0, uint32_t q0, uint32_t slice)
+{
+    const GradOut& o = e.o;
+    const uint32_t lane = threadIdx.x & 63, up = 4 * (lane >> 5);
+    const float scale = o.scale ? *o.scale : 1.0f;
+#pragma unroll
+    for (int tq = 0; tq < TQ; ++tq) {
+        const uint32_t q = q0 + 32 * tq + (lane & 31);
+        if (q >= e.q) continue;
+#pragma unroll
+        for (int tp = 0; tp < TP; ++tp)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const uint32_t p = p0 + 32 * tp + 8 * (i >> 2) + up;
+                if (p >= e.p) continue;
+                const uint32_t n = min(4u, e.p - p);
+                f32x4 x = {acc[tp][tq][i], acc[tp][tq][i + 1], acc[tp][tq][i + 2], acc[tp][tq][i + 3]};
+                if (o.add) {
+                    const float* add = o.add + (uint64_t)q * o.add_ld + p;
+                    for (uint32_t j = 0; j < 4; ++j)
+                        if (j < n) x[j] += add[j];
+                }
+                x *= scale;
+                const uint64_t at = (uint64_t)slice * o.slice + (uint64_t)q * o.ld + p;
+                if (o.f32) {
+                    float* out = (float*)o.out + at;
+                    if (n == 4)
+                        *(f32x4_any*)out = x;
+                    else
+                        for (uint32_t j = 0; j < 3; ++j)
+                            if (j < n) out[j] = x[j];
+                } else {
+                    uint16_t* out = (uint16_t*)o.out + at;
+                    const u16x4 u = {bf16_of(x[0]), bf16_of(x[1]), bf16_of(x[2]), bf16_of(x[3])};
+                    if (n == 4)
+                        *(u16x4_any*)out = u;
+                    else
+                        for (uint32_t j = 0; j < 3; ++j)
+                            if (j < n) out[j] = u[j];
+                }
+            }
+    }
+}
+
+// ---- the product ----
+//
+// A workgroup of NWP x NWQ waves makes a BP x BQ tile of out[q][p] = sum_k P(p, k) Q(q, k), each wave a part of it in
+// registers.  Two buffers in LDS: while one is multiplied the loads of the next BK values of k write the other one.
+// PLANES = 3: fp32 operands as 3 bf16 planes; of the 9 products of planes the 6 whose sum of indexes is at most 2
+// are made (the others are below 2^-24 of the value), smallest first.
+template <int PLANES, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, class End>
+__global__ __launch_bounds__(NWP* NWQ * 64) void product_kernel(const Operand P, const Operand Q,
+                                                                const ProductShape shape, const End end)
+{
+    constexpr int kThreads = NWP * NWQ * 64;
+    constexpr int TP = BP / NWP / 32, TQ = BQ / NWQ / 32;
+    using TileP = Tile<BP, BK, PA>;
+    using TileQ = Tile<BQ, BK, QA>;
+    constexpr int kBuffer = PLANES * (TileP::kElems + TileQ::kElems);
+    __shared__ __attribute__((aligned(16))) uint16_t s0[kBuffer], s1[kBuffer];
+
+    const uint32_t np = (shape.p + BP - 1) / BP;
+    const uint32_t bp = blockIdx.x % np, bq = blockIdx.x / np;
+    const uint32_t p0 = bp * BP, q0 = bq * BQ;
+    const uint32_t steps = shape.k / BK;
+    const uint32_t first = (uint32_t)((uint64_t)steps * blockIdx.y / shape.slices);
+    const uint32_t last = (uint32_t)((uint64_t)steps * (blockIdx.y + 1) / shape.slices);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wp = (wave % NWP) * (BP / NWP), wq = (wave / NWP) * (BQ / NWQ);
+
+    f32x16 acc[TP][TQ];
+#pragma unroll
+    for (int a = 0; a < TP; ++a)
+#pragma unroll
+        for (int b = 0; b < TQ; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0;
+
+    auto load = [&](uint16_t* s, uint32_t step) {
+#pragma unroll
+        for (int z = 0; z < PLANES; ++z) {
+            TileP::template load<kThreads>(P, P.base + z * P.plane, p0, step * BK, s + z * TileP::kElems);
+            TileQ::template load<kThreads>(Q, Q.base + z * Q.plane, q0, step * BK,
+                                           s + PLANES * TileP::kElems + z * TileQ::kElems);
+        }
+    };
+    auto multiply = [&](const uint16_t* s) {
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k) {
+            bf16x8 a[PLANES][TP], b[PLANES][TQ];
+#pragma unroll
+            for (int z = 0; z < PLANES; ++z) {
+#pragma unroll
+                for (int t = 0; t < TP; ++t) a[z][t] = TileP::read(s + z * TileP::kElems, wp + 32 * t, k);
+#pragma unroll
+                for (int t = 0; t < TQ; ++t)
+                    b[z][t] = TileQ::read(s + PLANES * TileP::kElems + z * TileQ::kElems, wq + 32 * t, k);
+            }
+#pragma unroll
+            for (int sum = PLANES - 1; sum >= 0; --sum)
+#pragma unroll
+                for (int z = 0; z <= sum; ++z)
+#pragma unroll
+                    for (int t = 0; t < TP; ++t)
+#pragma unroll
+                        for (int u = 0; u < TQ; ++u)
+                            acc[t][u] =
+                                __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[z][t], b[sum - z][u], acc[t][u], 0, 0, 0);
+        }
+    };
+    // The wave's own loads have landed; then everyone's.
+    auto landed = [&] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+
+    if (first < last) {
+        load(s0, first);
+        for (uint32_t step = first; step < last; step += 2) {
+            landed();
+            if (step + 1 < last) load(s1, step + 1);
+            multiply(s0);
+            if (step + 1 >= last) break;
+            landed();
+            if (step + 2 < last) load(s0, step + 2);
+            multiply(s1);
+        }
+    }
+    finish<TP, TQ>(end, acc, p0 + wp, q0 + wq, blockIdx.y);
+}
+
+template <int PLANES, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, class End>
+hipError_t launch_product(const Operand& P, const Operand& Q, const ProductShape& s, const End& end, hipStream_t stream)
+{
+    const uint64_t tiles = (uint64_t)((s.p + BP - 1) / BP) * ((s.q + BQ - 1) / BQ);
+    if (tiles == 0 || tiles > 0x7fffffff || s.slices == 0 || s.slices > 65535 || s.k % BK) return hipErrorInvalidValue;
+    product_kernel<PLANES, PA, QA, BP, BQ, NWP, NWQ, BK, End>
+        <<<dim3((uint32_t)tiles, s.slices), NWP * NWQ * 64, 0, stream>>>(P, Q, s, end);
+    return hipGetLastError();
+}
+
+// ---- rows ----
+
+__device__ inline float load1(const void* p, uint64_t at, bool f32)
+{
+    return f32 ? ((const float*)p)[at] : __uint_as_float((uint32_t)((const uint16_t*)p)[at] << 16);
+}
+
+constexpr int kRowThreads = 256;
+
+__device__ inline float wave_max(float x)
+{
+    for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+    return x;
+}
+__device__ inline float wave_sum(float x)
+{
+    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+}
+template <int WAVES>
+__device__ inline float block_max(float x, float* s)
+{
+    x = wave_max(x);
+    if (WAVES == 1) return x;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) x = fmaxf(x, s[w]);
+    return x;
+}
+template <int WAVES>
+__device__ inline float block_sum(float x, float* s)
+{
+    x = wave_sum(x);
+    if (WAVES == 1) return x;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0;
+    for (int w = 0; w < WAVES; ++w) x += s[w];
+    return x;
+}
+
+// A teacher entry that is there: a word, and any logit but -inf.
+__device__ inline bool entry(const LossRows& r, uint64_t n, uint32_t k, int64_t* word, float* logit)
+{
+    *word = r.t_index[n * r.t_index_ld + k];
+    *logit = load1(r.t_logits, n * r.t_logits_ld + k, r.t_f32);
+    return *word >= 0 && *logit != -kInf;
+}
+
+// One wave a row.
+__global__ __launch_bounds__(kRowThreads) void prepare_kernel(const LossRows r, bool weigh, uint32_t row0, uint32_t rows,
+                                                              const RowCopy c)
+{
+    const uint32_t lane = threadIdx.x & 63, row = blockIdx.x * (kRowThreads / 64) + (threadIdx.x >> 6);
+    bool counts = row < rows;
+    if (weigh && counts) {
+        const uint64_t n = row0 + row;
+        const float w = r.token_weight ? r.token_weight[n] : 1.0f;
+        counts = r.target && r.alpha < 1 && r.target[n] != r.ignore_index;
+        for (uint32_t k = lane; k < r.topk && r.alpha > 0; k += 64) {
+            int64_t word;
+            float logit;
+            counts |= entry(r, n, k, &word, &logit);
+        }
+        counts = __ballot(counts) != 0 && w != 0;
+        if (lane == 0) r.row_weight[n] = counts ? w : 0.0f;
+    }
+    if (!c.src || row >= c.dst_rows) return;
+    const uint64_t src = (uint64_t)(row0 + row) * c.src_ld;
+    uint16_t* dst = c.dst + (uint64_t)row * c.dst_cols;
+    for (uint32_t at = 4 * lane; at < c.dst_cols; at += 256) { // dst_cols: a multiple of 64
+        if (c.f32) {
+            uint16_t x[4][3];
+            for (int j = 0; j < 4; ++j)
+                split3(counts && at + j < c.cols ? ((const float*)c.src)[src + at + j] : 0.0f, x[j]);
+            for (int z = 0; z < 3; ++z) *(u16x4*)(dst + z * c.plane + at) = {x[0][z], x[1][z], x[2][z], x[3][z]};
+        } else {
+            u16x4 x = {0, 0, 0, 0};
+            const uint16_t* from = (const uint16_t*)c.src + src + at;
+            if (counts && at + 4 <= c.cols)
+                x = *(const u16x4_any*)from;
+            else if (counts)
+                for (int j = 0; j < 3; ++j)
+                    if (at + j < c.cols) x[j] = from[j];
+            *(u16x4*)(dst + at) = x;
+        }
+    }
+}
+
+// One workgroup a row: its log-sum-exp and loss and, with d_logits, its row of
+//   w (alpha T (p^T - q) + (1 - alpha) (p - 1_y)).
+// The factor that all rows share (grad_scale and the mean's) is left to the products' fp32 sums: here the label's term
+// is near -1 for most tokens of a new model, which bf16 holds exactly, and -1/tokens would be rounded the same way in
+// all of them.  Rounding d_logits to bf16 (fp32: to 3 planes, that is not at all) is what feeds the matrix cores; its
+// errors are independent from word to word and of the size of the gradients' own rounding.
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, const LossPiece p)
+{
+    extern __shared__ float s_entries[]; // topk weights q, then topk words
+    __shared__ float s_wave[WAVES];
+    constexpr uint32_t kThreads = WAVES * 64;
+    const uint32_t row = blockIdx.x, tid = threadIdx.x;
+    const uint64_t n = p.row0 + (uint64_t)row;
+    const float weight = row < p.rows ? r.row_weight[n] : 0.0f;
+    uint16_t* dl = p.d_logits ? p.d_logits + (uint64_t)row * p.dl_ld : nullptr;
+    const uint32_t planes = p.f32 ? 3 : 1;
+    if (weight == 0) {
+        if (row < p.rows && tid == 0) {
+            r.token_loss[n] = 0;
+            r.lse[n] = 0;
+        }
+        if (dl)
+            for (uint32_t z = 0; z < planes; ++z)
+                for (uint64_t v = 4 * tid; v < p.dl_ld; v += 4 * kThreads) *(u16x4*)(dl + z * p.dl_plane + v) = {0, 0, 0, 0};
+        return;
+    }
+    const bool teach = r.alpha > 0;
+    const float inv_t = 1 / r.temperature;
+    float top = -kInf;
+    for (uint32_t k = tid; k < p.parts; k += kThreads) top = fmaxf(top, p.part[(uint64_t)k * p.part_ld + row].x);
+    top = block_max<WAVES>(top, s_wave);
+    const float low = top == -kInf ? 0.0f : top;
+    float sum = 0, sum_t = 0;
+    for (uint32_t k = tid; k < p.parts; k += kThreads) {
+        const uint64_t at = (uint64_t)k * p.part_ld + row;
+        const float2 x = p.part[at];
+        if (x.x == -kInf && x.y == 0) continue;
+        sum += x.y * exp_of(x.x - low);
+        if (p.part_t) sum_t += p.part_t[at] * exp_of((x.x - low) * inv_t);
+    }
+    sum = block_sum<WAVES>(sum, s_wave);
+    const float lse = low + __builtin_amdgcn_logf(sum) * kLn2;
+    float lse_t = lse;
+    if (p.part_t) {
+        sum_t = block_sum<WAVES>(sum_t, s_wave);
+        lse_t = low * inv_t + __builtin_amdgcn_logf(sum_t) * kLn2;
+    }
+    const float* logits = p.logits + (uint64_t)row * p.ld;
+
+    float loss = 0, hard = 0;
+    int64_t label = -1;
+    if (r.target && r.alpha < 1 && (label = r.target[n]) != r.ignore_index) {
+        const bool word = label >= 0 && label < r.vocab;
+        hard = word ? 1 - r.alpha : __builtin_nanf(""); // the loss and the gradient show a label that is no word
+        loss = word ? hard * (lse - r.target_logit[n]) : hard;
+    } else {
+        label = -1;
+    }
+    float soft = 0;
+    float* s_q = s_entries;
+    int* s_word = (int*)(s_entries + r.topk);
+    if (teach) {
+        // q over the entries that are there
+        int64_t word;
+        float t, t_top = -kInf, t_sum = 0;
+        constexpr float kBad = 4096; // above the entries a row can have
+        for (uint32_t k = tid; k < r.topk; k += kThreads)
+            if (entry(r, n, k, &word, &t)) {
+                t_top = fmaxf(t_top, t);
+                t_sum += word < r.vocab ? 1 : kBad;
+            }
+        t_top = block_max<WAVES>(t_top, s_wave);
+        const float count = block_sum<WAVES>(t_sum, s_wave);
+        const bool any = count > 0, bad = count >= kBad;
+        t_sum = 0;
+        for (uint32_t k = tid; k < r.topk; k += kThreads) {
+            const bool there = entry(r, n, k, &word, &t);
+            const float e = there ? exp_of((t - t_top) * inv_t) : 0.0f;
+            s_q[k] = e;
+            s_word[k] = there && word < r.vocab ? (int)word : -1;
+            t_sum += e;
+        }
+        t_sum = block_sum<WAVES>(t_sum, s_wave);
+        const float log_sum = __builtin_amdgcn_logf(t_sum) * kLn2;
+        float kd = 0;
+        for (uint32_t k = tid; k < r.topk; k += kThreads) {
+            const float q = s_q[k] / t_sum;
+            s_q[k] = any ? q : 0.0f;
+            if (s_word[k] < 0 || q == 0) continue;
+            entry(r, n, k, &word, &t);
+            kd += q * (((t - t_top) * inv_t - log_sum) - (logits[s_word[k]] * inv_t - lse_t));
+        }
+        kd = block_sum<WAVES>(kd, s_wave);
+        if (any) {
+            soft = bad ? __builtin_nanf("") : r.alpha * r.temperature;
+            loss += soft * r.temperature * kd;
+        }
+    }
+    if (tid == 0) {
+        r.token_loss[n] = loss;
+        r.lse[n] = teach ? lse_t : lse;
+    }
+    if (!dl) return;
+
+    const float soft_w = weight * soft, hard_w = weight * hard;
+    auto gradient = [&](uint32_t v, float l) {
+        float g = 0;
+        if (hard != 0) g = hard_w * (exp_of(l - lse) - (v == (uint64_t)label ? 1.0f : 0.0f));
+        if (soft != 0) g += soft_w * exp_of(l * inv_t - lse_t);
+        return g;
+    };
+    auto put = [&](uint32_t v, float g) {
+        if (p.f32) {
+            uint16_t x[3];
+            split3(g, x);
+            for (int z = 0; z < 3; ++z) dl[z * p.dl_plane + v] = x[z];
+        } else {
+            dl[v] = bf16_of(g);
+        }
+    };
+    for (uint32_t v = 4 * tid; v < p.dl_ld; v += 4 * kThreads) {
+        f32x4 g = {0, 0, 0, 0};
+        if (v < r.vocab) {
+            const f32x4 l = *(const f32x4*)(logits + v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) g[j] = v + j < r.vocab ? gradient(v + j, l[j]) : 0.0f;
+        }
+        if (p.f32) {
+            uint16_t x[4][3];
+            for (int j = 0; j < 4; ++j) split3(g[j], x[j]);
+            for (int z = 0; z < 3; ++z) *(u16x4*)(dl + z * p.dl_plane + v) = {x[0][z], x[1][z], x[2][z], x[3][z]};
+        } else {
+            *(u16x4*)(dl + v) = {bf16_of(g[0]), bf16_of(g[1]), bf16_of(g[2]), bf16_of(g[3])};
+        }
+    }
+    if (soft == 0) return;
+    // The teacher's words once more, each by the first of its entries, when the stores above have been made.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    for (uint32_t k = tid; k < r.topk; k += kThreads) {
+        const int word = s_word[k];
+        if (word < 0) continue;
+        float q = 0;
+        bool first = true;
+        for (uint32_t j = 0; j < r.topk; ++j) {
+            if (s_word[j] != word) continue;
+            first &= j >= k;
+            q += s_q[j];
+        }
+        if (first) put(word, gradient(word, logits[word]) - soft_w * q);
+    }
+}
+
+__global__ __launch_bounds__(1024) void finish_kernel(const LossRows r, bool total)
+{
+    __shared__ double s[2][16];
+    double weight = 0, loss = 0;
+    for (uint32_t n = threadIdx.x; n < r.tokens; n += 1024) {
+        const float w = r.row_weight[n];
+        weight += w;
+        if (total && w != 0) loss += (double)w * r.token_loss[n];
+    }
+    for (int o = 32; o; o >>= 1) {
+        weight += __shfl_xor(weight, o);
+        loss += __shfl_xor(loss, o);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        s[0][threadIdx.x >> 6] = weight;
+        s[1][threadIdx.x >> 6] = loss;
+    }
+    __syncthreads();
+    if (threadIdx.x) return;
+    weight = loss = 0;
+    for (int w = 0; w < 16; ++w) {
+        weight += s[0][w];
+        loss += s[1][w];
+    }
+    const double over = r.mean ? (weight != 0 ? 1 / weight : 0.0) : 1.0;
+    *r.scale = (float)(over * (r.grad_scale ? *r.grad_scale : 1.0f));
+    if (total) *r.loss = (float)(loss * over);
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(void* out, uint32_t rows, uint32_t cols, uint64_t ld, bool f32)
+{
+    for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x)
+        for (uint32_t c = threadIdx.x; c < cols; c += 256)
+            if (f32)
+                ((float*)out)[row * ld + c] = 0;
+            else
+                ((uint16_t*)out)[row * ld + c] = 0;
+}
+
+__global__ __launch_bounds__(256) void join_kernel(const float* slices, uint32_t n, uint32_t p, uint32_t q, const GradOut o)
+{
+    const uint64_t count = (uint64_t)p * q, at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= count) return;
+    float x = 0;
+    for (uint32_t k = 0; k < n; ++k) x += slices[k * count + at];
+    x *= o.scale ? *o.scale : 1.0f;
+    const uint64_t to = at / p * o.ld + at % p;
+    if (o.f32)
+        ((float*)o.out)[to] = x;
+    else
+        ((uint16_t*)o.out)[to] = bf16_of(x);
+}
+
+} // namespace
+
+hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape& s, uint32_t planes,
+                         const LogitsOut& o, hipStream_t stream)
+{
+    return planes == 3 ? launch_product<3, false, false, 128, 128, 2, 2, 32>(w, h, s, o, stream)
+                       : launch_product<1, false, false, 128, 128, 2, 2, 64>(w, h, s, o, stream);
+}
+
+hipError_t launch_d_hidden(const Operand& w, const Operand& dl, const ProductShape& s, uint32_t planes,
+                           const GradOut& o, hipStream_t stream)
+{
+    const GradEnd end = {o, s.p, s.q};
+    return planes == 3 ? launch_product<3, true, false, 128, 128, 2, 2, 32>(w, dl, s, end, stream)
+                       : launch_product<1, true, false, 128, 128, 2, 2, 64>(w, dl, s, end, stream);
+}
+
+hipError_t launch_d_weight(const Operand& h, const Operand& dl, const ProductShape& s, uint32_t planes,
+                           const GradOut& o, hipStream_t stream)
+{
+    const GradEnd end = {o, s.p, s.q};
+    return planes == 3 ? launch_product<3, true, true, 128, 128, 2, 2, 32>(h, dl, s, end, stream)
+                       : launch_product<1, true, true, 128, 128, 2, 2, 64>(h, dl, s, end, stream);
+}
+
+uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t, uint32_t most)
+{
+    const uint64_t tiles = (uint64_t)((p + 127) / 128) * ((q + 127) / 128);
+    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({512 / tiles, k / 256, most, 64}));
+}
+
+hipError_t launch_join(const float* slices, uint32_t n, uint32_t p, uint32_t q, const GradOut& o, hipStream_t stream)
+{
+    const uint64_t blocks = ((uint64_t)p * q + 255) / 256;
+    if (blocks == 0 || blocks > 0x7fffffff) return hipErrorInvalidValue;
+    join_kernel<<<(uint32_t)blocks, 256, 0, stream>>>(slices, n, p, q, o);
+    return hipGetLastError();
+}
+
+hipError_t launch_zero(void* out, uint32_t rows, uint32_t cols, uint64_t ld, bool f32, hipStream_t stream)
+{
+    zero_kernel<<<std::min(rows, 16384u), 256, 0, stream>>>(out, rows, cols, ld, f32);
+    return hipGetLastError();
+}
+
+hipError_t launch_prepare(const LossRows* r, uint32_t row0, uint32_t rows, const RowCopy& c, hipStream_t stream)
+{
+    const uint32_t all = c.src ? std::max(rows, c.dst_rows) : rows;
+    if (all == 0) return hipSuccess;
+    prepare_kernel<<<(all + 3) / 4, kRowThreads, 0, stream>>>(r ? *r : LossRows(), r != nullptr, row0, rows, c);
+    return hipGetLastError();
+}
+
+hipError_t launch_rows(const LossRows& r, const LossPiece& p, hipStream_t stream)
+{
+    const uint32_t all = p.d_logits ? std::max(p.rows, p.dl_rows) : p.rows;
+    if (all == 0) return hipSuccess;
+    rows_kernel<4><<<all, 256, r.topk * 8, stream>>>(r, p);
+    return hipGetLastError();
+}
+
+hipError_t launch_finish(const LossRows& r, bool total, hipStream_t stream)
+{
+    finish_kernel<<<1, 1024, 0, stream>>>(r, total);
+    return hipGetLastError();
+}
+
+} // namespace ckpt

@@ -1,0 +1,154 @@
+// Internal interface between the training-step operators (ckpt_ops.cpp) and
+// their gfx950 kernels.  Not installed; the public ABI is include/ckpt_ops.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ckpt {
+
+// ---- products on the matrix cores (loss_kernels.hip) ----
+
+// One operand of out[q][p] = sum_k P(p, k) Q(q, k): bf16, as 1 plane or as the
+// 3 whose sum is an fp32 value.  Rows are 16-byte aligned (base and ld).
+//   k contiguous:     element (r, k) at base[r * ld + k]; row indices are
+//                     clamped below `rows`, k runs to a multiple of 64
+//   k across rows:    element (r, k) at base[k * ld + r]; k is clamped below
+//                     `rows`, r to `cols`, a multiple of 8
+// What a clamp repeats only reaches outputs that are not written, or meets
+// zeros of the other operand.
+struct Operand {
+    const uint16_t* base;
+    uint64_t plane; // elements between planes
+    uint64_t ld;
+    uint32_t rows, cols;
+};
+
+struct ProductShape {
+    uint32_t p, q, k; // k: a multiple of 64
+    uint32_t slices;  // k is cut into this many runs, each a product of its own
+};
+
+// What becomes of a tile of l = P Q: the logits' statistics.
+struct LogitsOut {
+    uint32_t vocab, tokens;
+    const int64_t* target; // or nullptr
+    float* target_logit;   // [tokens], written where the target is a word
+    float2* part;          // [parts][tokens]: (max, sum exp(l - max)) over each run of kPartWords words
+    float* part_t;         // the same sum at 1/temperature, or nullptr
+    float inv_t;
+    float* logits; // [tokens][ld], or nullptr
+    uint64_t ld;
+};
+constexpr uint32_t kPartWords = 64;
+
+// What becomes of a product that is a gradient (or a slice of one).
+struct GradOut {
+    const float* scale; // multiplies the sum; nullptr = 1
+    const float* add;   // [q][add_ld] added to the product before the scale, or nullptr
+    uint64_t add_ld;
+    void* out; // [q][ld]; with slices > 1: fp32 [slices][q][ld]
+    uint64_t ld, slice;
+    bool f32; // type of out
+};
+
+hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape& s, uint32_t planes,
+                         const LogitsOut& o, hipStream_t stream);
+// d_hidden: P = weight (k = words across rows), Q = d_logits (k contiguous)
+hipError_t launch_d_hidden(const Operand& w, const Operand& dl, const ProductShape& s, uint32_t planes,
+                           const GradOut& o, hipStream_t stream);
+// d_weight: P = hidden, Q = d_logits (both with k = tokens across rows)
+hipError_t launch_d_weight(const Operand& h, const Operand& dl, const ProductShape& s, uint32_t planes,
+                           const GradOut& o, hipStream_t stream);
+// out = scale * sum of the slices (fp32 [slices][q][p], dense)
+hipError_t launch_join(const float* slices, uint32_t n, uint32_t p, uint32_t q, const GradOut& o, hipStream_t stream);
+hipError_t launch_zero(void* out, uint32_t rows, uint32_t cols, uint64_t ld, bool f32, hipStream_t stream);
+// The run count that fills the GPU, at most most.
+uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t planes, uint32_t most);
+
+// ---- rows of the loss (loss_kernels.hip) ----
+
+struct LossRows {
+    uint32_t tokens, vocab;
+    const int64_t* target; // or nullptr
+    int64_t ignore_index;
+    const float* token_weight; // or nullptr
+    uint32_t topk;
+    const int64_t* t_index;
+    uint64_t t_index_ld;
+    const void* t_logits;
+    uint64_t t_logits_ld;
+    bool t_f32;
+    float temperature, alpha; // alpha: 0 without a teacher
+    float* row_weight;        // [tokens]: the weight of a row that counts, else 0
+    float* target_logit;
+    float *token_loss, *lse;
+    float *loss, *scale; // scalars: the loss; grad_scale over the weights' sum
+    const float* grad_scale;
+    bool mean;
+};
+
+// Copies rows [row0, row0 + rows) of src, fp32 into 3 planes, with zeros to
+// the width dst_cols and in rows up to dst_rows; src == nullptr copies
+// nothing.  With r != nullptr also computes row_weight of those rows, and
+// copies rows that do not count as zeros.
+struct RowCopy {
+    const void* src;
+    uint64_t src_ld;
+    uint32_t cols;
+    bool f32;
+    uint16_t* dst;
+    uint64_t plane;
+    uint32_t dst_cols, dst_rows;
+};
+hipError_t launch_prepare(const LossRows* r, uint32_t row0, uint32_t rows, const RowCopy& c, hipStream_t stream);
+
+// From the statistics of `parts` runs of words to token_loss and lse of rows
+// [row0, row0 + rows); part, part_t and logits are the piece's own.  With
+// d_logits also writes its rows ([3 planes where f32][.][dl_ld], dl_rows of
+// them: zeros beyond the vocabulary and beyond `rows`).
+struct LossPiece {
+    uint32_t row0, rows, parts;
+    uint32_t part_ld; // rows between two parts
+    const float2* part;
+    const float* part_t;
+    const float* logits;
+    uint64_t ld;
+    uint16_t* d_logits;
+    uint64_t dl_ld, dl_plane;
+    uint32_t dl_rows;
+    bool f32;
+};
+hipError_t launch_rows(const LossRows& r, const LossPiece& p, hipStream_t stream);
+// scale (from row_weight) and, if `total`, the loss.
+hipError_t launch_finish(const LossRows& r, bool total, hipStream_t stream);
+
+// ---- optimizer (optim_kernels.hip) ----
+
+constexpr uint32_t kAdamFrags = 64; // per launch; their tiles' first numbers fit one wave
+struct AdamArgs {
+    struct {
+        uint64_t param, master, m, v, grad, numel;
+    } f[kAdamFrags];
+    uint32_t first[kAdamFrags]; // first tile of each fragment
+    uint32_t count, tiles;
+    float beta1, one_beta1, beta2, one_beta2, keep, lr, inv_bc1, inv_bc2, eps;
+    const float* scale;
+};
+constexpr uint32_t kAdamTile = 2048;
+hipError_t launch_adamw(const AdamArgs& a, bool param_f32, bool grad_f32, hipStream_t stream);
+
+constexpr uint32_t kNormFrags = 160;
+struct NormArgs {
+    struct {
+        uint64_t ptr, numel;
+    } f[kNormFrags];
+    uint32_t first[kNormFrags];
+    uint32_t count, tiles;
+};
+constexpr uint32_t kNormTile = 8192, kNormBlocks = 2048;
+// Adds the fragments' squares to part (kNormBlocks sums; `fresh`: stores them).
+hipError_t launch_norm(const NormArgs& a, bool f32, bool fresh, double* part, hipStream_t stream);
+hipError_t launch_norm_finish(const double* part, double max_norm, float* out, hipStream_t stream);
+
+} // namespace ckpt
