@@ -60,7 +60,7 @@ extern "C" {
 typedef struct {
     uint32_t dtype;     /* CKPT_TYPE_*: hidden, weight and their gradients */
     uint32_t reduction; /* CKPT_LOSS_* */
-    uint64_t tokens, dim, vocab; /* tokens may be 0; each below 2^31, topk at most 1024 */
+    uint64_t tokens, dim, vocab; /* tokens below 2^31 (0 is allowed), the others 1 to 2^22 */
     const void* hidden; /* [tokens, dim], rows hidden_stride elements apart */
     uint64_t hidden_stride;
     const void* weight; /* [vocab, dim] */
@@ -68,7 +68,7 @@ typedef struct {
     const int64_t* target; /* [tokens]; NULL where the cross entropy has no share */
     int64_t ignore_index;
     const float* token_weight; /* [tokens] or NULL (1 for each) */
-    uint32_t topk;             /* teacher entries a token; 0 = cross entropy alone */
+    uint32_t topk;             /* teacher entries a token, at most 1024; 0 = cross entropy alone */
     uint32_t teacher_dtype;    /* CKPT_TYPE_* of teacher_logits */
     const int64_t* teacher_index; /* [tokens, topk] */
     uint64_t teacher_index_stride;

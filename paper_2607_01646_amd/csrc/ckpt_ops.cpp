@@ -11,7 +11,8 @@
 namespace ckpt {
 namespace {
 
-constexpr uint64_t kMost = 0x7fffffffull; // of tokens, dim, vocab
+constexpr uint64_t kMost = 0x7fffffffull;  // tokens
+constexpr uint64_t kMostWidth = 1ull << 22; // dim, vocab: a tile's rows of an operand stay within 31 bits of bytes
 constexpr uint64_t kDefaultPiece = 2ull << 30;
 constexpr uint64_t kSliceBytes = 256ull << 20; // of the partial sums of a product cut along k
 
@@ -40,8 +41,8 @@ ckpt_status check_loss(const ckpt_linear_loss_args* a)
         return fail_free(CKPT_EINVAL, "hidden and weight are bf16 or fp32, not type %u", a->dtype);
     if (a->reduction != CKPT_LOSS_MEAN && a->reduction != CKPT_LOSS_SUM)
         return fail_free(CKPT_EINVAL, "no reduction %u", a->reduction);
-    if (a->tokens > kMost || a->dim == 0 || a->dim > kMost || a->vocab == 0 || a->vocab > kMost)
-        return fail_free(CKPT_EINVAL, "%llu tokens, %llu wide, %llu words: each below 2^31, and width and words above 0",
+    if (a->tokens > kMost || a->dim == 0 || a->dim > kMostWidth || a->vocab == 0 || a->vocab > kMostWidth)
+        return fail_free(CKPT_EINVAL, "%llu tokens, %llu wide, %llu words: below 2^31, and 1 to 2^22 each",
                          (unsigned long long)a->tokens, (unsigned long long)a->dim, (unsigned long long)a->vocab);
     if (a->topk > 1024) return fail_free(CKPT_EINVAL, "%u teacher entries: at most 1024", a->topk);
     if (a->topk) {
@@ -72,7 +73,7 @@ LossPlan plan_loss(const ckpt_linear_loss_args* a)
     l.two_sums = l.teach && a->temperature != 1;
     l.parts = (uint32_t)up(v, kPartWords) / kPartWords;
     const auto direct = [&](const void* p, uint64_t ld) { // as it is fit for the loads of a product
-        return !f32 && d % 64 == 0 && ld % 8 == 0 && (uintptr_t)p % 16 == 0;
+        return !f32 && d % 64 == 0 && ld % 8 == 0 && ld <= kMostWidth && (uintptr_t)p % 16 == 0;
     };
     l.copy_weight = !direct(a->weight, a->weight_stride);
     // With gradients the hidden states are copied so that those of rows that do not count are zero: the products over

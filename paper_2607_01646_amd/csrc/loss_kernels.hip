@@ -71,27 +71,47 @@ struct Tile {
         return B >= 128 ? (k & 3) << 1 : B == 64 ? (k & 2) : 0;
     }
 
+    // Load instructions of a wave.
     template <int THREADS>
-    static __device__ inline void load(const Operand& o, const uint16_t* base, uint32_t row0, uint32_t k0,
-                                       uint16_t* lds)
+    static constexpr int loads()
     {
-        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-        for (int i = 0; i < (kChunks + THREADS - 1) / THREADS; ++i) {
-            const uint32_t s = i * THREADS + threadIdx.x;
-            if (kChunks % THREADS != 0 && i * THREADS + wave * 64 >= kChunks) break;
-            const uint16_t* src;
+        return (kChunks + THREADS - 1) / THREADS;
+    }
+    // What a lane keeps for its loads: byte offsets from the tile's first row (below 2^31: 256 rows of 2^22 values), or
+    // for k across rows the column's, which all its loads share.
+    template <int THREADS>
+    struct Lane {
+        uint32_t off[ACROSS ? 1 : loads<THREADS>()];
+        __device__ inline Lane(const Operand& o, uint32_t row0)
+        {
             if constexpr (!ACROSS) {
-                const uint32_t r = s / (BK / 8), c = (s % (BK / 8)) ^ turn(r);
-                src = base + (uint64_t)min(row0 + r, o.rows - 1) * o.ld + k0 + c * 8;
+#pragma unroll
+                for (int i = 0; i < loads<THREADS>(); ++i) {
+                    const uint32_t s = i * THREADS + threadIdx.x, r = s / (BK / 8), c = (s % (BK / 8)) ^ turn(r);
+                    off[i] = (min(row0 + r, o.rows - 1) - row0) * (uint32_t)o.ld * 2 + c * 16;
+                }
             } else {
-                const uint32_t k = s / (B / 8), at = s % (B / 8), c = ((at >> 1) ^ turn_pair(k)) << 1 | (at & 1);
-                src = base + (uint64_t)min(k0 + k, o.rows - 1) * o.ld + min(row0 + c * 8, o.cols - 8);
+                static_assert(THREADS / (B / 8) % 4 == 0, "a lane's loads are of rows with the same turn");
+                const uint32_t k = threadIdx.x / (B / 8), at = threadIdx.x % (B / 8);
+                off[0] = min(row0 + (((at >> 1) ^ turn_pair(k)) << 1 | (at & 1)) * 8, o.cols - 8) * 2;
             }
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                             (__attribute__((address_space(3))) void*)(lds + (i * THREADS + wave * 64) * 8),
-                                             16, 0, 0);
         }
+    };
+    // The wave's load `i`.  Nothing is fetched unless `any`: a buffer of no bytes.
+    template <int THREADS>
+    static __device__ inline void load(const Operand& o, const uint16_t* base, const Lane<THREADS>& lane, uint32_t row0,
+                                       uint32_t k0, bool any, int i, uint16_t* lds)
+    {
+        static_assert(kChunks % THREADS == 0, "every wave has the same loads");
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint16_t* from = base + (ACROSS ? (uint64_t)k0 * o.ld : (uint64_t)row0 * o.ld + k0);
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)from, 0, __builtin_amdgcn_readfirstlane(any ? -1 : 0), 0x00020000);
+        uint32_t off = lane.off[ACROSS ? 0 : i];
+        if constexpr (ACROSS)
+            off += min((uint32_t)((i * THREADS + threadIdx.x) / (B / 8)), o.rows - 1 - k0) * (uint32_t)o.ld * 2;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            r, (__attribute__((address_space(3))) void*)(lds + (i * THREADS + wave * 64) * 8), 16, off, 0, 0, 0);
     }
 
     // The lane's 8 values of rows [r0, r0 + 32), k [16 step, 16 step + 16): row lane % 32, k 8 (lane / 32) + 0..7.
@@ -123,63 +143,57 @@ struct Tile {
 // p = p0 + 32 tp + 8 (i / 4) + 4 (lane / 32) + i % 4: every lane has runs of 4 consecutive p of one q.
 
 template <int TP, int TQ>
-__device__ inline void finish(const LogitsOut& o, f32x16 (&acc)[TP][TQ], uint32_t p0, uint32_t q0, uint32_t)
+__device__ inline void finish(const LogitsOut& o, f32x16 (&acc)[TP][TQ], uint32_t wave_p0, uint32_t q0, uint32_t)
 {
-    static_assert(TP * 32 == kPartWords, "a wave's words are one part");
+    constexpr int kTiles = kPartWords / 32; // of a part
+    static_assert(TP % kTiles == 0, "a wave's words are whole parts");
     const uint32_t lane = threadIdx.x & 63, up = 4 * (lane >> 5);
 #pragma unroll
-    for (int tq = 0; tq < TQ; ++tq) {
-        const uint32_t q = q0 + 32 * tq + (lane & 31);
-        const bool here = q < o.tokens;
-        float top = -kInf;
+    for (int part = 0; part < TP / kTiles; ++part) {
+        const uint32_t p0 = wave_p0 + part * kPartWords;
+        if (p0 >= o.vocab) break;
 #pragma unroll
-        for (int tp = 0; tp < TP; ++tp)
+        for (int tq = 0; tq < TQ; ++tq) {
+            const uint32_t q = q0 + 32 * tq + (lane & 31);
+            const bool here = q < o.tokens;
+            float x[kTiles * 16]; // of words p0 + 32 (j / 16) + 8 (j / 4 % 4) + up + j % 4
+            float top = -kInf;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t p = p0 + 32 * tp + 8 * (i >> 2) + up + (i & 3);
-                const float x = acc[tp][tq][i];
-                top = p < o.vocab ? fmaxf(top, x) : top; // fmaxf passes a NaN by; the sum below does not
+            for (int j = 0; j < kTiles * 16; ++j) {
+                x[j] = acc[part * kTiles + j / 16][tq][j % 16];
+                const uint32_t p = p0 + 32 * (j / 16) + 8 * (j / 4 % 4) + up + j % 4;
+                top = p < o.vocab ? fmaxf(top, x[j]) : top; // fmaxf passes a NaN by; the sum below does not
             }
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float low = top == -kInf ? 0.0f : top;
-        float sum = 0, sum_t = 0;
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float low = top == -kInf ? 0.0f : top;
+            float sum = 0, sum_t = 0;
 #pragma unroll
-        for (int tp = 0; tp < TP; ++tp)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t p = p0 + 32 * tp + 8 * (i >> 2) + up + (i & 3);
-                const float x = acc[tp][tq][i] - low;
-                sum += p < o.vocab ? exp_of(x) : 0.0f;
-                if (o.part_t) sum_t += p < o.vocab ? exp_of(x * o.inv_t) : 0.0f;
+            for (int j = 0; j < kTiles * 16; ++j) {
+                const uint32_t p = p0 + 32 * (j / 16) + 8 * (j / 4 % 4) + up + j % 4;
+                sum += p < o.vocab ? exp_of(x[j] - low) : 0.0f;
+                if (o.part_t) sum_t += p < o.vocab ? exp_of((x[j] - low) * o.inv_t) : 0.0f;
             }
-        sum += __shfl_xor(sum, 32);
-        if (o.part_t) sum_t += __shfl_xor(sum_t, 32);
-        if (here && lane < 32 && p0 < o.vocab) {
-            const uint64_t at = (uint64_t)(p0 / kPartWords) * o.tokens + q;
-            o.part[at] = make_float2(top, sum);
-            if (o.part_t) o.part_t[at] = sum_t;
-        }
-        if (o.target && here) {
-            const int64_t t = o.target[q] - p0;
-            if (t >= 0 && t < TP * 32) {
-#pragma unroll
-                for (int tp = 0; tp < TP; ++tp)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if ((uint32_t)t == 32u * tp + 8 * (i >> 2) + up + (i & 3) && p0 + t < o.vocab)
-                            o.target_logit[q] = acc[tp][tq][i];
+            sum += __shfl_xor(sum, 32);
+            if (o.part_t) sum_t += __shfl_xor(sum_t, 32);
+            if (!here) continue;
+            if (lane < 32) {
+                const uint64_t at = (uint64_t)(p0 / kPartWords) * o.tokens + q;
+                o.part[at] = make_float2(top, sum);
+                if (o.part_t) o.part_t[at] = sum_t;
             }
-        }
-        if (o.logits && here) {
-            float* row = o.logits + (uint64_t)q * o.ld;
+            if (o.target) {
+                const int64_t t = o.target[q] - p0;
+                if (t >= 0 && t < kPartWords && p0 + t < o.vocab)
 #pragma unroll
-            for (int tp = 0; tp < TP; ++tp)
+                    for (int j = 0; j < kTiles * 16; ++j)
+                        if ((uint32_t)t == 32u * (j / 16) + 8 * (j / 4 % 4) + up + j % 4) o.target_logit[q] = x[j];
+            }
+            if (o.logits) {
+                float* row = o.logits + (uint64_t)q * o.ld + p0 + up; // ld covers whole parts
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const uint32_t p = p0 + 32 * tp + 8 * (i >> 2) + up;
-                    if (p < o.vocab) // ld covers whole runs
-                        *(f32x4*)(row + p) = {acc[tp][tq][i], acc[tp][tq][i + 1], acc[tp][tq][i + 2], acc[tp][tq][i + 3]};
-                }
+                for (int j = 0; j < kTiles * 16; j += 4)
+                    *(f32x4*)(row + 32 * (j / 16) + 8 * (j / 4 % 4)) = {x[j], x[j + 1], x[j + 2], x[j + 3]};
+            }
         }
     }
 }
@@ -234,14 +248,27 @@ __device__ inline void finish(const GradEnd& e, f32x16 (&acc)[TP][TQ], uint32_t 
     }
 }
 
+// Which tile a workgroup takes.  Workgroups go round the 8 XCDs, each with an L2 of its own: an XCD gets a run of
+// consecutive tiles, and runs go through bands of kBand tiles of q, so that the tiles which an XCD works on at a time
+// share their operands' rows.
+constexpr uint32_t kXcds = 8, kBand = 8;
+__device__ inline uint2 tile_of(uint32_t block, uint32_t np, uint32_t nq)
+{
+    const uint32_t n = np * nq, each = n / kXcds, more = n % kXcds;
+    const uint32_t xcd = block % kXcds, at = block / kXcds;
+    const uint32_t t = xcd * each + min(xcd, more) + at;
+    const uint32_t band = t / (kBand * np), in = t % (kBand * np), width = min(kBand, nq - band * kBand);
+    return make_uint2(in / width, band * kBand + in % width);
+}
+
 // ---- the product ----
 //
 // A workgroup of NWP x NWQ waves makes a BP x BQ tile of out[q][p] = sum_k P(p, k) Q(q, k), each wave a part of it in
 // registers.  Two buffers in LDS: while one is multiplied the loads of the next BK values of k write the other one.
 // PLANES = 3: fp32 operands as 3 bf16 planes; of the 9 products of planes the 6 whose sum of indexes is at most 2
 // are made (the others are below 2^-24 of the value), smallest first.
-template <int PLANES, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, class End>
-__global__ __launch_bounds__(NWP* NWQ * 64) void product_kernel(const Operand P, const Operand Q,
+template <int PLANES, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, int BUFS, class End>
+__global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_kernel(const Operand P, const Operand Q,
                                                                 const ProductShape shape, const End end)
 {
     constexpr int kThreads = NWP * NWQ * 64;
@@ -249,14 +276,17 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void product_kernel(const Operand P,
     using TileP = Tile<BP, BK, PA>;
     using TileQ = Tile<BQ, BK, QA>;
     constexpr int kBuffer = PLANES * (TileP::kElems + TileQ::kElems);
-    __shared__ __attribute__((aligned(16))) uint16_t s0[kBuffer], s1[kBuffer];
+    static_assert(BUFS >= 2 && BUFS <= 4, "");
+    // Arrays of their own, so that the compiler sees that a read of one waits for no load into another.
+    __shared__ __attribute__((aligned(16))) uint16_t s0[kBuffer], s1[kBuffer], s2[BUFS > 2 ? kBuffer : 1],
+        s3[BUFS > 3 ? kBuffer : 1];
 
-    const uint32_t np = (shape.p + BP - 1) / BP;
-    const uint32_t bp = blockIdx.x % np, bq = blockIdx.x / np;
-    const uint32_t p0 = bp * BP, q0 = bq * BQ;
+    const uint32_t np = (shape.p + BP - 1) / BP, nq = (shape.q + BQ - 1) / BQ;
+    const uint2 tile = tile_of(blockIdx.x, np, nq);
+    const uint32_t p0 = __builtin_amdgcn_readfirstlane(tile.x * BP), q0 = __builtin_amdgcn_readfirstlane(tile.y * BQ);
     const uint32_t steps = shape.k / BK;
-    const uint32_t first = (uint32_t)((uint64_t)steps * blockIdx.y / shape.slices);
-    const uint32_t last = (uint32_t)((uint64_t)steps * (blockIdx.y + 1) / shape.slices);
+    const uint32_t first = __builtin_amdgcn_readfirstlane((uint64_t)steps * blockIdx.y / shape.slices);
+    const uint32_t last = __builtin_amdgcn_readfirstlane((uint64_t)steps * (blockIdx.y + 1) / shape.slices);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wp = (wave % NWP) * (BP / NWP), wq = (wave / NWP) * (BQ / NWQ);
 
@@ -268,65 +298,112 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void product_kernel(const Operand P,
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0;
 
-    auto load = [&](uint16_t* s, uint32_t step) {
+    const typename TileP::template Lane<kThreads> lane_p(P, p0);
+    const typename TileQ::template Lane<kThreads> lane_q(Q, q0);
+    // The wave's load `i` of a step's kLoads into buffer s; none past the last step.
+    constexpr int kLoadsP = TileP::template loads<kThreads>(), kLoadsQ = TileQ::template loads<kThreads>();
+    constexpr int kLoads = PLANES * (kLoadsP + kLoadsQ);
+    auto load = [&](uint16_t* s, uint32_t step, int i) {
+        const bool any = step < last;
+        const uint32_t k0 = any ? step * BK : 0;
+        const int z = i % PLANES, j = i / PLANES;
+        if (j < kLoadsP)
+            TileP::template load<kThreads>(P, P.base + z * P.plane, lane_p, p0, k0, any, j, s + z * TileP::kElems);
+        else
+            TileQ::template load<kThreads>(Q, Q.base + z * Q.plane, lane_q, q0, k0, any, j - kLoadsP,
+                                           s + PLANES * TileP::kElems + z * TileQ::kElems);
+    };
+    struct Part { // a wave's operands of 16 values of k
+        bf16x8 a[PLANES][TP], b[PLANES][TQ];
+    };
+    auto read = [&](Part& f, const uint16_t* s, int k) {
 #pragma unroll
         for (int z = 0; z < PLANES; ++z) {
-            TileP::template load<kThreads>(P, P.base + z * P.plane, p0, step * BK, s + z * TileP::kElems);
-            TileQ::template load<kThreads>(Q, Q.base + z * Q.plane, q0, step * BK,
-                                           s + PLANES * TileP::kElems + z * TileQ::kElems);
+#pragma unroll
+            for (int t = 0; t < TP; ++t) f.a[z][t] = TileP::read(s + z * TileP::kElems, wp + 32 * t, k);
+#pragma unroll
+            for (int t = 0; t < TQ; ++t)
+                f.b[z][t] = TileQ::read(s + PLANES * TileP::kElems + z * TileQ::kElems, wq + 32 * t, k);
         }
     };
-    auto multiply = [&](const uint16_t* s) {
+    // Nothing moves past: a part's reads stay ahead of the products that hide them, and loads between products.
+    auto hold = [] { __builtin_amdgcn_sched_barrier(0); };
+    // The products of a part, with the first `loads` loads of `step` into s spread among them: issued at once by all
+    // waves they fill the queue to the caches, and no wave gets past it to its products (8192 x 4096 x 32000: 1.97 ms,
+    // spread 1.65 ms).
+    auto multiply = [&](const Part& f, uint16_t* s, uint32_t step, int loads) {
+        constexpr int kProducts = TP * TQ * PLANES * (PLANES + 1) / 2;
+        int n = 0;
 #pragma unroll
-        for (int k = 0; k < BK / 16; ++k) {
-            bf16x8 a[PLANES][TP], b[PLANES][TQ];
+        for (int sum = PLANES - 1; sum >= 0; --sum)
 #pragma unroll
-            for (int z = 0; z < PLANES; ++z) {
+            for (int z = 0; z <= sum; ++z)
 #pragma unroll
-                for (int t = 0; t < TP; ++t) a[z][t] = TileP::read(s + z * TileP::kElems, wp + 32 * t, k);
+                for (int t = 0; t < TP; ++t)
 #pragma unroll
-                for (int t = 0; t < TQ; ++t)
-                    b[z][t] = TileQ::read(s + PLANES * TileP::kElems + z * TileQ::kElems, wq + 32 * t, k);
-            }
+                    for (int u = 0; u < TQ; ++u) {
+                        acc[t][u] =
+                            __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[z][t], f.b[sum - z][u], acc[t][u], 0, 0, 0);
+                        ++n;
+                        for (int i = loads * (n - 1) / kProducts; i < loads * n / kProducts; ++i) {
+                            hold();
+                            load(s, step, i);
+                            hold();
+                        }
+                    }
+    };
+    // Once this wave's reads are done and its loads but those of the last BUFS - 2 steps have landed: when that is so
+    // for all.
+    auto meet = [] {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((BUFS - 2) * kLoads) : "memory");
+    };
+    // One step on buffer s: each part is read while the one before is multiplied.  All of s is in registers before the
+    // last part is multiplied, so the waves meet there: behind that part's products s is filled again and the next
+    // buffer's first part is read.  There is no branch around the loads and reads past the last step: a branch would
+    // make the compiler wait for what its other path has not loaded, and what they fetch is not used.
+    Part even, odd;
+    auto one_step = [&](uint16_t* s, uint16_t* next, uint32_t step) {
+        constexpr int kParts = BK / 16;
+        static_assert(kParts % 2 == 0, "a step ends with its parts where it began");
 #pragma unroll
-            for (int sum = PLANES - 1; sum >= 0; --sum)
-#pragma unroll
-                for (int z = 0; z <= sum; ++z)
-#pragma unroll
-                    for (int t = 0; t < TP; ++t)
-#pragma unroll
-                        for (int u = 0; u < TQ; ++u)
-                            acc[t][u] =
-                                __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[z][t], b[sum - z][u], acc[t][u], 0, 0, 0);
+        for (int k = 0; k < kParts; k += 2) {
+            const bool end_part = k + 2 == kParts;
+            read(odd, s, k + 1);
+            hold();
+            multiply(even, s, step, 0);
+            hold();
+            if (end_part) meet();
+            read(even, end_part ? next : s, end_part ? 0 : k + 2);
+            hold();
+            multiply(odd, s, step + BUFS, end_part ? kLoads : 0);
+            hold();
         }
     };
-    // The wave's own loads have landed; then everyone's.
-    auto landed = [&] {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-
-    if (first < last) {
-        load(s0, first);
-        for (uint32_t step = first; step < last; step += 2) {
-            landed();
-            if (step + 1 < last) load(s1, step + 1);
-            multiply(s0);
-            if (step + 1 >= last) break;
-            landed();
-            if (step + 2 < last) load(s0, step + 2);
-            multiply(s1);
-        }
+#pragma unroll
+    for (int i = 0; i < BUFS * kLoads; ++i)
+        load(i / kLoads == 0 ? s0 : i / kLoads == 1 ? s1 : i / kLoads == 2 ? s2 : s3, first + i / kLoads, i % kLoads);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((BUFS - 1) * kLoads) : "memory");
+    read(even, s0, 0);
+    uint32_t step = first;
+    for (; step + BUFS <= last; step += BUFS) {
+        one_step(s0, s1, step);
+        one_step(s1, BUFS > 2 ? s2 : s0, step + 1);
+        if constexpr (BUFS > 2) one_step(s2, BUFS > 3 ? s3 : s0, step + 2);
+        if constexpr (BUFS > 3) one_step(s3, s0, step + 3);
     }
+    if (step < last) one_step(s0, s1, step);
+    if (BUFS > 2 && step + 1 < last) one_step(s1, s2, step + 1);
+    if (BUFS > 3 && step + 2 < last) one_step(s2, s3, step + 2);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // no load is left that would write the LDS of another workgroup
     finish<TP, TQ>(end, acc, p0 + wp, q0 + wq, blockIdx.y);
 }
 
-template <int PLANES, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, class End>
+template <int PLANES, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, int BUFS, class End>
 hipError_t launch_product(const Operand& P, const Operand& Q, const ProductShape& s, const End& end, hipStream_t stream)
 {
     const uint64_t tiles = (uint64_t)((s.p + BP - 1) / BP) * ((s.q + BQ - 1) / BQ);
     if (tiles == 0 || tiles > 0x7fffffff || s.slices == 0 || s.slices > 65535 || s.k % BK) return hipErrorInvalidValue;
-    product_kernel<PLANES, PA, QA, BP, BQ, NWP, NWQ, BK, End>
+    product_kernel<PLANES, PA, QA, BP, BQ, NWP, NWQ, BK, BUFS, End>
         <<<dim3((uint32_t)tiles, s.slices), NWP * NWQ * 64, 0, stream>>>(P, Q, s, end);
     return hipGetLastError();
 }
@@ -631,33 +708,72 @@ __global__ __launch_bounds__(256) void join_kernel(const float* slices, uint32_t
 
 } // namespace
 
+namespace {
+
+// Workgroup tiles.  bf16: 256 x 256 (8 waves of 64 x 128) reaches 1.2-1.3 PFLOP/s where its tiles fill the 256 compute
+// units, 128 x 128 (4 waves, two workgroups a unit) 1.0-1.07.  Three planes: 256 x 128 (8 waves of 64 x 64; LDS has no
+// room for more) and 128 x 128.
+struct Tiling {
+    bool large;
+    uint32_t slices;
+};
+
+// The tile and the number of runs of k that finish first, by the whole rounds of tiles that the units need.
+Tiling tiling(const ProductShape& s, uint32_t planes, uint32_t most)
+{
+    const double rate = planes == 3 ? 6 : 1; // products of planes
+    Tiling best = {false, 1};
+    double least = 1e30;
+    for (int large = 0; large < 2; ++large) {
+        const uint32_t bp = large ? 256 : 128, bq = large && planes == 1 ? 256 : 128;
+        const uint64_t tiles = (uint64_t)((s.p + bp - 1) / bp) * ((s.q + bq - 1) / bq);
+        const uint32_t slots = large || planes == 3 ? 256 : 512;
+        // seconds for 64 values of k on one unit
+        const double step = 2.0 * bp * bq * 64 * rate / ((large ? (planes == 1 ? 1250e12 : 1400e12) : 1050e12) / slots);
+        for (uint32_t n = 1; n <= std::min({most, 64u, s.k / 256 ? s.k / 256 : 1}); ++n) {
+            const uint64_t rounds = (tiles * n + slots - 1) / slots;
+            const double t = rounds * ((double)((s.k / 64 + n - 1) / n) * step + 3e-6) +
+                             (n > 1 ? 3e-6 + 8.0 * s.p * s.q * n / 4e12 : 0);
+            if (t < least) least = t, best = {large != 0, n};
+        }
+    }
+    return best;
+}
+
+template <bool PA, bool QA, class End>
+hipError_t dispatch(const Operand& P, const Operand& Q, const ProductShape& s, uint32_t planes, bool large,
+                    const End& end, hipStream_t stream)
+{
+    if (planes == 3)
+        return large ? launch_product<3, PA, QA, 256, 128, 4, 2, 32, 2>(P, Q, s, end, stream)
+                     : launch_product<3, PA, QA, 128, 128, 2, 2, 32, 2>(P, Q, s, end, stream);
+    return large ? launch_product<1, PA, QA, 256, 256, 4, 2, 64, 2>(P, Q, s, end, stream)
+                 : launch_product<1, PA, QA, 128, 128, 2, 2, 64, 2>(P, Q, s, end, stream);
+}
+
+} // namespace
+
 hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape& s, uint32_t planes,
                          const LogitsOut& o, hipStream_t stream)
 {
-    return planes == 3 ? launch_product<3, false, false, 128, 128, 2, 2, 32>(w, h, s, o, stream)
-                       : launch_product<1, false, false, 128, 128, 2, 2, 64>(w, h, s, o, stream);
+    return dispatch<false, false>(w, h, s, planes, tiling(s, planes, 1).large, o, stream);
 }
 
 hipError_t launch_d_hidden(const Operand& w, const Operand& dl, const ProductShape& s, uint32_t planes,
                            const GradOut& o, hipStream_t stream)
 {
-    const GradEnd end = {o, s.p, s.q};
-    return planes == 3 ? launch_product<3, true, false, 128, 128, 2, 2, 32>(w, dl, s, end, stream)
-                       : launch_product<1, true, false, 128, 128, 2, 2, 64>(w, dl, s, end, stream);
+    return dispatch<true, false>(w, dl, s, planes, tiling(s, planes, s.slices).large, GradEnd{o, s.p, s.q}, stream);
 }
 
 hipError_t launch_d_weight(const Operand& h, const Operand& dl, const ProductShape& s, uint32_t planes,
                            const GradOut& o, hipStream_t stream)
 {
-    const GradEnd end = {o, s.p, s.q};
-    return planes == 3 ? launch_product<3, true, true, 128, 128, 2, 2, 32>(h, dl, s, end, stream)
-                       : launch_product<1, true, true, 128, 128, 2, 2, 64>(h, dl, s, end, stream);
+    return dispatch<true, true>(h, dl, s, planes, tiling(s, planes, 1).large, GradEnd{o, s.p, s.q}, stream);
 }
 
-uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t, uint32_t most)
+uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t planes, uint32_t most)
 {
-    const uint64_t tiles = (uint64_t)((p + 127) / 128) * ((q + 127) / 128);
-    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({512 / tiles, k / 256, most, 64}));
+    return tiling({p, q, k, 1}, planes, std::max(1u, most)).slices;
 }
 
 hipError_t launch_join(const float* slices, uint32_t n, uint32_t p, uint32_t q, const GradOut& o, hipStream_t stream)

@@ -10,7 +10,8 @@ namespace ckpt {
 // ---- products on the matrix cores (loss_kernels.hip) ----
 
 // One operand of out[q][p] = sum_k P(p, k) Q(q, k): bf16, as 1 plane or as the
-// 3 whose sum is an fp32 value.  Rows are 16-byte aligned (base and ld).
+// 3 whose sum is an fp32 value.  Rows are 16-byte aligned (base and ld), ld is
+// at most 2^22.
 //   k contiguous:     element (r, k) at base[r * ld + k]; row indices are
 //                     clamped below `rows`, k runs to a multiple of 64
 //   k across rows:    element (r, k) at base[k * ld + r]; k is clamped below
