@@ -142,6 +142,15 @@ def lib():
 _pack = None
 
 
+def _native_module():
+    """_ckpt_py, or None where it was not built for this Python and torch."""
+    try:
+        from . import _ckpt_py
+    except ImportError:
+        return None
+    return _ckpt_py if torch.__version__.split("+")[0] == _ckpt_py.torch_version else None
+
+
 def _native_pack():
     """(_ckpt_py.pack_noalloc, address of ckpt_pack_noalloc); where the module
     was not built for this Python and torch, a pack_noalloc that leaves every
@@ -149,12 +158,8 @@ def _native_pack():
     global _pack
     if _pack is None:
         fn = C.cast(lib().ckpt_pack_noalloc, C.c_void_p).value
-        try:
-            from . import _ckpt_py
-            usable = torch.__version__.split("+")[0] == _ckpt_py.torch_version
-        except ImportError:
-            usable = False
-        _pack = (_ckpt_py.pack_noalloc if usable else lambda *args: None, fn)
+        module = _native_module()
+        _pack = (module.pack_noalloc if module is not None else lambda *args: None, fn)
     return _pack
 
 

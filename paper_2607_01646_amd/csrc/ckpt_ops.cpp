@@ -121,13 +121,36 @@ uint64_t extent(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t elem)
     return rows ? ((rows - 1) * ld + cols) * elem : 0;
 }
 
+// Allocations that this call has met: most of its pointers share a few (a
+// flat buffer's fragments, a caching allocator's segments), and asking the
+// runtime about one takes a microsecond.
+struct Known {
+    static constexpr int kMost = 8;
+    uint64_t lo[kMost], hi[kMost];
+    int n = 0, at = 0;
+
+    bool holds(uint64_t p, uint64_t bytes) const
+    {
+        for (int k = 0; k < n; ++k)
+            if (p >= lo[k] && p <= hi[k] && bytes <= hi[k] - p) return true;
+        return false;
+    }
+    void add(uint64_t base, uint64_t size)
+    {
+        lo[at] = base;
+        hi[at] = base + size;
+        at = (at + 1) % kMost;
+        n = n < kMost ? n + 1 : n;
+    }
+};
+
 struct Given {
     const void* p;
     uint64_t rows, cols, ld, elem;
     const char* what;
 };
 
-ckpt_status check_given(const Given& g, int device)
+ckpt_status check_given(const Given& g, int device, Known& known)
 {
     if (g.rows == 0 || g.cols == 0) return CKPT_OK;
     if (!g.p) return fail_free(CKPT_EINVAL, "%s: null pointer", g.what);
@@ -136,7 +159,16 @@ ckpt_status check_given(const Given& g, int device)
         return fail_free(CKPT_EINVAL, "%s: rows of %llu elements are %llu apart", g.what, (unsigned long long)g.cols,
                          (unsigned long long)g.ld);
     if (g.ld > (1ull << 40)) return fail_free(CKPT_EINVAL, "%s: a stride of %llu", g.what, (unsigned long long)g.ld);
-    return check_range(g.p, extent(g.rows, g.cols, g.ld, g.elem), device, g.what);
+    const uint64_t p = (uint64_t)(uintptr_t)g.p, bytes = extent(g.rows, g.cols, g.ld, g.elem);
+    if (known.holds(p, bytes)) return CKPT_OK;
+    if (ckpt_status st = check_range(g.p, bytes, device, g.what)) return st;
+    hipDeviceptr_t base = nullptr;
+    size_t size = 0;
+    if (hipMemGetAddressRange(&base, &size, (hipDeviceptr_t)g.p) == hipSuccess)
+        known.add((uint64_t)(uintptr_t)base, size);
+    else
+        (void)hipGetLastError();
+    return CKPT_OK;
 }
 
 } // namespace
@@ -165,6 +197,7 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
                          (unsigned long long)l.bytes);
     DeviceGuard dg;
     if (ckpt_status st = enter_device(device, dg)) return st;
+    Known known;
     const bool f32 = a->dtype == CKPT_TYPE_F32;
     const uint64_t e = f32 ? 4 : 2, n = a->tokens, d = a->dim, v = a->vocab, k = a->topk;
     const uint64_t te = a->teacher_dtype == CKPT_TYPE_F32 ? 4 : 2;
@@ -184,7 +217,7 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
         {workspace, 1, l.bytes, l.bytes, 1, "workspace"},
     };
     for (const Given& g : given)
-        if (ckpt_status st = check_given(g, device)) return st;
+        if (ckpt_status st = check_given(g, device, known)) return st;
 
     hipStream_t s = (hipStream_t)stream;
     uint8_t* w = (uint8_t*)workspace;
@@ -333,14 +366,18 @@ extern "C" ckpt_status ckpt_grad_norm(const ckpt_tensor* grads, uint32_t n, uint
     if (std::isnan(max_norm)) return fail_free(CKPT_EINVAL, "max_norm is not a number");
     DeviceGuard dg;
     if (ckpt_status st = enter_device(device, dg)) return st;
-    if (ckpt_status st = check_given({out, 1, 2, 2, 4, "out"}, device)) return st;
-    if (ckpt_status st = check_given({scratch, 1, CKPT_GRAD_NORM_SCRATCH / 8, CKPT_GRAD_NORM_SCRATCH / 8, 8, "scratch"}, device)) return st;
+    Known known;
+    if (ckpt_status st = check_given({out, 1, 2, 2, 4, "out"}, device, known)) return st;
+    if (ckpt_status st = check_given({scratch, 1, CKPT_GRAD_NORM_SCRATCH / 8, CKPT_GRAD_NORM_SCRATCH / 8, 8, "scratch"}, device, known)) return st;
     for (uint32_t i = 0; i < n; ++i) {
+        if (grads[i].nbytes % e == 0 && (uintptr_t)grads[i].dev_ptr % e == 0 &&
+            known.holds((uint64_t)(uintptr_t)grads[i].dev_ptr, grads[i].nbytes))
+            continue;
         char what[32];
         snprintf(what, sizeof what, "gradient %u", i);
         if (grads[i].nbytes % e) return fail_free(CKPT_EINVAL, "%s: %llu bytes", what, (unsigned long long)grads[i].nbytes);
         const uint64_t c = grads[i].nbytes / e;
-        if (ckpt_status st = check_given({grads[i].dev_ptr, 1, c, c, e, what}, device)) return st;
+        if (ckpt_status st = check_given({grads[i].dev_ptr, 1, c, c, e, what}, device, known)) return st;
     }
     static_assert(CKPT_GRAD_NORM_SCRATCH == kNormBlocks * 8, "one sum for each workgroup");
     NormArgs a;
@@ -387,8 +424,9 @@ extern "C" ckpt_status ckpt_adamw(const ckpt_adamw_fragment* f, uint32_t n, uint
         return fail_free(CKPT_EINVAL, "lr %g, eps %g, weight_decay %g", lr, eps, weight_decay);
     DeviceGuard dg;
     if (ckpt_status st = enter_device(device, dg)) return st;
+    Known known;
     if (grad_scale)
-        if (ckpt_status st = check_given({grad_scale, 1, 1, 1, 4, "grad_scale"}, device)) return st;
+        if (ckpt_status st = check_given({grad_scale, 1, 1, 1, 4, "grad_scale"}, device, known)) return st;
     for (uint32_t i = 0; i < n; ++i) {
         const struct {
             const void* p;
@@ -398,9 +436,10 @@ extern "C" ckpt_status ckpt_adamw(const ckpt_adamw_fragment* f, uint32_t n, uint
                     {f[i].exp_avg_sq, 4, "exp_avg_sq"}, {f[i].grad, ge, "grad"}};
         if (f[i].numel > (1ull << 60)) return fail_free(CKPT_EINVAL, "fragment %u: %llu elements", i, (unsigned long long)f[i].numel);
         for (const auto& x : part) {
+            if ((uintptr_t)x.p % x.e == 0 && known.holds((uint64_t)(uintptr_t)x.p, f[i].numel * x.e)) continue;
             char what[48];
             snprintf(what, sizeof what, "fragment %u, %s", i, x.name);
-            if (ckpt_status st = check_given({x.p, 1, f[i].numel, f[i].numel, x.e, what}, device)) return st;
+            if (ckpt_status st = check_given({x.p, 1, f[i].numel, f[i].numel, x.e, what}, device, known)) return st;
         }
     }
     AdamArgs a;

@@ -15,7 +15,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .ckpt import CKPT_OK, CkptError, _stream, ckpt_tensor, lib, tensor_bytes
+from .ckpt import CKPT_OK, CkptError, _native_module, ckpt_tensor, lib, tensor_bytes
 
 CKPT_TYPE_BF16 = 1
 CKPT_TYPE_F32 = 2
@@ -53,6 +53,25 @@ class LinearLoss(NamedTuple):
 
 
 _lib = None
+_native = None
+
+
+def _module():
+    """(the native module or None, addresses of the entry points)."""
+    global _native
+    if _native is None:
+        L = _ops()
+        _native = (_native_module(), {n: C.cast(getattr(L, n), C.c_void_p).value for n in
+                                      ("ckpt_linear_loss_workspace", "ckpt_linear_loss", "ckpt_grad_norm",
+                                       "ckpt_adamw")})
+    return _native
+
+
+def _handle(stream, tensor):
+    """hipStream_t handle of a torch stream, an int handle, or (None) torch's current stream on the tensor's device."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(tensor.get_device())
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _ops():
@@ -124,6 +143,17 @@ def _plain(t, what, dtype, n):
 
 def _linear_loss(hidden, weight, target, teacher, temperature, alpha, token_weight, ignore_index, reduction, grad,
                  grad_scale, piece_bytes, stream):
+    native, at = _module()
+    if native is not None and isinstance(hidden, torch.Tensor) and hidden.is_cuda and reduction in _REDUCTIONS:
+        with _on(stream):
+            got = native.linear_loss(at["ckpt_linear_loss_workspace"], at["ckpt_linear_loss"], hidden, weight, target,
+                                     None if teacher is None else teacher[0], None if teacher is None else teacher[1],
+                                     temperature, alpha, token_weight, ignore_index, _REDUCTIONS[reduction], grad,
+                                     grad_scale, piece_bytes, _handle(stream, hidden))
+        if got is not None:
+            _check(got[0])
+            return LinearLoss(*got[1:])
+    # Arguments that the native module leaves to this code, and those refused; every call where there is none.
     a = ckpt_linear_loss_args()
     a.dtype = _type(hidden, "hidden")
     if _type(weight, "weight") != a.dtype:
@@ -176,7 +206,7 @@ def _linear_loss(hidden, weight, target, teacher, temperature, alpha, token_weig
         L = _ops()
         _check(L.ckpt_linear_loss_workspace(C.byref(a), C.byref(need)))
         work = torch.empty(need.value, dtype=torch.uint8, device=hidden.device)
-        _check(L.ckpt_linear_loss(C.byref(a), hidden.device.index, work.data_ptr(), need.value, _stream(stream)))
+        _check(L.ckpt_linear_loss(C.byref(a), hidden.device.index, work.data_ptr(), need.value, _handle(stream, hidden)))
     return LinearLoss(out[0], out[1:n + 1].view(shape), out[n + 1:].view(shape), d_hidden, d_weight)
 
 
@@ -211,6 +241,13 @@ def ckpt_grad_norm(grads, max_norm=0.0, stream=None):
     grads = list(grads)
     if not grads:
         raise ValueError("no gradients")
+    native, at = _module()
+    if native is not None and isinstance(grads[0], torch.Tensor) and grads[0].is_cuda:
+        with _on(stream):
+            got = native.grad_norm(at["ckpt_grad_norm"], grads, max_norm, _handle(stream, grads[0]))
+        if got is not None:
+            _check(got[0])
+            return got[1]
     kind = _type(grads[0], "gradient 0")
     arr = (ckpt_tensor * len(grads))()
     for i, t in enumerate(grads):
@@ -223,7 +260,7 @@ def ckpt_grad_norm(grads, max_norm=0.0, stream=None):
         out = torch.empty(2, dtype=torch.float32, device=device)
         scratch = torch.empty(CKPT_GRAD_NORM_SCRATCH, dtype=torch.uint8, device=device)
         _check(_ops().ckpt_grad_norm(arr, len(grads), kind, max_norm, out.data_ptr(), scratch.data_ptr(), device.index,
-                                     _stream(stream)))
+                                     _handle(stream, grads[0])))
     return out
 
 
@@ -239,6 +276,13 @@ def ckpt_adamw(params, masters, exp_avgs, exp_avg_sqs, grads, step, lr, beta1=0.
         raise ValueError("lists of %s fragments" % ", ".join(str(len(x)) for x in lists))
     if n == 0:
         return
+    native, at = _module()
+    if native is not None and isinstance(lists[0][0], torch.Tensor) and lists[0][0].is_cuda:
+        rc = native.adamw(at["ckpt_adamw"], *lists, step, lr, beta1, beta2, eps, weight_decay, grad_scale,
+                          _handle(stream, lists[0][0]))
+        if rc is not None:
+            _check(rc)
+            return
     pt, gt = _type(lists[0][0], "param 0"), _type(lists[4][0], "grad 0")
     kinds = (pt, CKPT_TYPE_F32, CKPT_TYPE_F32, CKPT_TYPE_F32, gt)
     names = ("param", "master", "exp_avg", "exp_avg_sq", "grad")
@@ -253,4 +297,4 @@ def ckpt_adamw(params, masters, exp_avgs, exp_avg_sqs, grads, step, lr, beta1=0.
         arr[i].numel = numel
     scale = _plain(grad_scale, "grad_scale", torch.float32, 1) if grad_scale is not None else None
     _check(_ops().ckpt_adamw(arr, n, pt, gt, step, lr, beta1, beta2, eps, weight_decay, scale,
-                             lists[0][0].device.index, _stream(stream)))
+                             lists[0][0].device.index, _handle(stream, lists[0][0])))
