@@ -14,19 +14,24 @@ namespace {
 constexpr uint64_t kMost = 0x7fffffffull;  // tokens
 constexpr uint64_t kMostWidth = 1ull << 22; // dim, vocab: a tile's rows of an operand stay within 31 bits of bytes
 constexpr uint64_t kDefaultPiece = 2ull << 30;
+// For so few tokens d_logits has a second bf16 plane: the products are bound by the weight's bytes, and the gradients
+// of few terms have no others to average their rounding with.
+constexpr uint64_t kFewTokens = 256;
 constexpr uint64_t kSliceBytes = 256ull << 20; // of the partial sums of a product cut along k
 
 uint64_t up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 
 // Where everything lies in the workspace, and how the tokens are cut.
 struct LossPlan {
-    uint32_t planes = 1;      // of an operand
+    uint32_t planes = 1;      // of hidden and weight
+    uint32_t dl_planes = 1;   // of d_logits
     uint64_t dim_pad = 0;     // width of copied operands
     uint64_t vocab_pad = 0;   // width of logits and d_logits
     uint64_t piece = 0;       // tokens in a piece
     uint32_t pieces = 0;
-    bool grad = false, teach = false, held = false; // held: a piece's logits are written
-    bool copy_weight = false, copy_hidden = false;
+    bool grad = false, teach = false, held = false; // held: a piece's logits are written,
+    bool e16 = false;                               // as exponentials in fp16 where d_logits goes
+    bool copy_weight = false, copy_hidden = false, masked_hidden = false;
     bool two_sums = false; // the softmax at 1/temperature has sums of its own
     uint32_t parts = 0;
     uint32_t slices = 1;
@@ -71,17 +76,20 @@ LossPlan plan_loss(const ckpt_linear_loss_args* a)
     l.teach = a->topk != 0 && a->alpha > 0;
     l.held = l.grad || l.teach;
     l.two_sums = l.teach && a->temperature != 1;
-    l.parts = (uint32_t)up(v, kPartWords) / kPartWords;
+    l.parts = (uint32_t)(up(v, kPartWords) / kPartWords);
+    l.dl_planes = f32 ? 3 : n <= kFewTokens ? 2 : 1;
+    l.e16 = l.grad && !l.teach && l.dl_planes == 1 && l.parts <= kE16Parts;
     const auto direct = [&](const void* p, uint64_t ld) { // as it is fit for the loads of a product
         return !f32 && d % 64 == 0 && ld % 8 == 0 && ld <= kMostWidth && (uintptr_t)p % 16 == 0;
     };
     l.copy_weight = !direct(a->weight, a->weight_stride);
     // With gradients the hidden states are copied so that those of rows that do not count are zero: the products over
     // the tokens multiply them by 0, and 0 * NaN is no 0.
-    l.copy_hidden = l.grad || !direct(a->hidden, a->hidden_stride);
+    l.masked_hidden = l.grad && direct(a->hidden, a->hidden_stride); // by the row kernel
+    l.copy_hidden = !direct(a->hidden, a->hidden_stride);             // before the logits
     l.piece = n;
     if (l.held) {
-        const uint64_t row = l.vocab_pad * (4 + (l.grad ? 2 * l.planes : 0));
+        const uint64_t row = l.vocab_pad * ((l.e16 ? 0 : 4) + (l.grad ? 2 * l.dl_planes : 0));
         const uint64_t most = std::max<uint64_t>(256, (a->piece_bytes ? a->piece_bytes : kDefaultPiece) / row / 64 * 64);
         l.piece = std::min(n, most);
     }
@@ -98,15 +106,15 @@ LossPlan plan_loss(const ckpt_linear_loss_args* a)
     l.row_weight = take(4 * n);
     l.target_logit = take(4 * l.piece);
     if (l.copy_weight) l.weight = take(2ull * l.planes * v * l.dim_pad);
-    if (l.copy_hidden) l.hidden = take(2ull * l.planes * piece_pad * l.dim_pad);
+    if (l.copy_hidden || l.masked_hidden) l.hidden = take(2ull * l.planes * piece_pad * l.dim_pad);
     l.part = take(8ull * l.parts * l.piece);
     if (l.two_sums) l.part_t = take(4ull * l.parts * l.piece);
-    if (l.held) l.logits = take(4 * l.piece * l.vocab_pad);
+    if (l.held && !l.e16) l.logits = take(4 * l.piece * l.vocab_pad);
     if (l.grad) {
-        l.d_logits = take(2ull * l.planes * piece_pad * l.vocab_pad);
+        l.d_logits = take(2ull * l.dl_planes * piece_pad * l.vocab_pad);
         if (l.pieces > 1) l.sum = take(4 * v * d);
-        const uint64_t one = 4 * l.piece * d;
-        l.slices = n ? d_hidden_slices((uint32_t)d, (uint32_t)l.piece, (uint32_t)l.vocab_pad, l.planes,
+        const uint64_t one = 4 * l.piece * l.dim_pad;
+        l.slices = n ? d_hidden_slices((uint32_t)d, (uint32_t)l.piece, (uint32_t)l.vocab_pad, l.planes, l.dl_planes,
                                        (uint32_t)std::min<uint64_t>(kSliceBytes / one, 1u << 20))
                      : 1;
         if (l.slices > 1) l.join = take(one * l.slices);
@@ -263,13 +271,14 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
         const uint64_t row0 = piece * l.piece, rows = std::min(l.piece, n - row0), rows_pad = up(rows, 64);
         const uint8_t* h = (const uint8_t*)a->hidden + row0 * a->hidden_stride * e;
         Operand H = {(const uint16_t*)h, 0, a->hidden_stride, (uint32_t)rows, (uint32_t)d};
-        RowCopy c = {};
+        RowCopy c = {a->hidden, a->hidden_stride, (uint32_t)d, f32, (uint16_t*)(w + l.hidden), rows_pad * l.dim_pad,
+                     (uint32_t)l.dim_pad, (uint32_t)rows_pad};
+        const Operand copied = {c.dst, c.plane, l.dim_pad, (uint32_t)rows_pad, (uint32_t)l.dim_pad};
         if (l.copy_hidden) {
-            c = {a->hidden, a->hidden_stride, (uint32_t)d, f32, (uint16_t*)(w + l.hidden), rows_pad * l.dim_pad,
-                 (uint32_t)l.dim_pad, (uint32_t)rows_pad};
-            H = {c.dst, c.plane, l.dim_pad, (uint32_t)rows_pad, (uint32_t)l.dim_pad};
+            CKPT_STEP(launch_prepare(&r, (uint32_t)row0, (uint32_t)rows, c, s), "rows");
+            H = copied;
         }
-        CKPT_STEP(launch_prepare(&r, (uint32_t)row0, (uint32_t)rows, c, s), "rows");
+        if (!l.masked_hidden) c = {};
 
         LogitsOut lo = {};
         lo.vocab = (uint32_t)v;
@@ -279,7 +288,8 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
         lo.part = (float2*)(w + l.part);
         lo.part_t = l.two_sums ? (float*)(w + l.part_t) : nullptr;
         lo.inv_t = 1 / r.temperature;
-        lo.logits = l.held ? (float*)(w + l.logits) : nullptr;
+        lo.logits = l.held && !l.e16 ? (float*)(w + l.logits) : nullptr;
+        lo.e16 = l.e16 ? (uint16_t*)(w + l.d_logits) : nullptr;
         lo.ld = l.vocab_pad;
         CKPT_STEP(launch_logits(W, H, {(uint32_t)v, (uint32_t)rows, (uint32_t)l.dim_pad, 1}, l.planes, lo, s), "logits");
 
@@ -292,7 +302,8 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
         p.part_t = lo.part_t;
         p.logits = lo.logits;
         p.ld = l.vocab_pad;
-        p.f32 = f32;
+        p.planes = l.dl_planes;
+        p.e16 = l.e16;
         if (l.grad) {
             p.d_logits = (uint16_t*)(w + l.d_logits);
             p.dl_ld = l.vocab_pad;
@@ -300,9 +311,10 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
             p.dl_rows = (uint32_t)rows_pad;
         }
         r.target_logit = lo.target_logit - row0;
-        CKPT_STEP(launch_rows(r, p, s), "loss rows");
+        CKPT_STEP(launch_rows(r, p, c, s), "loss rows");
         if (piece + 1 == l.pieces) CKPT_STEP(launch_finish(r, true, s), "loss");
         if (!l.grad) continue;
+        if (l.masked_hidden) H = copied;
 
         const Operand dl_rows = {p.d_logits, p.dl_plane, l.vocab_pad, (uint32_t)rows_pad, (uint32_t)l.vocab_pad};
         GradOut g = {};
@@ -315,12 +327,14 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
             GradOut part = {};
             part.out = w + l.join;
             part.f32 = true;
-            part.ld = d;
-            part.slice = rows * d;
-            CKPT_STEP(launch_d_hidden(W, dl_rows, dh, l.planes, part, s), "d_hidden");
-            CKPT_STEP(launch_join((const float*)part.out, l.slices, (uint32_t)d, (uint32_t)rows, g, s), "d_hidden");
+            part.ld = l.dim_pad;
+            part.slice = rows * l.dim_pad;
+            CKPT_STEP(launch_d_hidden(W, l.planes, dl_rows, l.dl_planes, dh, part, s), "d_hidden");
+            CKPT_STEP(launch_join((const float*)part.out, part.slice, (uint32_t)l.dim_pad, l.slices, (uint32_t)d,
+                                  (uint32_t)rows, g, s),
+                      "d_hidden");
         } else {
-            CKPT_STEP(launch_d_hidden(W, dl_rows, dh, l.planes, g, s), "d_hidden");
+            CKPT_STEP(launch_d_hidden(W, l.planes, dl_rows, l.dl_planes, dh, g, s), "d_hidden");
         }
 
         GradOut gw = {};
@@ -335,7 +349,7 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
             gw.f32 = true;
             gw.scale = nullptr;
         }
-        CKPT_STEP(launch_d_weight(H, dl_rows, {(uint32_t)d, (uint32_t)v, (uint32_t)rows_pad, 1}, l.planes, gw, s),
+        CKPT_STEP(launch_d_weight(H, l.planes, dl_rows, l.dl_planes, {(uint32_t)d, (uint32_t)v, (uint32_t)rows_pad, 1}, gw, s),
                   "d_weight");
     }
     if (l.pieces == 0) { // no token: a loss of 0, and its gradient

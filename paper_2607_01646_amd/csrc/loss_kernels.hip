@@ -21,11 +21,15 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u16x4 u16x4_any __attribute__((aligned(2)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kInf = __builtin_inff();
+constexpr float kE16 = 32768; // scale of the exponentials held in fp16
 
 __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 __device__ inline uint16_t bf16_of(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
@@ -188,6 +192,17 @@ __device__ inline void finish(const LogitsOut& o, f32x16 (&acc)[TP][TQ], uint32_
                     for (int j = 0; j < kTiles * 16; ++j)
                         if ((uint32_t)t == 32u * (j / 16) + 8 * (j / 4 % 4) + up + j % 4) o.target_logit[q] = x[j];
             }
+            if (o.e16) {
+                // exp(l - top) 2^15, in 11 bits from 2^-29 on: its rounding is an eighth of d_logits' own
+                _Float16* row = (_Float16*)o.e16 + (uint64_t)q * o.ld + p0 + up;
+#pragma unroll
+                for (int j = 0; j < kTiles * 16; j += 4) {
+                    f16x4 e;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[i] = (_Float16)(exp_of(x[j + i] - low) * kE16);
+                    *(f16x4*)(row + 32 * (j / 16) + 8 * (j / 4 % 4)) = e;
+                }
+            }
             if (o.logits) {
                 float* row = o.logits + (uint64_t)q * o.ld + p0 + up; // ld covers whole parts
 #pragma unroll
@@ -265,9 +280,9 @@ __device__ inline uint2 tile_of(uint32_t block, uint32_t np, uint32_t nq)
 //
 // A workgroup of NWP x NWQ waves makes a BP x BQ tile of out[q][p] = sum_k P(p, k) Q(q, k), each wave a part of it in
 // registers.  Two buffers in LDS: while one is multiplied the loads of the next BK values of k write the other one.
-// PLANES = 3: fp32 operands as 3 bf16 planes; of the 9 products of planes the 6 whose sum of indexes is at most 2
-// are made (the others are below 2^-24 of the value), smallest first.
-template <int PLANES, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, int BUFS, class End>
+// ZP and ZQ planes an operand.  3 and 3: fp32 operands as 3 bf16 planes; of the 9 products of planes the 6 whose sum of
+// indexes is at most 2 are made (the others are below 2^-24 of the value), smallest first.
+template <int ZP, int ZQ, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, int BUFS, class End>
 __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_kernel(const Operand P, const Operand Q,
                                                                 const ProductShape shape, const End end)
 {
@@ -275,7 +290,7 @@ __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_
     constexpr int TP = BP / NWP / 32, TQ = BQ / NWQ / 32;
     using TileP = Tile<BP, BK, PA>;
     using TileQ = Tile<BQ, BK, QA>;
-    constexpr int kBuffer = PLANES * (TileP::kElems + TileQ::kElems);
+    constexpr int kAtQ = ZP * TileP::kElems, kBuffer = kAtQ + ZQ * TileQ::kElems;
     static_assert(BUFS >= 2 && BUFS <= 4, "");
     // Arrays of their own, so that the compiler sees that a read of one waits for no load into another.
     __shared__ __attribute__((aligned(16))) uint16_t s0[kBuffer], s1[kBuffer], s2[BUFS > 2 ? kBuffer : 1],
@@ -302,29 +317,30 @@ __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_
     const typename TileQ::template Lane<kThreads> lane_q(Q, q0);
     // The wave's load `i` of a step's kLoads into buffer s; none past the last step.
     constexpr int kLoadsP = TileP::template loads<kThreads>(), kLoadsQ = TileQ::template loads<kThreads>();
-    constexpr int kLoads = PLANES * (kLoadsP + kLoadsQ);
+    constexpr int kLoads = ZP * kLoadsP + ZQ * kLoadsQ;
     auto load = [&](uint16_t* s, uint32_t step, int i) {
         const bool any = step < last;
         const uint32_t k0 = any ? step * BK : 0;
-        const int z = i % PLANES, j = i / PLANES;
-        if (j < kLoadsP)
+        if (i < ZP * kLoadsP) {
+            const int z = i % ZP, j = i / ZP;
             TileP::template load<kThreads>(P, P.base + z * P.plane, lane_p, p0, k0, any, j, s + z * TileP::kElems);
-        else
-            TileQ::template load<kThreads>(Q, Q.base + z * Q.plane, lane_q, q0, k0, any, j - kLoadsP,
-                                           s + PLANES * TileP::kElems + z * TileQ::kElems);
+        } else {
+            const int z = (i - ZP * kLoadsP) % ZQ, j = (i - ZP * kLoadsP) / ZQ;
+            TileQ::template load<kThreads>(Q, Q.base + z * Q.plane, lane_q, q0, k0, any, j, s + kAtQ + z * TileQ::kElems);
+        }
     };
     struct Part { // a wave's operands of 16 values of k
-        bf16x8 a[PLANES][TP], b[PLANES][TQ];
+        bf16x8 a[ZP][TP], b[ZQ][TQ];
     };
     auto read = [&](Part& f, const uint16_t* s, int k) {
 #pragma unroll
-        for (int z = 0; z < PLANES; ++z) {
+        for (int z = 0; z < ZP; ++z)
 #pragma unroll
             for (int t = 0; t < TP; ++t) f.a[z][t] = TileP::read(s + z * TileP::kElems, wp + 32 * t, k);
 #pragma unroll
-            for (int t = 0; t < TQ; ++t)
-                f.b[z][t] = TileQ::read(s + PLANES * TileP::kElems + z * TileQ::kElems, wq + 32 * t, k);
-        }
+        for (int z = 0; z < ZQ; ++z)
+#pragma unroll
+            for (int t = 0; t < TQ; ++t) f.b[z][t] = TileQ::read(s + kAtQ + z * TileQ::kElems, wq + 32 * t, k);
     };
     // Nothing moves past: a part's reads stay ahead of the products that hide them, and loads between products.
     auto hold = [] { __builtin_amdgcn_sched_barrier(0); };
@@ -332,12 +348,13 @@ __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_
     // waves they fill the queue to the caches, and no wave gets past it to its products (8192 x 4096 x 32000: 1.97 ms,
     // spread 1.65 ms).
     auto multiply = [&](const Part& f, uint16_t* s, uint32_t step, int loads) {
-        constexpr int kProducts = TP * TQ * PLANES * (PLANES + 1) / 2;
+        constexpr int kPairs = ZP == 3 && ZQ == 3 ? 6 : ZP * ZQ, kProducts = TP * TQ * kPairs;
         int n = 0;
 #pragma unroll
-        for (int sum = PLANES - 1; sum >= 0; --sum)
+        for (int sum = kPairs == 6 ? 2 : ZP + ZQ - 2; sum >= 0; --sum)
 #pragma unroll
-            for (int z = 0; z <= sum; ++z)
+            for (int z = 0; z <= sum; ++z) {
+                if (z >= ZP || sum - z >= ZQ) continue;
 #pragma unroll
                 for (int t = 0; t < TP; ++t)
 #pragma unroll
@@ -351,6 +368,7 @@ __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_
                             hold();
                         }
                     }
+            }
     };
     // Once this wave's reads are done and its loads but those of the last BUFS - 2 steps have landed: when that is so
     // for all.
@@ -398,12 +416,12 @@ __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_
     finish<TP, TQ>(end, acc, p0 + wp, q0 + wq, blockIdx.y);
 }
 
-template <int PLANES, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, int BUFS, class End>
+template <int ZP, int ZQ, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, int BUFS, class End>
 hipError_t launch_product(const Operand& P, const Operand& Q, const ProductShape& s, const End& end, hipStream_t stream)
 {
     const uint64_t tiles = (uint64_t)((s.p + BP - 1) / BP) * ((s.q + BQ - 1) / BQ);
     if (tiles == 0 || tiles > 0x7fffffff || s.slices == 0 || s.slices > 65535 || s.k % BK) return hipErrorInvalidValue;
-    product_kernel<PLANES, PA, QA, BP, BQ, NWP, NWQ, BK, BUFS, End>
+    product_kernel<ZP, ZQ, PA, QA, BP, BQ, NWP, NWQ, BK, BUFS, End>
         <<<dim3((uint32_t)tiles, s.slices), NWP * NWQ * 64, 0, stream>>>(P, Q, s, end);
     return hipGetLastError();
 }
@@ -499,35 +517,118 @@ __global__ __launch_bounds__(kRowThreads) void prepare_kernel(const LossRows r, 
     }
 }
 
+// What a row's gradient is stored as: bf16, 2 bf16 whose sum has 16 bits, or the 3 of an fp32 value.
+__device__ inline void put4(const LossPiece& p, uint16_t* dl, uint32_t v, f32x4 g)
+{
+    if (p.planes == 3) {
+        uint16_t x[4][3];
+        for (int j = 0; j < 4; ++j) split3(g[j], x[j]);
+        for (int z = 0; z < 3; ++z) *(u16x4*)(dl + z * p.dl_plane + v) = {x[0][z], x[1][z], x[2][z], x[3][z]};
+        return;
+    }
+    const u16x4 hi = {bf16_of(g[0]), bf16_of(g[1]), bf16_of(g[2]), bf16_of(g[3])};
+    *(u16x4*)(dl + v) = hi;
+    if (p.planes == 2) {
+        f32x4 rest;
+        for (int j = 0; j < 4; ++j) rest[j] = g[j] - __uint_as_float((uint32_t)hi[j] << 16);
+        *(u16x4*)(dl + p.dl_plane + v) = {bf16_of(rest[0]), bf16_of(rest[1]), bf16_of(rest[2]), bf16_of(rest[3])};
+    }
+}
+__device__ inline void put1(const LossPiece& p, uint16_t* dl, uint32_t v, float g)
+{
+    if (p.planes == 3) {
+        uint16_t x[3];
+        split3(g, x);
+        for (int z = 0; z < 3; ++z) dl[z * p.dl_plane + v] = x[z];
+        return;
+    }
+    dl[v] = bf16_of(g);
+    if (p.planes == 2) dl[p.dl_plane + v] = bf16_of(g - __uint_as_float((uint32_t)dl[v] << 16));
+}
+
+// The row of hidden states as d_weight reads it: zeros where the row does not count.
+template <int THREADS>
+__device__ inline void copy_row(const RowCopy& c, uint32_t row, uint64_t n, bool counts)
+{
+    if (!c.src) return;
+    const uint16_t* from = (const uint16_t*)c.src + n * c.src_ld;
+    uint16_t* to = c.dst + (uint64_t)row * c.dst_cols;
+    for (uint32_t at = 8 * threadIdx.x; at < c.dst_cols; at += 8 * THREADS)
+        *(u16x8*)(to + at) = counts ? *(const u16x8*)(from + at) : u16x8{0, 0, 0, 0, 0, 0, 0, 0};
+}
+
+template <int THREADS>
+__device__ inline void zero_row(const LossPiece& p, uint16_t* dl)
+{
+    if (!dl) return;
+    for (uint32_t z = 0; z < p.planes; ++z)
+        for (uint64_t v = 8 * threadIdx.x; v < p.dl_ld; v += 8 * THREADS) // dl_ld: a multiple of 64
+            *(u16x8*)(dl + z * p.dl_plane + v) = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
+}
+
+// The row's target where the cross entropy has a share in it, else -1; *word: whether it is one of the vocabulary.
+__device__ inline bool labelled(const LossRows& r, uint64_t n, int64_t* label, bool* word)
+{
+    *label = -1;
+    *word = false;
+    if (!r.target || r.alpha >= 1 || r.target[n] == r.ignore_index) return false;
+    *label = r.target[n];
+    *word = *label >= 0 && *label < r.vocab;
+    return true;
+}
+
 // One workgroup a row: its log-sum-exp and loss and, with d_logits, its row of
 //   w (alpha T (p^T - q) + (1 - alpha) (p - 1_y)).
 // The factor that all rows share (grad_scale and the mean's) is left to the products' fp32 sums: here the label's term
 // is near -1 for most tokens of a new model, which bf16 holds exactly, and -1/tokens would be rounded the same way in
-// all of them.  Rounding d_logits to bf16 (fp32: to 3 planes, that is not at all) is what feeds the matrix cores; its
-// errors are independent from word to word and of the size of the gradients' own rounding.
-template <int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, const LossPiece p)
+// all of them.  Rounding d_logits to bf16 is what feeds the matrix cores; its errors are independent from word to word
+// and of the size of the gradients' own rounding.
+//
+// E16: the logits are held as exponentials in fp16 (cross entropy in bf16), in the place where d_logits goes, and
+// the factors of the parts in LDS: 4 bytes of traffic a word, not 6.  Bound by HBM.
+template <int WAVES, bool E16>
+__global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, const LossPiece p, const RowCopy copy)
 {
-    extern __shared__ float s_entries[]; // topk weights q, then topk words
+    extern __shared__ float s_more[]; // E16: a factor for each part; else topk weights q, then topk words
     __shared__ float s_wave[WAVES];
     constexpr uint32_t kThreads = WAVES * 64;
     const uint32_t row = blockIdx.x, tid = threadIdx.x;
     const uint64_t n = p.row0 + (uint64_t)row;
-    const float weight = row < p.rows ? r.row_weight[n] : 0.0f;
     uint16_t* dl = p.d_logits ? p.d_logits + (uint64_t)row * p.dl_ld : nullptr;
-    const uint32_t planes = p.f32 ? 3 : 1;
-    if (weight == 0) {
-        if (row < p.rows && tid == 0) {
-            r.token_loss[n] = 0;
-            r.lse[n] = 0;
-        }
-        if (dl)
-            for (uint32_t z = 0; z < planes; ++z)
-                for (uint64_t v = 4 * tid; v < p.dl_ld; v += 4 * kThreads) *(u16x4*)(dl + z * p.dl_plane + v) = {0, 0, 0, 0};
+    if (row >= p.rows) {
+        copy_row<kThreads>(copy, row, n, false);
+        zero_row<kThreads>(p, dl);
         return;
     }
-    const bool teach = r.alpha > 0;
+    const float given = r.token_weight ? r.token_weight[n] : 1.0f;
+    int64_t label;
+    bool word;
+    const bool has_label = labelled(r, n, &label, &word);
+    const bool teach = !E16 && r.alpha > 0;
     const float inv_t = 1 / r.temperature;
+    constexpr float kBad = 4096; // for an entry that is no word of the vocabulary: above the entries a row can have
+    float t_top = -kInf, t_count = 0;
+    if (teach) {
+        int64_t at;
+        float t;
+        for (uint32_t k = tid; k < r.topk; k += kThreads)
+            if (entry(r, n, k, &at, &t)) {
+                t_top = fmaxf(t_top, t);
+                t_count += at < r.vocab ? 1 : kBad;
+            }
+        t_top = block_max<WAVES>(t_top, s_wave);
+        t_count = block_sum<WAVES>(t_count, s_wave);
+    }
+    const bool counts = (has_label || t_count > 0) && given != 0;
+    const float weight = counts ? given : 0.0f;
+    if (tid == 0) r.row_weight[n] = weight;
+    copy_row<kThreads>(copy, row, n, counts);
+    if (!counts) {
+        if (tid == 0) r.token_loss[n] = r.lse[n] = 0;
+        zero_row<kThreads>(p, dl);
+        return;
+    }
+
     float top = -kInf;
     for (uint32_t k = tid; k < p.parts; k += kThreads) top = fmaxf(top, p.part[(uint64_t)k * p.part_ld + row].x);
     top = block_max<WAVES>(top, s_wave);
@@ -536,9 +637,10 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
     for (uint32_t k = tid; k < p.parts; k += kThreads) {
         const uint64_t at = (uint64_t)k * p.part_ld + row;
         const float2 x = p.part[at];
-        if (x.x == -kInf && x.y == 0) continue;
-        sum += x.y * exp_of(x.x - low);
-        if (p.part_t) sum_t += p.part_t[at] * exp_of((x.x - low) * inv_t);
+        const float f = x.x == -kInf ? (x.y == 0 ? 0.0f : x.y) : exp_of(x.x - low); // all words at -inf, or NaN
+        sum += x.y * f;
+        if (E16) s_more[k] = f;
+        if (p.part_t && x.x != -kInf) sum_t += p.part_t[at] * exp_of((x.x - low) * inv_t);
     }
     sum = block_sum<WAVES>(sum, s_wave);
     const float lse = low + __builtin_amdgcn_logf(sum) * kLn2;
@@ -547,39 +649,48 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
         sum_t = block_sum<WAVES>(sum_t, s_wave);
         lse_t = low * inv_t + __builtin_amdgcn_logf(sum_t) * kLn2;
     }
-    const float* logits = p.logits + (uint64_t)row * p.ld;
 
     float loss = 0, hard = 0;
-    int64_t label = -1;
-    if (r.target && r.alpha < 1 && (label = r.target[n]) != r.ignore_index) {
-        const bool word = label >= 0 && label < r.vocab;
+    if (has_label) {
         hard = word ? 1 - r.alpha : __builtin_nanf(""); // the loss and the gradient show a label that is no word
         loss = word ? hard * (lse - r.target_logit[n]) : hard;
-    } else {
-        label = -1;
     }
-    float soft = 0;
-    float* s_q = s_entries;
-    int* s_word = (int*)(s_entries + r.topk);
-    if (teach) {
-        // q over the entries that are there
-        int64_t word;
-        float t, t_top = -kInf, t_sum = 0;
-        constexpr float kBad = 4096; // above the entries a row can have
-        for (uint32_t k = tid; k < r.topk; k += kThreads)
-            if (entry(r, n, k, &word, &t)) {
-                t_top = fmaxf(t_top, t);
-                t_sum += word < r.vocab ? 1 : kBad;
+    if constexpr (E16) {
+        if (tid == 0) {
+            r.token_loss[n] = loss;
+            r.lse[n] = lse;
+        }
+        __syncthreads(); // the parts' factors
+        const float scale = weight * hard / (kE16 * sum);
+        for (uint32_t v = 8 * tid; v < p.dl_ld; v += 8 * kThreads) {
+            u16x8 g = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (v < r.vocab) {
+                const f16x8 e = *(const f16x8*)(dl + v);
+                const float f = scale * s_more[v / kPartWords];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float x = f * (float)e[j];
+                    if (v + j == (uint64_t)label) x -= weight * hard;
+                    g[j] = v + j < r.vocab ? bf16_of(x) : 0;
+                }
             }
-        t_top = block_max<WAVES>(t_top, s_wave);
-        const float count = block_sum<WAVES>(t_sum, s_wave);
-        const bool any = count > 0, bad = count >= kBad;
-        t_sum = 0;
+            *(u16x8*)(dl + v) = g;
+        }
+        return;
+    }
+
+    const float* logits = p.logits + (uint64_t)row * p.ld;
+    float soft = 0;
+    float* s_q = s_more;
+    int* s_word = (int*)(s_more + r.topk);
+    if (teach) {
+        int64_t at;
+        float t, t_sum = 0;
         for (uint32_t k = tid; k < r.topk; k += kThreads) {
-            const bool there = entry(r, n, k, &word, &t);
+            const bool there = entry(r, n, k, &at, &t);
             const float e = there ? exp_of((t - t_top) * inv_t) : 0.0f;
             s_q[k] = e;
-            s_word[k] = there && word < r.vocab ? (int)word : -1;
+            s_word[k] = there && at < r.vocab ? (int)at : -1;
             t_sum += e;
         }
         t_sum = block_sum<WAVES>(t_sum, s_wave);
@@ -587,14 +698,14 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
         float kd = 0;
         for (uint32_t k = tid; k < r.topk; k += kThreads) {
             const float q = s_q[k] / t_sum;
-            s_q[k] = any ? q : 0.0f;
+            s_q[k] = t_count > 0 ? q : 0.0f;
             if (s_word[k] < 0 || q == 0) continue;
-            entry(r, n, k, &word, &t);
+            entry(r, n, k, &at, &t);
             kd += q * (((t - t_top) * inv_t - log_sum) - (logits[s_word[k]] * inv_t - lse_t));
         }
         kd = block_sum<WAVES>(kd, s_wave);
-        if (any) {
-            soft = bad ? __builtin_nanf("") : r.alpha * r.temperature;
+        if (t_count > 0) {
+            soft = t_count >= kBad ? __builtin_nanf("") : r.alpha * r.temperature;
             loss += soft * r.temperature * kd;
         }
     }
@@ -611,15 +722,6 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
         if (soft != 0) g += soft_w * exp_of(l * inv_t - lse_t);
         return g;
     };
-    auto put = [&](uint32_t v, float g) {
-        if (p.f32) {
-            uint16_t x[3];
-            split3(g, x);
-            for (int z = 0; z < 3; ++z) dl[z * p.dl_plane + v] = x[z];
-        } else {
-            dl[v] = bf16_of(g);
-        }
-    };
     for (uint32_t v = 4 * tid; v < p.dl_ld; v += 4 * kThreads) {
         f32x4 g = {0, 0, 0, 0};
         if (v < r.vocab) {
@@ -627,29 +729,23 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
 #pragma unroll
             for (int j = 0; j < 4; ++j) g[j] = v + j < r.vocab ? gradient(v + j, l[j]) : 0.0f;
         }
-        if (p.f32) {
-            uint16_t x[4][3];
-            for (int j = 0; j < 4; ++j) split3(g[j], x[j]);
-            for (int z = 0; z < 3; ++z) *(u16x4*)(dl + z * p.dl_plane + v) = {x[0][z], x[1][z], x[2][z], x[3][z]};
-        } else {
-            *(u16x4*)(dl + v) = {bf16_of(g[0]), bf16_of(g[1]), bf16_of(g[2]), bf16_of(g[3])};
-        }
+        put4(p, dl, v, g);
     }
     if (soft == 0) return;
     // The teacher's words once more, each by the first of its entries, when the stores above have been made.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     for (uint32_t k = tid; k < r.topk; k += kThreads) {
-        const int word = s_word[k];
-        if (word < 0) continue;
+        const int at = s_word[k];
+        if (at < 0) continue;
         float q = 0;
         bool first = true;
         for (uint32_t j = 0; j < r.topk; ++j) {
-            if (s_word[j] != word) continue;
+            if (s_word[j] != at) continue;
             first &= j >= k;
             q += s_q[j];
         }
-        if (first) put(word, gradient(word, logits[word]) - soft_w * q);
+        if (first) put1(p, dl, at, gradient(at, logits[at]) - soft_w * q);
     }
 }
 
@@ -692,63 +788,85 @@ __global__ __launch_bounds__(256) void zero_kernel(void* out, uint32_t rows, uin
                 ((uint16_t*)out)[row * ld + c] = 0;
 }
 
-__global__ __launch_bounds__(256) void join_kernel(const float* slices, uint32_t n, uint32_t p, uint32_t q, const GradOut o)
+// One row of q a y, 4 values a lane: p is a multiple of 4 in `slices` (rows of ld_s).
+__global__ __launch_bounds__(256) void join_kernel(const float* slices, uint64_t slice, uint32_t ld_s, uint32_t n, uint32_t p,
+                                                   const GradOut o)
 {
-    const uint64_t count = (uint64_t)p * q, at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= count) return;
-    float x = 0;
-    for (uint32_t k = 0; k < n; ++k) x += slices[k * count + at];
+    const uint32_t at = 4 * (blockIdx.x * 256 + threadIdx.x), q = blockIdx.y;
+    if (at >= p) return;
+    const float* from = slices + (uint64_t)q * ld_s + at;
+    f32x4 x = {0, 0, 0, 0};
+    for (uint32_t k = 0; k < n; ++k) x += *(const f32x4*)(from + k * slice);
     x *= o.scale ? *o.scale : 1.0f;
-    const uint64_t to = at / p * o.ld + at % p;
-    if (o.f32)
-        ((float*)o.out)[to] = x;
-    else
-        ((uint16_t*)o.out)[to] = bf16_of(x);
+    const uint64_t to = (uint64_t)q * o.ld + at;
+    for (int j = 0; j < 4; ++j) {
+        if (at + j >= p) break;
+        if (o.f32)
+            ((float*)o.out)[to + j] = x[j];
+        else
+            ((uint16_t*)o.out)[to + j] = bf16_of(x[j]);
+    }
 }
 
 } // namespace
 
 namespace {
 
-// Workgroup tiles.  bf16: 256 x 256 (8 waves of 64 x 128) reaches 1.2-1.3 PFLOP/s where its tiles fill the 256 compute
-// units, 128 x 128 (4 waves, two workgroups a unit) 1.0-1.07.  Three planes: 256 x 128 (8 waves of 64 x 64; LDS has no
-// room for more) and 128 x 128.
+// Workgroup tiles, and what a step of 64 values of k takes one of them (us) where the compute units have one, and
+// where all have two; each round of tiles takes 3 us more.
+//   bf16:     256 x 256 (8 waves of 64 x 128): bound by the matrix cores, 1.2-1.3 PFLOP/s with all units busy
+//             128 x 128 (4 waves of 64 x 64): 1.0-1.07 PFLOP/s; alone on a unit its steps wait for their loads
+//             64 x 64 (2 waves of 64 x 32): 4 buffers hide that; for few tokens, where loads are all of the time
+//             (64 x 2048 x 8192: 9.8 us, 128 x 128 23.6 us)
+//   2 planes of d_logits: the smaller two (they are used for few tokens)
+//   3 planes: 256 x 128 (8 waves of 64 x 64; LDS has no room for more), 128 x 128 and 64 x 64
+enum Size { kSmall, kMiddle, kLarge };
 struct Tiling {
-    bool large;
+    Size size;
     uint32_t slices;
 };
 
-// The tile and the number of runs of k that finish first, by the whole rounds of tiles that the units need.
-Tiling tiling(const ProductShape& s, uint32_t planes, uint32_t most)
+// The tile and the number of runs of k that finish first.
+Tiling tiling(const ProductShape& s, uint32_t zp, uint32_t zq, uint32_t most)
 {
-    const double rate = planes == 3 ? 6 : 1; // products of planes
-    Tiling best = {false, 1};
+    Tiling best = {kMiddle, 1};
     double least = 1e30;
-    for (int large = 0; large < 2; ++large) {
-        const uint32_t bp = large ? 256 : 128, bq = large && planes == 1 ? 256 : 128;
+    for (int size = kSmall; size <= kLarge; ++size) {
+        if (size == kLarge && zp != zq) continue;
+        const uint32_t bp = size == kSmall ? 64 : size == kMiddle ? 128 : 256;
+        const uint32_t bq = size == kLarge && zp == 3 ? 128 : bp;
+        const double alone = zp == 3 ? (size == kSmall ? 0.95 : size == kMiddle ? 3.0 : 4.6)
+                                     : (size == kSmall ? 0.25 : size == kMiddle ? 0.65 : 1.7) * zq;
+        const double both = size == kLarge || zp == 3 ? 2 * alone : (size == kSmall ? 0.38 : 1.02) * zq;
         const uint64_t tiles = (uint64_t)((s.p + bp - 1) / bp) * ((s.q + bq - 1) / bq);
-        const uint32_t slots = large || planes == 3 ? 256 : 512;
-        // seconds for 64 values of k on one unit
-        const double step = 2.0 * bp * bq * 64 * rate / ((large ? (planes == 1 ? 1250e12 : 1400e12) : 1050e12) / slots);
-        for (uint32_t n = 1; n <= std::min({most, 64u, s.k / 256 ? s.k / 256 : 1}); ++n) {
-            const uint64_t rounds = (tiles * n + slots - 1) / slots;
-            const double t = rounds * ((double)((s.k / 64 + n - 1) / n) * step + 3e-6) +
-                             (n > 1 ? 3e-6 + 8.0 * s.p * s.q * n / 4e12 : 0);
-            if (t < least) least = t, best = {large != 0, n};
+        for (uint32_t n = 1; n <= std::min({most, 64u, std::max(1u, s.k / 256)}); ++n) {
+            const uint64_t all = tiles * n, pairs = all / 512, left = all % 512;
+            const double steps = (double)((s.k / 64 + n - 1) / n);
+            const double t = pairs * (steps * both + 3) +
+                             (left == 0 ? 0 : left <= 256 ? steps * alone + 3 : steps * both + 3) +
+                             (n > 1 ? 3 + 8.0 * s.p * s.q * n / 4e6 : 0);
+            if (t < least) least = t, best = {(Size)size, n};
         }
     }
     return best;
 }
 
 template <bool PA, bool QA, class End>
-hipError_t dispatch(const Operand& P, const Operand& Q, const ProductShape& s, uint32_t planes, bool large,
+hipError_t dispatch(const Operand& P, const Operand& Q, const ProductShape& s, uint32_t zp, uint32_t zq, Size size,
                     const End& end, hipStream_t stream)
 {
-    if (planes == 3)
-        return large ? launch_product<3, PA, QA, 256, 128, 4, 2, 32, 2>(P, Q, s, end, stream)
-                     : launch_product<3, PA, QA, 128, 128, 2, 2, 32, 2>(P, Q, s, end, stream);
-    return large ? launch_product<1, PA, QA, 256, 256, 4, 2, 64, 2>(P, Q, s, end, stream)
-                 : launch_product<1, PA, QA, 128, 128, 2, 2, 64, 2>(P, Q, s, end, stream);
+    if (zp == 3 && zq == 3)
+        return size == kLarge    ? launch_product<3, 3, PA, QA, 256, 128, 4, 2, 32, 2>(P, Q, s, end, stream)
+               : size == kMiddle ? launch_product<3, 3, PA, QA, 128, 128, 2, 2, 32, 2>(P, Q, s, end, stream)
+                                 : launch_product<3, 3, PA, QA, 64, 64, 1, 2, 32, 3>(P, Q, s, end, stream);
+    if constexpr (PA) // a gradient
+        if (zp == 1 && zq == 2)
+            return size == kMiddle ? launch_product<1, 2, PA, QA, 128, 128, 2, 2, 64, 2>(P, Q, s, end, stream)
+                                   : launch_product<1, 2, PA, QA, 64, 64, 1, 2, 64, 3>(P, Q, s, end, stream);
+    if (zp != 1 || zq != 1) return hipErrorInvalidValue;
+    return size == kLarge    ? launch_product<1, 1, PA, QA, 256, 256, 4, 2, 64, 2>(P, Q, s, end, stream)
+           : size == kMiddle ? launch_product<1, 1, PA, QA, 128, 128, 2, 2, 64, 2>(P, Q, s, end, stream)
+                             : launch_product<1, 1, PA, QA, 64, 64, 1, 2, 64, 4>(P, Q, s, end, stream);
 }
 
 } // namespace
@@ -756,31 +874,36 @@ hipError_t dispatch(const Operand& P, const Operand& Q, const ProductShape& s, u
 hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape& s, uint32_t planes,
                          const LogitsOut& o, hipStream_t stream)
 {
-    return dispatch<false, false>(w, h, s, planes, tiling(s, planes, 1).large, o, stream);
+    return dispatch<false, false>(w, h, s, planes, planes, tiling(s, planes, planes, 1).size, o, stream);
 }
 
-hipError_t launch_d_hidden(const Operand& w, const Operand& dl, const ProductShape& s, uint32_t planes,
+hipError_t launch_d_hidden(const Operand& w, uint32_t zp, const Operand& dl, uint32_t zq, const ProductShape& s,
                            const GradOut& o, hipStream_t stream)
 {
-    return dispatch<true, false>(w, dl, s, planes, tiling(s, planes, s.slices).large, GradEnd{o, s.p, s.q}, stream);
+    const Size size = tiling(s, zp, zq, s.slices).size;
+    return dispatch<true, false>(w, dl, s, zp, zq, size, GradEnd{o, s.p, s.q}, stream);
 }
 
-hipError_t launch_d_weight(const Operand& h, const Operand& dl, const ProductShape& s, uint32_t planes,
+hipError_t launch_d_weight(const Operand& h, uint32_t zp, const Operand& dl, uint32_t zq, const ProductShape& s,
                            const GradOut& o, hipStream_t stream)
 {
-    return dispatch<true, true>(h, dl, s, planes, tiling(s, planes, 1).large, GradEnd{o, s.p, s.q}, stream);
+    return dispatch<true, true>(h, dl, s, zp, zq, tiling(s, zp, zq, 1).size, GradEnd{o, s.p, s.q}, stream);
 }
 
-uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t planes, uint32_t most)
+uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t zp, uint32_t zq, uint32_t most)
 {
-    return tiling({p, q, k, 1}, planes, std::max(1u, most)).slices;
+    return tiling({p, q, k, 1}, zp, zq, std::max(1u, most)).slices;
 }
 
-hipError_t launch_join(const float* slices, uint32_t n, uint32_t p, uint32_t q, const GradOut& o, hipStream_t stream)
+hipError_t launch_join(const float* slices, uint64_t slice, uint32_t ld_s, uint32_t n, uint32_t p, uint32_t q,
+                       const GradOut& o, hipStream_t stream)
 {
-    const uint64_t blocks = ((uint64_t)p * q + 255) / 256;
-    if (blocks == 0 || blocks > 0x7fffffff) return hipErrorInvalidValue;
-    join_kernel<<<(uint32_t)blocks, 256, 0, stream>>>(slices, n, p, q, o);
+    for (uint32_t q0 = 0; q0 < q; q0 += 65535) { // rows of a launch
+        GradOut part = o;
+        part.out = (uint8_t*)o.out + (uint64_t)q0 * o.ld * (o.f32 ? 4 : 2);
+        join_kernel<<<dim3((p + 1023) / 1024, std::min(q - q0, 65535u)), 256, 0, stream>>>(
+            slices + (uint64_t)q0 * ld_s, slice, ld_s, n, p, part);
+    }
     return hipGetLastError();
 }
 
@@ -798,11 +921,14 @@ hipError_t launch_prepare(const LossRows* r, uint32_t row0, uint32_t rows, const
     return hipGetLastError();
 }
 
-hipError_t launch_rows(const LossRows& r, const LossPiece& p, hipStream_t stream)
+hipError_t launch_rows(const LossRows& r, const LossPiece& p, const RowCopy& copy, hipStream_t stream)
 {
-    const uint32_t all = p.d_logits ? std::max(p.rows, p.dl_rows) : p.rows;
+    const uint32_t all = std::max({p.rows, p.d_logits ? p.dl_rows : 0, copy.src ? copy.dst_rows : 0});
     if (all == 0) return hipSuccess;
-    rows_kernel<4><<<all, 256, r.topk * 8, stream>>>(r, p);
+    if (p.e16)
+        rows_kernel<4, true><<<all, 256, p.parts * 4, stream>>>(r, p, copy);
+    else
+        rows_kernel<4, false><<<all, 256, r.topk * 8, stream>>>(r, p, copy);
     return hipGetLastError();
 }
 

@@ -39,9 +39,11 @@ struct LogitsOut {
     float* part_t;         // the same sum at 1/temperature, or nullptr
     float inv_t;
     float* logits; // [tokens][ld], or nullptr
-    uint64_t ld;
+    uint16_t* e16; // [tokens][ld] exp(l - its part's max) in fp16, or nullptr
+    uint64_t ld;   // a multiple of kPartWords
 };
 constexpr uint32_t kPartWords = 64;
+constexpr uint32_t kE16Parts = 8192; // of a row held in fp16: their factors fit in LDS
 
 // What becomes of a product that is a gradient (or a slice of one).
 struct GradOut {
@@ -55,17 +57,19 @@ struct GradOut {
 
 hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape& s, uint32_t planes,
                          const LogitsOut& o, hipStream_t stream);
+// zp, zq: planes of P and Q; (1, 1), (1, 2) or (3, 3).
 // d_hidden: P = weight (k = words across rows), Q = d_logits (k contiguous)
-hipError_t launch_d_hidden(const Operand& w, const Operand& dl, const ProductShape& s, uint32_t planes,
+hipError_t launch_d_hidden(const Operand& w, uint32_t zp, const Operand& dl, uint32_t zq, const ProductShape& s,
                            const GradOut& o, hipStream_t stream);
 // d_weight: P = hidden, Q = d_logits (both with k = tokens across rows)
-hipError_t launch_d_weight(const Operand& h, const Operand& dl, const ProductShape& s, uint32_t planes,
+hipError_t launch_d_weight(const Operand& h, uint32_t zp, const Operand& dl, uint32_t zq, const ProductShape& s,
                            const GradOut& o, hipStream_t stream);
-// out = scale * sum of the slices (fp32 [slices][q][p], dense)
-hipError_t launch_join(const float* slices, uint32_t n, uint32_t p, uint32_t q, const GradOut& o, hipStream_t stream);
+// out = scale * sum of the n slices (fp32 [n][q][ld_s], `slice` apart; ld_s a multiple of 4)
+hipError_t launch_join(const float* slices, uint64_t slice, uint32_t ld_s, uint32_t n, uint32_t p, uint32_t q,
+                       const GradOut& o, hipStream_t stream);
 hipError_t launch_zero(void* out, uint32_t rows, uint32_t cols, uint64_t ld, bool f32, hipStream_t stream);
-// The run count that fills the GPU, at most most.
-uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t planes, uint32_t most);
+// Into how many runs of k to cut d_hidden, at most `most`.
+uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t zp, uint32_t zq, uint32_t most);
 
 // ---- rows of the loss (loss_kernels.hip) ----
 
@@ -104,10 +108,12 @@ struct RowCopy {
 };
 hipError_t launch_prepare(const LossRows* r, uint32_t row0, uint32_t rows, const RowCopy& c, hipStream_t stream);
 
-// From the statistics of `parts` runs of words to token_loss and lse of rows
-// [row0, row0 + rows); part, part_t and logits are the piece's own.  With
-// d_logits also writes its rows ([3 planes where f32][.][dl_ld], dl_rows of
-// them: zeros beyond the vocabulary and beyond `rows`).
+// From the statistics of `parts` runs of words to row_weight, token_loss and
+// lse of rows [row0, row0 + rows); part, part_t and logits are the piece's own.
+// With d_logits also writes its rows ([planes][.][dl_ld], dl_rows of them:
+// zeros beyond the vocabulary and beyond `rows`); e16: from the exponentials
+// that d_logits holds.  With copy.src (bf16, 16-byte aligned rows of dst_cols)
+// also copies those rows, zeros for the ones that do not count.
 struct LossPiece {
     uint32_t row0, rows, parts;
     uint32_t part_ld; // rows between two parts
@@ -117,10 +123,10 @@ struct LossPiece {
     uint64_t ld;
     uint16_t* d_logits;
     uint64_t dl_ld, dl_plane;
-    uint32_t dl_rows;
-    bool f32;
+    uint32_t dl_rows, planes;
+    bool e16;
 };
-hipError_t launch_rows(const LossRows& r, const LossPiece& p, hipStream_t stream);
+hipError_t launch_rows(const LossRows& r, const LossPiece& p, const RowCopy& copy, hipStream_t stream);
 // scale (from row_weight) and, if `total`, the loss.
 hipError_t launch_finish(const LossRows& r, bool total, hipStream_t stream);
 
