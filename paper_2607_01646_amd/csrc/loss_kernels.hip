@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ops_internal.h"
 
@@ -26,6 +27,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u16x4 u16x4_any __attribute__((aligned(2)));
+typedef u16x8 u16x8_any __attribute__((aligned(2)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kInf = __builtin_inff();
@@ -36,20 +38,18 @@ __device__ inline uint16_t bf16_of(float x) { return __builtin_bit_cast(uint16_t
 
 // An fp32 value as the sum of 3 bf16: each takes the next 8 bits of the
 // significand, cut off, not rounded, so the rests are exact and all 24 bits are
-// kept.  A value that is not finite is its first plane alone.
+// kept.  A value that is not finite is its first plane alone (a NaN whose bits
+// would all be cut off keeps one).
 __device__ inline void split3(float x, uint16_t (&p)[3])
 {
-    const uint32_t a = __float_as_uint(x) & 0xFFFF0000u;
-    p[0] = (uint16_t)(a >> 16);
-    if ((a & 0x7F800000u) == 0x7F800000u) {
-        if ((__float_as_uint(x) & 0x007FFFFFu) != 0) p[0] |= 0x40; // a NaN whose payload was cut off stays one
-        p[1] = p[2] = 0;
-        return;
-    }
+    const uint32_t u = __float_as_uint(x), a = u & 0xFFFF0000u;
+    const bool finite = (u & 0x7F800000u) != 0x7F800000u, nan = !finite && (u & 0x007FFFFFu) != 0;
     const float r = x - __uint_as_float(a);
     const uint32_t b = __float_as_uint(r) & 0xFFFF0000u;
-    p[1] = (uint16_t)(b >> 16);
-    p[2] = (uint16_t)(__float_as_uint(r - __uint_as_float(b)) >> 16);
+    const uint32_t c = __float_as_uint(r - __uint_as_float(b));
+    p[0] = (uint16_t)((a >> 16) | (nan ? 0x40 : 0));
+    p[1] = finite ? (uint16_t)(b >> 16) : 0;
+    p[2] = finite ? (uint16_t)(c >> 16) : 0;
 }
 
 // ---- tiles of an operand in LDS ----
@@ -144,70 +144,113 @@ struct Tile {
 // ---- epilogues ----
 //
 // acc[tp][tq] holds out[q][p] of 32 x 32 tiles: q = q0 + 32 tq + lane % 32 and, for register i,
-// p = p0 + 32 tp + 8 (i / 4) + 4 (lane / 32) + i % 4: every lane has runs of 4 consecutive p of one q.
+// p = p0 + 32 tp + 8 (i / 4) + 4 (lane / 32) + i % 4: every lane has runs of 4 consecutive p of one q.  They are what a
+// workgroup does while no product is made, so they are kept short: tiles that lie inside the output check no bounds.
+
+// Two runs of 4 values in 16 bits, p + 4 half.. and p + 8 + 4 half.., of the lanes of both halves: as 8 consecutive ones,
+// p + 8 half.., for one store of 16 bytes.
+__device__ inline u16x8 pair_of(uint2 a, uint2 b)
+{
+    const auto x = __builtin_amdgcn_permlane32_swap(a.x, b.x, false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(a.y, b.y, false, false);
+    const uint4 r = {x[0], y[0], x[1], y[1]};
+    return __builtin_bit_cast(u16x8, r);
+}
+__device__ inline uint2 bf16_run(f32x4 x)
+{
+    return __builtin_bit_cast(uint2, u16x4{bf16_of(x[0]), bf16_of(x[1]), bf16_of(x[2]), bf16_of(x[3])});
+}
+
+// What a lane reads for its epilogue ahead of the products.
+template <class End, int TQ>
+struct Early {
+    __device__ inline Early(const End&, uint32_t) {}
+};
+template <int TQ>
+struct Early<LogitsOut, TQ> {
+    int32_t target[TQ];
+    __device__ inline Early(const LogitsOut& o, uint32_t q0)
+    {
+#pragma unroll
+        for (int t = 0; t < TQ; ++t) {
+            const uint32_t q = q0 + 32 * t + (threadIdx.x & 31);
+            const int64_t y = o.target && q < o.tokens ? o.target[q] : -1;
+            target[t] = y >= 0 && y < o.vocab ? (int32_t)y : -1;
+        }
+    }
+};
 
 template <int TP, int TQ>
-__device__ inline void finish(const LogitsOut& o, f32x16 (&acc)[TP][TQ], uint32_t wave_p0, uint32_t q0, uint32_t)
+__device__ inline void finish(const LogitsOut& o, const Early<LogitsOut, TQ>& early, f32x16 (&acc)[TP][TQ],
+                              uint32_t wave_p0, uint32_t q0, uint32_t)
 {
-    constexpr int kTiles = kPartWords / 32; // of a part
+    constexpr int kTiles = kPartWords / 32, kMine = kTiles * 16; // of a part; a lane's words of it
     static_assert(TP % kTiles == 0, "a wave's words are whole parts");
-    const uint32_t lane = threadIdx.x & 63, up = 4 * (lane >> 5);
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
 #pragma unroll
     for (int part = 0; part < TP / kTiles; ++part) {
         const uint32_t p0 = wave_p0 + part * kPartWords;
         if (p0 >= o.vocab) break;
+        const bool whole = p0 + kPartWords <= o.vocab;
 #pragma unroll
         for (int tq = 0; tq < TQ; ++tq) {
             const uint32_t q = q0 + 32 * tq + (lane & 31);
             const bool here = q < o.tokens;
-            float x[kTiles * 16]; // of words p0 + 32 (j / 16) + 8 (j / 4 % 4) + up + j % 4
-            float top = -kInf;
+            float x[kMine]; // of words p0 + 32 (j / 16) + 8 (j / 4 % 4) + 4 half + j % 4
 #pragma unroll
-            for (int j = 0; j < kTiles * 16; ++j) {
-                x[j] = acc[part * kTiles + j / 16][tq][j % 16];
-                const uint32_t p = p0 + 32 * (j / 16) + 8 * (j / 4 % 4) + up + j % 4;
-                top = p < o.vocab ? fmaxf(top, x[j]) : top; // fmaxf passes a NaN by; the sum below does not
+            for (int j = 0; j < kMine; ++j) x[j] = acc[part * kTiles + j / 16][tq][j % 16];
+            if (!whole) {
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+                    if (p0 + 32 * (j / 16) + 8 * (j / 4 % 4) + 4 * half + j % 4 >= o.vocab) x[j] = -kInf;
             }
+            const uint32_t t = (uint32_t)early.target[tq] - p0;
+            if (t < kPartWords && (t >> 2 & 1) == half) {
+                const uint32_t mine = (t >> 5) * 16 + (t >> 3 & 3) * 4 + (t & 3);
+                float l = 0;
+#pragma unroll
+                for (int j = 0; j < kMine; ++j) l = mine == j ? x[j] : l;
+                o.target_logit[q] = l;
+            }
+            if (o.logits && here) {
+                float* row = o.logits + (uint64_t)q * o.ld + p0 + 4 * half; // ld covers whole parts
+#pragma unroll
+                for (int j = 0; j < kMine; j += 4)
+                    *(f32x4*)(row + 32 * (j / 16) + 8 * (j / 4 % 4)) = {x[j], x[j + 1], x[j + 2], x[j + 3]};
+            }
+            float top = -kInf; // fmaxf passes a NaN by; the sum below does not
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) top = fmaxf(top, x[j]);
             top = fmaxf(top, __shfl_xor(top, 32));
             const float low = top == -kInf ? 0.0f : top;
             float sum = 0, sum_t = 0;
+            if (o.part_t) {
 #pragma unroll
-            for (int j = 0; j < kTiles * 16; ++j) {
-                const uint32_t p = p0 + 32 * (j / 16) + 8 * (j / 4 % 4) + up + j % 4;
-                sum += p < o.vocab ? exp_of(x[j] - low) : 0.0f;
-                if (o.part_t) sum_t += p < o.vocab ? exp_of((x[j] - low) * o.inv_t) : 0.0f;
+                for (int j = 0; j < kMine; ++j) sum_t += exp_of((x[j] - low) * o.inv_t);
+                sum_t += __shfl_xor(sum_t, 32);
+            }
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+                x[j] = exp_of(x[j] - low);
+                sum += x[j];
             }
             sum += __shfl_xor(sum, 32);
-            if (o.part_t) sum_t += __shfl_xor(sum_t, 32);
-            if (!here) continue;
-            if (lane < 32) {
+            if (here && half == 0) {
                 const uint64_t at = (uint64_t)(p0 / kPartWords) * o.tokens + q;
                 o.part[at] = make_float2(top, sum);
                 if (o.part_t) o.part_t[at] = sum_t;
             }
-            if (o.target) {
-                const int64_t t = o.target[q] - p0;
-                if (t >= 0 && t < kPartWords && p0 + t < o.vocab)
-#pragma unroll
-                    for (int j = 0; j < kTiles * 16; ++j)
-                        if ((uint32_t)t == 32u * (j / 16) + 8 * (j / 4 % 4) + up + j % 4) o.target_logit[q] = x[j];
-            }
             if (o.e16) {
                 // exp(l - top) 2^15, in 11 bits from 2^-29 on: its rounding is an eighth of d_logits' own
-                _Float16* row = (_Float16*)o.e16 + (uint64_t)q * o.ld + p0 + up;
+                _Float16* row = (_Float16*)o.e16 + (uint64_t)q * o.ld + p0 + 8 * half;
 #pragma unroll
-                for (int j = 0; j < kTiles * 16; j += 4) {
-                    f16x4 e;
+                for (int j = 0; j < kMine; j += 8) {
+                    f16x4 e[2];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = (_Float16)(exp_of(x[j + i] - low) * kE16);
-                    *(f16x4*)(row + 32 * (j / 16) + 8 * (j / 4 % 4)) = e;
+                    for (int i = 0; i < 8; ++i) e[i / 4][i % 4] = (_Float16)(x[j + i] * kE16);
+                    const u16x8 v = pair_of(__builtin_bit_cast(uint2, e[0]), __builtin_bit_cast(uint2, e[1]));
+                    if (here) *(u16x8*)(row + 32 * (j / 16) + 8 * (j / 4 % 4)) = v;
                 }
-            }
-            if (o.logits) {
-                float* row = o.logits + (uint64_t)q * o.ld + p0 + up; // ld covers whole parts
-#pragma unroll
-                for (int j = 0; j < kTiles * 16; j += 4)
-                    *(f32x4*)(row + 32 * (j / 16) + 8 * (j / 4 % 4)) = {x[j], x[j + 1], x[j + 2], x[j + 3]};
             }
         }
     }
@@ -218,47 +261,59 @@ struct GradEnd {
     uint32_t p, q;
 };
 
+template <int TQ>
+struct Early<GradEnd, TQ> {
+    float scale;
+    __device__ inline Early(const GradEnd& e, uint32_t) : scale(e.o.scale ? *e.o.scale : 1.0f) {}
+};
+
 template <int TP, int TQ>
-__device__ inline void finish(const GradEnd& e, f32x16 (&acc)[TP][TQ], uint32_t p0, uint32_t q0, uint32_t slice)
+__device__ inline void finish(const GradEnd& e, const Early<GradEnd, TQ>& early, f32x16 (&acc)[TP][TQ], uint32_t p0,
+                              uint32_t q0, uint32_t slice)
 {
     const GradOut& o = e.o;
-    const uint32_t lane = threadIdx.x & 63, up = 4 * (lane >> 5);
-    const float scale = o.scale ? *o.scale : 1.0f;
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
+    const bool whole = p0 + 32 * TP <= e.p;
 #pragma unroll
     for (int tq = 0; tq < TQ; ++tq) {
         const uint32_t q = q0 + 32 * tq + (lane & 31);
-        if (q >= e.q) continue;
+        const bool here = q < e.q;
+        const uint64_t row = (uint64_t)slice * o.slice + (uint64_t)q * o.ld;
 #pragma unroll
         for (int tp = 0; tp < TP; ++tp)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const uint32_t p = p0 + 32 * tp + 8 * (i >> 2) + up;
-                if (p >= e.p) continue;
-                const uint32_t n = min(4u, e.p - p);
-                f32x4 x = {acc[tp][tq][i], acc[tp][tq][i + 1], acc[tp][tq][i + 2], acc[tp][tq][i + 3]};
-                if (o.add) {
-                    const float* add = o.add + (uint64_t)q * o.add_ld + p;
-                    for (uint32_t j = 0; j < 4; ++j)
-                        if (j < n) x[j] += add[j];
+            for (int i = 0; i < 16; i += 8) {
+                f32x4 x[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int r = i + 4 * u;
+                    const uint32_t p = p0 + 32 * tp + 2 * r + 4 * half;
+                    x[u] = {acc[tp][tq][r], acc[tp][tq][r + 1], acc[tp][tq][r + 2], acc[tp][tq][r + 3]};
+                    if (o.add && here) {
+                        const float* add = o.add + (uint64_t)q * o.add_ld + p;
+                        for (uint32_t j = 0; j < 4; ++j)
+                            if (p + j < e.p) x[u][j] += add[j];
+                    }
+                    x[u] *= early.scale;
+                    if (o.f32 && here) {
+                        float* out = (float*)o.out + row + p;
+                        if (whole)
+                            *(f32x4_any*)out = x[u];
+                        else
+                            for (uint32_t j = 0; j < 4; ++j)
+                                if (p + j < e.p) out[j] = x[u][j];
+                    }
                 }
-                x *= scale;
-                const uint64_t at = (uint64_t)slice * o.slice + (uint64_t)q * o.ld + p;
-                if (o.f32) {
-                    float* out = (float*)o.out + at;
-                    if (n == 4)
-                        *(f32x4_any*)out = x;
-                    else
-                        for (uint32_t j = 0; j < 3; ++j)
-                            if (j < n) out[j] = x[j];
-                } else {
-                    uint16_t* out = (uint16_t*)o.out + at;
-                    const u16x4 u = {bf16_of(x[0]), bf16_of(x[1]), bf16_of(x[2]), bf16_of(x[3])};
-                    if (n == 4)
-                        *(u16x4_any*)out = u;
-                    else
-                        for (uint32_t j = 0; j < 3; ++j)
-                            if (j < n) out[j] = u[j];
-                }
+                if (o.f32) continue;
+                const u16x8 v = pair_of(bf16_run(x[0]), bf16_run(x[1]));
+                const uint32_t p = p0 + 32 * tp + 2 * i + 8 * half;
+                uint16_t* out = (uint16_t*)o.out + row + p;
+                if (!here) continue;
+                if (whole)
+                    *(u16x8_any*)out = v;
+                else
+                    for (uint32_t j = 0; j < 8; ++j)
+                        if (p + j < e.p) out[j] = v[j];
             }
     }
 }
@@ -305,6 +360,7 @@ __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wp = (wave % NWP) * (BP / NWP), wq = (wave / NWP) * (BQ / NWQ);
 
+    const Early<End, TQ> early(end, q0 + wq);
     f32x16 acc[TP][TQ];
 #pragma unroll
     for (int a = 0; a < TP; ++a)
@@ -413,7 +469,7 @@ __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_
     if (BUFS > 2 && step + 1 < last) one_step(s1, s2, step + 1);
     if (BUFS > 3 && step + 2 < last) one_step(s2, s3, step + 2);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // no load is left that would write the LDS of another workgroup
-    finish<TP, TQ>(end, acc, p0 + wp, q0 + wq, blockIdx.y);
+    finish<TP, TQ>(end, early, acc, p0 + wp, q0 + wq, blockIdx.y);
 }
 
 template <int ZP, int ZQ, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, int BUFS, class End>
@@ -477,6 +533,25 @@ __device__ inline bool entry(const LossRows& r, uint64_t n, uint32_t k, int64_t*
     return *word >= 0 && *logit != -kInf;
 }
 
+// 8 values as PLANES planes of bf16, `plane` apart: rounded, 2 bf16 whose sum has 16 bits, or the 3 of an fp32 value.
+template <int PLANES>
+__device__ inline void put8(uint16_t* to, uint64_t plane, const float (&g)[8])
+{
+    u16x8 x[PLANES];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (PLANES == 3) {
+            uint16_t y[3];
+            split3(g[j], y);
+            for (int z = 0; z < 3; ++z) x[z][j] = y[z];
+        } else {
+            x[0][j] = bf16_of(g[j]);
+            if constexpr (PLANES == 2) x[1][j] = bf16_of(g[j] - __uint_as_float((uint32_t)x[0][j] << 16));
+        }
+    }
+#pragma unroll
+    for (int z = 0; z < PLANES; ++z) *(u16x8*)(to + z * plane) = x[z];
+}
 // One wave a row.
 __global__ __launch_bounds__(kRowThreads) void prepare_kernel(const LossRows r, bool weigh, uint32_t row0, uint32_t rows,
                                                               const RowCopy c)
@@ -498,42 +573,31 @@ __global__ __launch_bounds__(kRowThreads) void prepare_kernel(const LossRows r, 
     if (!c.src || row >= c.dst_rows) return;
     const uint64_t src = (uint64_t)(row0 + row) * c.src_ld;
     uint16_t* dst = c.dst + (uint64_t)row * c.dst_cols;
-    for (uint32_t at = 4 * lane; at < c.dst_cols; at += 256) { // dst_cols: a multiple of 64
+    for (uint32_t at = 8 * lane; at < c.dst_cols; at += 512) { // dst_cols: a multiple of 64
         if (c.f32) {
-            uint16_t x[4][3];
-            for (int j = 0; j < 4; ++j)
-                split3(counts && at + j < c.cols ? ((const float*)c.src)[src + at + j] : 0.0f, x[j]);
-            for (int z = 0; z < 3; ++z) *(u16x4*)(dst + z * c.plane + at) = {x[0][z], x[1][z], x[2][z], x[3][z]};
-        } else {
-            u16x4 x = {0, 0, 0, 0};
-            const uint16_t* from = (const uint16_t*)c.src + src + at;
-            if (counts && at + 4 <= c.cols)
-                x = *(const u16x4_any*)from;
-            else if (counts)
-                for (int j = 0; j < 3; ++j)
+            const float* from = (const float*)c.src + src + at;
+            float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (counts && at + 8 <= c.cols) {
+                const f32x4 a = *(const f32x4_any*)from, b = *(const f32x4_any*)(from + 4);
+                for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
+            } else if (counts) {
+                for (int j = 0; j < 7; ++j)
                     if (at + j < c.cols) x[j] = from[j];
-            *(u16x4*)(dst + at) = x;
+            }
+            put8<3>(dst + at, c.plane, x);
+        } else {
+            u16x8 x = {0, 0, 0, 0, 0, 0, 0, 0};
+            const uint16_t* from = (const uint16_t*)c.src + src + at;
+            if (counts && at + 8 <= c.cols)
+                x = *(const u16x8_any*)from;
+            else if (counts)
+                for (int j = 0; j < 7; ++j)
+                    if (at + j < c.cols) x[j] = from[j];
+            *(u16x8*)(dst + at) = x;
         }
     }
 }
 
-// What a row's gradient is stored as: bf16, 2 bf16 whose sum has 16 bits, or the 3 of an fp32 value.
-__device__ inline void put4(const LossPiece& p, uint16_t* dl, uint32_t v, f32x4 g)
-{
-    if (p.planes == 3) {
-        uint16_t x[4][3];
-        for (int j = 0; j < 4; ++j) split3(g[j], x[j]);
-        for (int z = 0; z < 3; ++z) *(u16x4*)(dl + z * p.dl_plane + v) = {x[0][z], x[1][z], x[2][z], x[3][z]};
-        return;
-    }
-    const u16x4 hi = {bf16_of(g[0]), bf16_of(g[1]), bf16_of(g[2]), bf16_of(g[3])};
-    *(u16x4*)(dl + v) = hi;
-    if (p.planes == 2) {
-        f32x4 rest;
-        for (int j = 0; j < 4; ++j) rest[j] = g[j] - __uint_as_float((uint32_t)hi[j] << 16);
-        *(u16x4*)(dl + p.dl_plane + v) = {bf16_of(rest[0]), bf16_of(rest[1]), bf16_of(rest[2]), bf16_of(rest[3])};
-    }
-}
 __device__ inline void put1(const LossPiece& p, uint16_t* dl, uint32_t v, float g)
 {
     if (p.planes == 3) {
@@ -650,6 +714,7 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
         lse_t = low * inv_t + __builtin_amdgcn_logf(sum_t) * kLn2;
     }
 
+    const uint32_t target = word ? (uint32_t)label : ~0u; // no word is as large
     float loss = 0, hard = 0;
     if (has_label) {
         hard = word ? 1 - r.alpha : __builtin_nanf(""); // the loss and the gradient show a label that is no word
@@ -663,18 +728,22 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
         __syncthreads(); // the parts' factors
         const float scale = weight * hard / (kE16 * sum);
         for (uint32_t v = 8 * tid; v < p.dl_ld; v += 8 * kThreads) {
-            u16x8 g = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (v < r.vocab) {
-                const f16x8 e = *(const f16x8*)(dl + v);
-                const float f = scale * s_more[v / kPartWords];
+            const f16x8 e = *(const f16x8*)(dl + v);
+            const float f = v < r.vocab ? scale * s_more[v / kPartWords] : 0.0f;
+            float g[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float x = f * (float)e[j];
-                    if (v + j == (uint64_t)label) x -= weight * hard;
-                    g[j] = v + j < r.vocab ? bf16_of(x) : 0;
-                }
+            for (int j = 0; j < 8; ++j) g[j] = f * (float)e[j];
+            if (target - v < 8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (target - v == j) g[j] -= weight * hard;
             }
-            *(u16x8*)(dl + v) = g;
+            if (v + 8 > r.vocab) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (v + j >= r.vocab) g[j] = 0;
+            }
+            put8<1>(dl + v, 0, g);
         }
         return;
     }
@@ -716,21 +785,37 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
     if (!dl) return;
 
     const float soft_w = weight * soft, hard_w = weight * hard;
-    auto gradient = [&](uint32_t v, float l) {
+    auto gradient = [&](float l) {
         float g = 0;
-        if (hard != 0) g = hard_w * (exp_of(l - lse) - (v == (uint64_t)label ? 1.0f : 0.0f));
+        if (hard != 0) g = hard_w * exp_of(l - lse);
         if (soft != 0) g += soft_w * exp_of(l * inv_t - lse_t);
         return g;
     };
-    for (uint32_t v = 4 * tid; v < p.dl_ld; v += 4 * kThreads) {
-        f32x4 g = {0, 0, 0, 0};
-        if (v < r.vocab) {
-            const f32x4 l = *(const f32x4*)(logits + v);
+    auto store = [&](auto planes) {
+        for (uint32_t v = 8 * tid; v < p.dl_ld; v += 8 * kThreads) {
+            const f32x4 a = *(const f32x4*)(logits + v), b = *(const f32x4*)(logits + v + 4);
+            float g[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) g[j] = v + j < r.vocab ? gradient(v + j, l[j]) : 0.0f;
+            for (int j = 0; j < 4; ++j) g[j] = gradient(a[j]), g[4 + j] = gradient(b[j]);
+            if (target - v < 8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (target - v == j) g[j] -= hard_w;
+            }
+            if (v + 8 > r.vocab) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (v + j >= r.vocab) g[j] = 0;
+            }
+            put8<planes>(dl + v, p.dl_plane, g);
         }
-        put4(p, dl, v, g);
-    }
+    };
+    if (p.planes == 1)
+        store(std::integral_constant<int, 1>());
+    else if (p.planes == 2)
+        store(std::integral_constant<int, 2>());
+    else
+        store(std::integral_constant<int, 3>());
     if (soft == 0) return;
     // The teacher's words once more, each by the first of its entries, when the stores above have been made.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -745,7 +830,7 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
             first &= j >= k;
             q += s_q[j];
         }
-        if (first) put1(p, dl, at, gradient(at, logits[at]) - soft_w * q);
+        if (first) put1(p, dl, at, gradient(logits[at]) - soft_w * q - ((uint32_t)at == target ? hard_w : 0.0f));
     }
 }
 
@@ -753,10 +838,23 @@ __global__ __launch_bounds__(1024) void finish_kernel(const LossRows r, bool tot
 {
     __shared__ double s[2][16];
     double weight = 0, loss = 0;
-    for (uint32_t n = threadIdx.x; n < r.tokens; n += 1024) {
-        const float w = r.row_weight[n];
-        weight += w;
-        if (total && w != 0) loss += (double)w * r.token_loss[n];
+    for (uint32_t n0 = 4 * threadIdx.x; n0 < r.tokens; n0 += 4096) {
+        f32x4 w = {0, 0, 0, 0}, x = {0, 0, 0, 0};
+        if (n0 + 4 <= r.tokens) {
+            w = *(const f32x4_any*)(r.row_weight + n0);
+            if (total) x = *(const f32x4_any*)(r.token_loss + n0);
+        } else {
+            for (int j = 0; j < 3; ++j)
+                if (n0 + j < r.tokens) {
+                    w[j] = r.row_weight[n0 + j];
+                    if (total) x[j] = r.token_loss[n0 + j];
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            weight += w[j];
+            if (w[j] != 0) loss += (double)w[j] * x[j];
+        }
     }
     for (int o = 32; o; o >>= 1) {
         weight += __shfl_xor(weight, o);
