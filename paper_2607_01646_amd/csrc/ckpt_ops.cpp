@@ -283,6 +283,7 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
         LogitsOut lo = {};
         lo.vocab = (uint32_t)v;
         lo.tokens = (uint32_t)rows;
+        lo.parts = l.parts;
         lo.target = r.target ? r.target + row0 : nullptr;
         lo.target_logit = (float*)(w + l.target_logit);
         lo.part = (float2*)(w + l.part);
@@ -297,7 +298,6 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
         p.row0 = (uint32_t)row0;
         p.rows = (uint32_t)rows;
         p.parts = l.parts;
-        p.part_ld = (uint32_t)rows;
         p.part = lo.part;
         p.part_t = lo.part_t;
         p.logits = lo.logits;

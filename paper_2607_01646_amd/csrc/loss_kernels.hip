@@ -236,7 +236,7 @@ __device__ inline void finish(const LogitsOut& o, const Early<LogitsOut, TQ>& ea
             }
             sum += __shfl_xor(sum, 32);
             if (here && half == 0) {
-                const uint64_t at = (uint64_t)(p0 / kPartWords) * o.tokens + q;
+                const uint64_t at = (uint64_t)q * o.parts + p0 / kPartWords;
                 o.part[at] = make_float2(top, sum);
                 if (o.part_t) o.part_t[at] = sum_t;
             }
@@ -653,7 +653,7 @@ __device__ inline bool labelled(const LossRows& r, uint64_t n, int64_t* label, b
 template <int WAVES, bool E16>
 __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, const LossPiece p, const RowCopy copy)
 {
-    extern __shared__ float s_more[]; // E16: a factor for each part; else topk weights q, then topk words
+    extern __shared__ float s_more[]; // E16: a factor for each part; else the teacher's entries
     __shared__ float s_wave[WAVES];
     constexpr uint32_t kThreads = WAVES * 64;
     const uint32_t row = blockIdx.x, tid = threadIdx.x;
@@ -671,15 +671,25 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
     const bool teach = !E16 && r.alpha > 0;
     const float inv_t = 1 / r.temperature;
     constexpr float kBad = 4096; // for an entry that is no word of the vocabulary: above the entries a row can have
+    // The teacher's entries: logit, then q; word, -1 where there is none; the student's logit.
+    float* s_q = s_more;
+    float* s_own = s_more + r.topk;
+    int* s_word = (int*)(s_more + 2 * r.topk);
+    const float* logits = E16 ? nullptr : p.logits + (uint64_t)row * p.ld;
     float t_top = -kInf, t_count = 0;
     if (teach) {
-        int64_t at;
-        float t;
-        for (uint32_t k = tid; k < r.topk; k += kThreads)
-            if (entry(r, n, k, &at, &t)) {
+        for (uint32_t k = tid; k < r.topk; k += kThreads) {
+            int64_t at;
+            float t;
+            const bool there = entry(r, n, k, &at, &t), known = there && at < r.vocab;
+            s_q[k] = there ? t : -kInf;
+            s_word[k] = known ? (int)at : -1;
+            s_own[k] = known ? logits[at] : 0.0f;
+            if (there) {
                 t_top = fmaxf(t_top, t);
-                t_count += at < r.vocab ? 1 : kBad;
+                t_count += known ? 1 : kBad;
             }
+        }
         t_top = block_max<WAVES>(t_top, s_wave);
         t_count = block_sum<WAVES>(t_count, s_wave);
     }
@@ -694,22 +704,23 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
     }
 
     float top = -kInf;
-    for (uint32_t k = tid; k < p.parts; k += kThreads) top = fmaxf(top, p.part[(uint64_t)k * p.part_ld + row].x);
+    const float2* part = p.part + (uint64_t)row * p.parts;
+    const float* part_t = p.part_t ? p.part_t + (uint64_t)row * p.parts : nullptr;
+    for (uint32_t k = tid; k < p.parts; k += kThreads) top = fmaxf(top, part[k].x);
     top = block_max<WAVES>(top, s_wave);
     const float low = top == -kInf ? 0.0f : top;
     float sum = 0, sum_t = 0;
     for (uint32_t k = tid; k < p.parts; k += kThreads) {
-        const uint64_t at = (uint64_t)k * p.part_ld + row;
-        const float2 x = p.part[at];
+        const float2 x = part[k];
         const float f = x.x == -kInf ? (x.y == 0 ? 0.0f : x.y) : exp_of(x.x - low); // all words at -inf, or NaN
         sum += x.y * f;
         if (E16) s_more[k] = f;
-        if (p.part_t && x.x != -kInf) sum_t += p.part_t[at] * exp_of((x.x - low) * inv_t);
+        if (part_t && x.x != -kInf) sum_t += part_t[k] * exp_of((x.x - low) * inv_t);
     }
     sum = block_sum<WAVES>(sum, s_wave);
     const float lse = low + __builtin_amdgcn_logf(sum) * kLn2;
     float lse_t = lse;
-    if (p.part_t) {
+    if (part_t) {
         sum_t = block_sum<WAVES>(sum_t, s_wave);
         lse_t = low * inv_t + __builtin_amdgcn_logf(sum_t) * kLn2;
     }
@@ -748,29 +759,17 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
         return;
     }
 
-    const float* logits = p.logits + (uint64_t)row * p.ld;
     float soft = 0;
-    float* s_q = s_more;
-    int* s_word = (int*)(s_more + r.topk);
     if (teach) {
-        int64_t at;
-        float t, t_sum = 0;
-        for (uint32_t k = tid; k < r.topk; k += kThreads) {
-            const bool there = entry(r, n, k, &at, &t);
-            const float e = there ? exp_of((t - t_top) * inv_t) : 0.0f;
-            s_q[k] = e;
-            s_word[k] = there && at < r.vocab ? (int)at : -1;
-            t_sum += e;
-        }
+        float t_sum = 0;
+        for (uint32_t k = tid; k < r.topk; k += kThreads) t_sum += exp_of((s_q[k] - t_top) * inv_t);
         t_sum = block_sum<WAVES>(t_sum, s_wave);
         const float log_sum = __builtin_amdgcn_logf(t_sum) * kLn2;
         float kd = 0;
         for (uint32_t k = tid; k < r.topk; k += kThreads) {
-            const float q = s_q[k] / t_sum;
-            s_q[k] = t_count > 0 ? q : 0.0f;
-            if (s_word[k] < 0 || q == 0) continue;
-            entry(r, n, k, &at, &t);
-            kd += q * (((t - t_top) * inv_t - log_sum) - (logits[s_word[k]] * inv_t - lse_t));
+            const float log_q = (s_q[k] - t_top) * inv_t - log_sum, q = t_count > 0 ? exp_of(log_q) : 0.0f;
+            s_q[k] = q;
+            if (s_word[k] >= 0 && q != 0) kd += q * (log_q - (s_own[k] * inv_t - lse_t));
         }
         kd = block_sum<WAVES>(kd, s_wave);
         if (t_count > 0) {
@@ -830,7 +829,7 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
             first &= j >= k;
             q += s_q[j];
         }
-        if (first) put1(p, dl, at, gradient(logits[at]) - soft_w * q - ((uint32_t)at == target ? hard_w : 0.0f));
+        if (first) put1(p, dl, at, gradient(s_own[k]) - soft_w * q - ((uint32_t)at == target ? hard_w : 0.0f));
     }
 }
 
@@ -1026,7 +1025,7 @@ hipError_t launch_rows(const LossRows& r, const LossPiece& p, const RowCopy& cop
     if (p.e16)
         rows_kernel<4, true><<<all, 256, p.parts * 4, stream>>>(r, p, copy);
     else
-        rows_kernel<4, false><<<all, 256, r.topk * 8, stream>>>(r, p, copy);
+        rows_kernel<4, false><<<all, 256, r.topk * 12, stream>>>(r, p, copy);
     return hipGetLastError();
 }
 

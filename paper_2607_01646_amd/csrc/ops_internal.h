@@ -32,10 +32,10 @@ struct ProductShape {
 
 // What becomes of a tile of l = P Q: the logits' statistics.
 struct LogitsOut {
-    uint32_t vocab, tokens;
+    uint32_t vocab, tokens, parts;
     const int64_t* target; // or nullptr
     float* target_logit;   // [tokens], written where the target is a word
-    float2* part;          // [parts][tokens]: (max, sum exp(l - max)) over each run of kPartWords words
+    float2* part;          // [tokens][parts]: (max, sum exp(l - max)) over each run of kPartWords words
     float* part_t;         // the same sum at 1/temperature, or nullptr
     float inv_t;
     float* logits; // [tokens][ld], or nullptr
@@ -116,7 +116,6 @@ hipError_t launch_prepare(const LossRows* r, uint32_t row0, uint32_t rows, const
 // also copies those rows, zeros for the ones that do not count.
 struct LossPiece {
     uint32_t row0, rows, parts;
-    uint32_t part_ld; // rows between two parts
     const float2* part;
     const float* part_t;
     const float* logits;
