@@ -17,6 +17,8 @@ constexpr uint64_t kDefaultPiece = 2ull << 30;
 // For so few tokens d_logits has a second bf16 plane: the products are bound by the weight's bytes, and the gradients
 // of few terms have no others to average their rounding with.
 constexpr uint64_t kFewTokens = 256;
+// So few tokens' weights are summed again by each workgroup that needs the sum.
+constexpr uint64_t kFewSums = 1024;
 constexpr uint64_t kSliceBytes = 256ull << 20; // of the partial sums of a product cut along k
 
 uint64_t up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
@@ -312,36 +314,23 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
         }
         r.target_logit = lo.target_logit - row0;
         CKPT_STEP(launch_rows(r, p, c, s), "loss rows");
-        if (piece + 1 == l.pieces) CKPT_STEP(launch_finish(r, true, s), "loss");
+        // Few tokens: one alone was summed with its row, some are summed by what uses their sums.
+        const bool few = l.grad && n <= kFewSums && l.pieces == 1;
+        if (piece + 1 == l.pieces && n > 1 && !few) CKPT_STEP(launch_finish(r, true, s), "loss");
         if (!l.grad) continue;
         if (l.masked_hidden) H = copied;
 
         const Operand dl_rows = {p.d_logits, p.dl_plane, l.vocab_pad, (uint32_t)rows_pad, (uint32_t)l.vocab_pad};
         GradOut g = {};
         g.scale = r.scale;
+        if (few && n > 1) g.sums = {(uint32_t)n, r.row_weight, r.token_loss, r.grad_scale, r.loss, r.mean};
         g.f32 = f32;
         g.out = (uint8_t*)a->d_hidden + row0 * a->d_hidden_stride * e;
         g.ld = a->d_hidden_stride;
-        const ProductShape dh = {(uint32_t)d, (uint32_t)rows, (uint32_t)l.vocab_pad, l.slices};
-        if (l.slices > 1) {
-            GradOut part = {};
-            part.out = w + l.join;
-            part.f32 = true;
-            part.ld = l.dim_pad;
-            part.slice = rows * l.dim_pad;
-            CKPT_STEP(launch_d_hidden(W, l.planes, dl_rows, l.dl_planes, dh, part, s), "d_hidden");
-            CKPT_STEP(launch_join((const float*)part.out, part.slice, (uint32_t)l.dim_pad, l.slices, (uint32_t)d,
-                                  (uint32_t)rows, g, s),
-                      "d_hidden");
-        } else {
-            CKPT_STEP(launch_d_hidden(W, l.planes, dl_rows, l.dl_planes, dh, g, s), "d_hidden");
-        }
-
-        GradOut gw = {};
-        gw.f32 = f32;
+        GradOut gw = g;
+        gw.total = few && n > 1;
         gw.out = a->d_weight;
         gw.ld = a->d_weight_stride;
-        gw.scale = r.scale;
         if (piece > 0) gw.add = (const float*)(w + l.sum), gw.add_ld = d;
         if (piece + 1 < l.pieces) {
             gw.out = w + l.sum;
@@ -349,8 +338,22 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
             gw.f32 = true;
             gw.scale = nullptr;
         }
-        CKPT_STEP(launch_d_weight(H, l.planes, dl_rows, l.dl_planes, {(uint32_t)d, (uint32_t)v, (uint32_t)rows_pad, 1}, gw, s),
-                  "d_weight");
+        GradOut gh = g;
+        if (l.slices > 1) {
+            gh = {};
+            gh.out = w + l.join;
+            gh.f32 = true;
+            gh.ld = l.dim_pad;
+            gh.slice = rows * l.dim_pad;
+        }
+        CKPT_STEP(launch_gradients(W, H, l.planes, dl_rows, l.dl_planes,
+                                   {(uint32_t)d, (uint32_t)rows, (uint32_t)l.vocab_pad, l.slices}, gh,
+                                   {(uint32_t)d, (uint32_t)v, (uint32_t)rows_pad, 1}, gw, s),
+                  "gradients");
+        if (l.slices > 1)
+            CKPT_STEP(launch_join((const float*)gh.out, gh.slice, (uint32_t)l.dim_pad, l.slices, (uint32_t)d,
+                                  (uint32_t)rows, g, s),
+                      "d_hidden");
     }
     if (l.pieces == 0) { // no token: a loss of 0, and its gradient
         CKPT_STEP(launch_finish(r, true, s), "loss");

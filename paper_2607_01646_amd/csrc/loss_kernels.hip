@@ -261,10 +261,33 @@ struct GradEnd {
     uint32_t p, q;
 };
 
+// The factor that all rows share, and the loss: one wave's sums, in an order of their own (of few tokens, where a
+// launch for them alone takes longer).
+__device__ inline float few_sums(const LossSums& s, bool total)
+{
+    double weight = 0, loss = 0;
+    for (uint32_t n = threadIdx.x & 63; n < s.tokens; n += 64) {
+        const float w = s.row_weight[n];
+        weight += w;
+        if (total && w != 0) loss += (double)w * s.token_loss[n];
+    }
+    for (int o = 32; o; o >>= 1) {
+        weight += __shfl_xor(weight, o);
+        loss += __shfl_xor(loss, o);
+    }
+    const double over = s.mean ? (weight != 0 ? 1 / weight : 0.0) : 1.0;
+    if (total && threadIdx.x == 0) *s.loss = (float)(loss * over);
+    return (float)(over * (s.grad_scale ? *s.grad_scale : 1.0f));
+}
+
 template <int TQ>
 struct Early<GradEnd, TQ> {
     float scale;
-    __device__ inline Early(const GradEnd& e, uint32_t) : scale(e.o.scale ? *e.o.scale : 1.0f) {}
+    __device__ inline Early(const GradEnd& e, uint32_t)
+    {
+        scale = e.o.sums.tokens ? few_sums(e.o.sums, e.o.total && blockIdx.x + 1 == gridDim.x)
+                                : (e.o.scale ? *e.o.scale : 1.0f);
+    }
 };
 
 template <int TP, int TQ>
@@ -337,30 +360,43 @@ __device__ inline uint2 tile_of(uint32_t block, uint32_t np, uint32_t nq)
 // registers.  Two buffers in LDS: while one is multiplied the loads of the next BK values of k write the other one.
 // ZP and ZQ planes an operand.  3 and 3: fp32 operands as 3 bf16 planes; of the 9 products of planes the 6 whose sum of
 // indexes is at most 2 are made (the others are below 2^-24 of the value), smallest first.
-template <int ZP, int ZQ, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, int BUFS, class End>
-__global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_kernel(const Operand P, const Operand Q,
-                                                                const ProductShape shape, const End end)
-{
-    constexpr int kThreads = NWP * NWQ * 64;
-    constexpr int TP = BP / NWP / 32, TQ = BQ / NWQ / 32;
-    using TileP = Tile<BP, BK, PA>;
-    using TileQ = Tile<BQ, BK, QA>;
-    constexpr int kAtQ = ZP * TileP::kElems, kBuffer = kAtQ + ZQ * TileQ::kElems;
+template <int ZP_, int ZQ_, bool PA_, bool QA_, int BP_, int BQ_, int NWP_, int NWQ_, int BK_, int BUFS_>
+struct Shape {
+    static constexpr int ZP = ZP_, ZQ = ZQ_, BP = BP_, BQ = BQ_, NWP = NWP_, NWQ = NWQ_, BK = BK_, BUFS = BUFS_;
+    static constexpr bool PA = PA_, QA = QA_;
+    static constexpr int kThreads = NWP * NWQ * 64;
+    static constexpr int kBuffer = (ZP * BP + ZQ * BQ) * BK; // elements
     static_assert(BUFS >= 2 && BUFS <= 4, "");
-    // Arrays of their own, so that the compiler sees that a read of one waits for no load into another.
-    __shared__ __attribute__((aligned(16))) uint16_t s0[kBuffer], s1[kBuffer], s2[BUFS > 2 ? kBuffer : 1],
-        s3[BUFS > 3 ? kBuffer : 1];
+};
 
-    const uint32_t np = (shape.p + BP - 1) / BP, nq = (shape.q + BQ - 1) / BQ;
-    const uint2 tile = tile_of(blockIdx.x, np, nq);
-    const uint32_t p0 = __builtin_amdgcn_readfirstlane(tile.x * BP), q0 = __builtin_amdgcn_readfirstlane(tile.y * BQ);
+// LDS of a kernel that makes products of shapes A and B.  Arrays of their own, so that the compiler sees that a read of
+// one waits for no load into another.
+#define CKPT_BUFFERS(A, B)                                                                                          \
+    constexpr int kBuf01 = std::max(A::kBuffer, B::kBuffer);                                                        \
+    constexpr int kBuf2 = std::max(A::BUFS > 2 ? A::kBuffer : 1, B::BUFS > 2 ? B::kBuffer : 1);                     \
+    constexpr int kBuf3 = std::max(A::BUFS > 3 ? A::kBuffer : 1, B::BUFS > 3 ? B::kBuffer : 1);                     \
+    __shared__ __attribute__((aligned(16))) uint16_t s0[kBuf01], s1[kBuf01], s2[kBuf2], s3[kBuf3]
+
+// `block` of the tiles' workgroups, for run `slice` of k.
+template <class S, class End>
+__device__ inline void product(const Operand& P, const Operand& Q, const ProductShape& shape, const End& end,
+                               uint32_t block, uint32_t slice, uint16_t* s0, uint16_t* s1, uint16_t* s2, uint16_t* s3)
+{
+    constexpr int ZP = S::ZP, ZQ = S::ZQ, BK = S::BK, BUFS = S::BUFS, kThreads = S::kThreads;
+    constexpr int TP = S::BP / S::NWP / 32, TQ = S::BQ / S::NWQ / 32;
+    using TileP = Tile<S::BP, BK, S::PA>;
+    using TileQ = Tile<S::BQ, BK, S::QA>;
+    constexpr int kAtQ = ZP * TileP::kElems;
+
+    const uint32_t np = (shape.p + S::BP - 1) / S::BP, nq = (shape.q + S::BQ - 1) / S::BQ;
+    const uint2 tile = tile_of(block, np, nq);
+    const uint32_t p0 = __builtin_amdgcn_readfirstlane(tile.x * S::BP), q0 = __builtin_amdgcn_readfirstlane(tile.y * S::BQ);
     const uint32_t steps = shape.k / BK;
-    const uint32_t first = __builtin_amdgcn_readfirstlane((uint64_t)steps * blockIdx.y / shape.slices);
-    const uint32_t last = __builtin_amdgcn_readfirstlane((uint64_t)steps * (blockIdx.y + 1) / shape.slices);
+    const uint32_t first = __builtin_amdgcn_readfirstlane((uint64_t)steps * slice / shape.slices);
+    const uint32_t last = __builtin_amdgcn_readfirstlane((uint64_t)steps * (slice + 1) / shape.slices);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t wp = (wave % NWP) * (BP / NWP), wq = (wave / NWP) * (BQ / NWQ);
+    const uint32_t wp = (wave % S::NWP) * 32 * TP, wq = (wave / S::NWP) * 32 * TQ;
 
-    const Early<End, TQ> early(end, q0 + wq);
     f32x16 acc[TP][TQ];
 #pragma unroll
     for (int a = 0; a < TP; ++a)
@@ -456,6 +492,7 @@ __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_
 #pragma unroll
     for (int i = 0; i < BUFS * kLoads; ++i)
         load(i / kLoads == 0 ? s0 : i / kLoads == 1 ? s1 : i / kLoads == 2 ? s2 : s3, first + i / kLoads, i % kLoads);
+    const Early<End, TQ> early(end, q0 + wq); // waits for all that was loaded before it
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((BUFS - 1) * kLoads) : "memory");
     read(even, s0, 0);
     uint32_t step = first;
@@ -469,16 +506,59 @@ __global__ __launch_bounds__(NWP* NWQ * 64, NWP* NWQ >= 8 ? 2 : 1) void product_
     if (BUFS > 2 && step + 1 < last) one_step(s1, s2, step + 1);
     if (BUFS > 3 && step + 2 < last) one_step(s2, s3, step + 2);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // no load is left that would write the LDS of another workgroup
-    finish<TP, TQ>(end, early, acc, p0 + wp, q0 + wq, blockIdx.y);
+    finish<TP, TQ>(end, early, acc, p0 + wp, q0 + wq, slice);
 }
 
-template <int ZP, int ZQ, bool PA, bool QA, int BP, int BQ, int NWP, int NWQ, int BK, int BUFS, class End>
+template <class S, class End>
+__global__ __launch_bounds__(S::kThreads, S::kThreads >= 512 ? 2 : 1) void product_kernel(
+    const Operand P, const Operand Q, const ProductShape shape, const End end)
+{
+    CKPT_BUFFERS(S, S);
+    product<S>(P, Q, shape, end, blockIdx.x, blockIdx.y, s0, s1, s2, s3);
+}
+
+// Two products that do not wait for each other in one launch: d_hidden's workgroups, then d_weight's.
+struct Both {
+    Operand hp, hq, wp, wq;
+    ProductShape hs, ws;
+    uint32_t h_tiles; // workgroups of one run of k
+    uint32_t h_all;
+};
+template <class H, class W>
+__global__ __launch_bounds__(H::kThreads, 1) void both_kernel(const Both b, const GradEnd h_end, const GradEnd w_end)
+{
+    static_assert(H::kThreads == W::kThreads, "");
+    CKPT_BUFFERS(H, W);
+    if (blockIdx.x < b.h_all)
+        product<H>(b.hp, b.hq, b.hs, h_end, blockIdx.x % b.h_tiles, blockIdx.x / b.h_tiles, s0, s1, s2, s3);
+    else
+        product<W>(b.wp, b.wq, b.ws, w_end, blockIdx.x - b.h_all, 0, s0, s1, s2, s3);
+}
+
+template <class S>
+uint64_t tiles_of(const ProductShape& s)
+{
+    return (uint64_t)((s.p + S::BP - 1) / S::BP) * ((s.q + S::BQ - 1) / S::BQ);
+}
+
+template <class S, class End>
 hipError_t launch_product(const Operand& P, const Operand& Q, const ProductShape& s, const End& end, hipStream_t stream)
 {
-    const uint64_t tiles = (uint64_t)((s.p + BP - 1) / BP) * ((s.q + BQ - 1) / BQ);
-    if (tiles == 0 || tiles > 0x7fffffff || s.slices == 0 || s.slices > 65535 || s.k % BK) return hipErrorInvalidValue;
-    product_kernel<ZP, ZQ, PA, QA, BP, BQ, NWP, NWQ, BK, BUFS, End>
-        <<<dim3((uint32_t)tiles, s.slices), NWP * NWQ * 64, 0, stream>>>(P, Q, s, end);
+    const uint64_t tiles = tiles_of<S>(s);
+    if (tiles == 0 || tiles * S::kThreads > 0xffffffffu || s.slices == 0 || s.slices > 65535 || s.k % S::BK)
+        return hipErrorInvalidValue;
+    product_kernel<S, End><<<dim3((uint32_t)tiles, s.slices), S::kThreads, 0, stream>>>(P, Q, s, end);
+    return hipGetLastError();
+}
+
+template <class H, class W>
+hipError_t launch_both(Both b, const GradEnd& h_end, const GradEnd& w_end, hipStream_t stream)
+{
+    const uint64_t h_tiles = tiles_of<H>(b.hs), all = h_tiles * b.hs.slices + tiles_of<W>(b.ws);
+    if (h_tiles == 0 || all * H::kThreads > 0xffffffffu || b.hs.k % H::BK || b.ws.k % W::BK) return hipErrorInvalidValue;
+    b.h_tiles = (uint32_t)h_tiles;
+    b.h_all = (uint32_t)(h_tiles * b.hs.slices);
+    both_kernel<H, W><<<(uint32_t)all, H::kThreads, 0, stream>>>(b, h_end, w_end);
     return hipGetLastError();
 }
 
@@ -501,28 +581,22 @@ __device__ inline float wave_sum(float x)
     for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
     return x;
 }
-template <int WAVES>
-__device__ inline float block_max(float x, float* s)
+// Over the workgroup: the maxima of the first MAX values and the sums of the others, the waves' in their order.  s holds
+// a value of each for every wave and is used once (one barrier).
+template <int WAVES, int MAX, int N>
+__device__ inline void block_reduce(float (&x)[N], float* s)
 {
-    x = wave_max(x);
-    if (WAVES == 1) return x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = i < MAX ? wave_max(x[i]) : wave_sum(x[i]);
+        if ((threadIdx.x & 63) == 0) s[i * WAVES + (threadIdx.x >> 6)] = x[i];
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
-    __syncthreads();
-    for (int w = 0; w < WAVES; ++w) x = fmaxf(x, s[w]);
-    return x;
-}
-template <int WAVES>
-__device__ inline float block_sum(float x, float* s)
-{
-    x = wave_sum(x);
-    if (WAVES == 1) return x;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = 0;
-    for (int w = 0; w < WAVES; ++w) x += s[w];
-    return x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = s[i * WAVES];
+        for (int w = 1; w < WAVES; ++w) x[i] = i < MAX ? fmaxf(x[i], s[i * WAVES + w]) : x[i] + s[i * WAVES + w];
+    }
 }
 
 // A teacher entry that is there: a word, and any logit but -inf.
@@ -641,6 +715,15 @@ __device__ inline bool labelled(const LossRows& r, uint64_t n, int64_t* label, b
     return true;
 }
 
+// The loss of one token alone.
+__device__ inline void only_row(const LossRows& r, float weight, float loss)
+{
+    if (r.tokens != 1) return;
+    const double over = r.mean ? (weight != 0 ? 1.0 / weight : 0.0) : 1.0;
+    *r.loss = weight != 0 ? (float)((double)weight * loss * over) : 0.0f;
+    *r.scale = (float)(over * (r.grad_scale ? *r.grad_scale : 1.0f));
+}
+
 // One workgroup a row: its log-sum-exp and loss and, with d_logits, its row of
 //   w (alpha T (p^T - q) + (1 - alpha) (p - 1_y)).
 // The factor that all rows share (grad_scale and the mean's) is left to the products' fp32 sums: here the label's term
@@ -654,7 +737,7 @@ template <int WAVES, bool E16>
 __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, const LossPiece p, const RowCopy copy)
 {
     extern __shared__ float s_more[]; // E16: a factor for each part; else the teacher's entries
-    __shared__ float s_wave[WAVES];
+    __shared__ float s_first[3 * WAVES], s_second[3 * WAVES], s_third[WAVES];
     constexpr uint32_t kThreads = WAVES * 64;
     const uint32_t row = blockIdx.x, tid = threadIdx.x;
     const uint64_t n = p.row0 + (uint64_t)row;
@@ -676,7 +759,10 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
     float* s_own = s_more + r.topk;
     int* s_word = (int*)(s_more + 2 * r.topk);
     const float* logits = E16 ? nullptr : p.logits + (uint64_t)row * p.ld;
-    float t_top = -kInf, t_count = 0;
+    const float2* part = p.part + (uint64_t)row * p.parts;
+    const float* part_t = p.part_t ? p.part_t + (uint64_t)row * p.parts : nullptr;
+    float first[3] = {-kInf, -kInf, 0}; // the largest logit, the teacher's largest, the count of entries
+    for (uint32_t k = tid; k < p.parts; k += kThreads) first[0] = fmaxf(first[0], part[k].x);
     if (teach) {
         for (uint32_t k = tid; k < r.topk; k += kThreads) {
             int64_t at;
@@ -686,44 +772,39 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
             s_word[k] = known ? (int)at : -1;
             s_own[k] = known ? logits[at] : 0.0f;
             if (there) {
-                t_top = fmaxf(t_top, t);
-                t_count += known ? 1 : kBad;
+                first[1] = fmaxf(first[1], t);
+                first[2] += known ? 1 : kBad;
             }
         }
-        t_top = block_max<WAVES>(t_top, s_wave);
-        t_count = block_sum<WAVES>(t_count, s_wave);
     }
+    block_reduce<WAVES, 2>(first, s_first);
+    const float low = first[0] == -kInf ? 0.0f : first[0], t_top = first[1], t_count = first[2];
     const bool counts = (has_label || t_count > 0) && given != 0;
     const float weight = counts ? given : 0.0f;
     if (tid == 0) r.row_weight[n] = weight;
     copy_row<kThreads>(copy, row, n, counts);
     if (!counts) {
-        if (tid == 0) r.token_loss[n] = r.lse[n] = 0;
+        if (tid == 0) {
+            r.token_loss[n] = r.lse[n] = 0;
+            only_row(r, 0, 0);
+        }
         zero_row<kThreads>(p, dl);
         return;
     }
 
-    float top = -kInf;
-    const float2* part = p.part + (uint64_t)row * p.parts;
-    const float* part_t = p.part_t ? p.part_t + (uint64_t)row * p.parts : nullptr;
-    for (uint32_t k = tid; k < p.parts; k += kThreads) top = fmaxf(top, part[k].x);
-    top = block_max<WAVES>(top, s_wave);
-    const float low = top == -kInf ? 0.0f : top;
-    float sum = 0, sum_t = 0;
+    float second[3] = {0, 0, 0}; // the sums of exponentials: the words', at the temperature, the teacher's
     for (uint32_t k = tid; k < p.parts; k += kThreads) {
         const float2 x = part[k];
         const float f = x.x == -kInf ? (x.y == 0 ? 0.0f : x.y) : exp_of(x.x - low); // all words at -inf, or NaN
-        sum += x.y * f;
+        second[0] += x.y * f;
         if (E16) s_more[k] = f;
-        if (part_t && x.x != -kInf) sum_t += part_t[k] * exp_of((x.x - low) * inv_t);
+        if (part_t && x.x != -kInf) second[1] += part_t[k] * exp_of((x.x - low) * inv_t);
     }
-    sum = block_sum<WAVES>(sum, s_wave);
-    const float lse = low + __builtin_amdgcn_logf(sum) * kLn2;
-    float lse_t = lse;
-    if (part_t) {
-        sum_t = block_sum<WAVES>(sum_t, s_wave);
-        lse_t = low * inv_t + __builtin_amdgcn_logf(sum_t) * kLn2;
-    }
+    if (teach)
+        for (uint32_t k = tid; k < r.topk; k += kThreads) second[2] += exp_of((s_q[k] - t_top) * inv_t);
+    block_reduce<WAVES, 0>(second, s_second);
+    const float sum = second[0], lse = low + __builtin_amdgcn_logf(sum) * kLn2;
+    const float lse_t = part_t ? low * inv_t + __builtin_amdgcn_logf(second[1]) * kLn2 : lse;
 
     const uint32_t target = word ? (uint32_t)label : ~0u; // no word is as large
     float loss = 0, hard = 0;
@@ -735,8 +816,8 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
         if (tid == 0) {
             r.token_loss[n] = loss;
             r.lse[n] = lse;
+            only_row(r, weight, loss);
         }
-        __syncthreads(); // the parts' factors
         const float scale = weight * hard / (kE16 * sum);
         for (uint32_t v = 8 * tid; v < p.dl_ld; v += 8 * kThreads) {
             const f16x8 e = *(const f16x8*)(dl + v);
@@ -761,25 +842,23 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
 
     float soft = 0;
     if (teach) {
-        float t_sum = 0;
-        for (uint32_t k = tid; k < r.topk; k += kThreads) t_sum += exp_of((s_q[k] - t_top) * inv_t);
-        t_sum = block_sum<WAVES>(t_sum, s_wave);
-        const float log_sum = __builtin_amdgcn_logf(t_sum) * kLn2;
-        float kd = 0;
+        const float log_sum = __builtin_amdgcn_logf(second[2]) * kLn2;
+        float kd[1] = {0};
         for (uint32_t k = tid; k < r.topk; k += kThreads) {
             const float log_q = (s_q[k] - t_top) * inv_t - log_sum, q = t_count > 0 ? exp_of(log_q) : 0.0f;
             s_q[k] = q;
-            if (s_word[k] >= 0 && q != 0) kd += q * (log_q - (s_own[k] * inv_t - lse_t));
+            if (s_word[k] >= 0 && q != 0) kd[0] += q * (log_q - (s_own[k] * inv_t - lse_t));
         }
-        kd = block_sum<WAVES>(kd, s_wave);
+        block_reduce<WAVES, 0>(kd, s_third);
         if (t_count > 0) {
             soft = t_count >= kBad ? __builtin_nanf("") : r.alpha * r.temperature;
-            loss += soft * r.temperature * kd;
+            loss += soft * r.temperature * kd[0];
         }
     }
     if (tid == 0) {
         r.token_loss[n] = loss;
         r.lse[n] = teach ? lse_t : lse;
+        only_row(r, weight, loss);
     }
     if (!dl) return;
 
@@ -890,11 +969,12 @@ __global__ __launch_bounds__(256) void join_kernel(const float* slices, uint64_t
                                                    const GradOut o)
 {
     const uint32_t at = 4 * (blockIdx.x * 256 + threadIdx.x), q = blockIdx.y;
+    const float scale = o.sums.tokens ? few_sums(o.sums, false) : (o.scale ? *o.scale : 1.0f);
     if (at >= p) return;
     const float* from = slices + (uint64_t)q * ld_s + at;
     f32x4 x = {0, 0, 0, 0};
     for (uint32_t k = 0; k < n; ++k) x += *(const f32x4*)(from + k * slice);
-    x *= o.scale ? *o.scale : 1.0f;
+    x *= scale;
     const uint64_t to = (uint64_t)q * o.ld + at;
     for (int j = 0; j < 4; ++j) {
         if (at + j >= p) break;
@@ -948,22 +1028,48 @@ Tiling tiling(const ProductShape& s, uint32_t zp, uint32_t zq, uint32_t most)
     return best;
 }
 
-template <bool PA, bool QA, class End>
-hipError_t dispatch(const Operand& P, const Operand& Q, const ProductShape& s, uint32_t zp, uint32_t zq, Size size,
-                    const End& end, hipStream_t stream)
+// The shapes.  The smaller two of gradients have 4 waves each, for one launch of both, and together no more LDS than
+// lets two workgroups share a unit (fp32: no such shapes).
+template <int ZP, int ZQ, bool PA, bool QA>
+using Large = std::conditional_t<ZP == 3, Shape<ZP, ZQ, PA, QA, 256, 128, 4, 2, 32, 2>,
+                                 Shape<ZP, ZQ, PA, QA, 256, 256, 4, 2, 64, 2>>;
+template <int ZP, int ZQ, bool PA, bool QA>
+using Middle = Shape<ZP, ZQ, PA, QA, 128, 128, 2, 2, ZP == 3 || ZQ == 2 ? 32 : 64, 2>;
+template <int ZP, int ZQ, bool PA, bool QA>
+using Small = Shape<ZP, ZQ, PA, QA, 64, 64, PA ? 2 : 1, 2, ZP == 3 ? 32 : 64, PA || ZP == 3 ? 3 : 4>;
+
+template <int Z>
+hipError_t logits_of(const Operand& w, const Operand& h, const ProductShape& s, const LogitsOut& o, hipStream_t stream)
 {
-    if (zp == 3 && zq == 3)
-        return size == kLarge    ? launch_product<3, 3, PA, QA, 256, 128, 4, 2, 32, 2>(P, Q, s, end, stream)
-               : size == kMiddle ? launch_product<3, 3, PA, QA, 128, 128, 2, 2, 32, 2>(P, Q, s, end, stream)
-                                 : launch_product<3, 3, PA, QA, 64, 64, 1, 2, 32, 3>(P, Q, s, end, stream);
-    if constexpr (PA) // a gradient
-        if (zp == 1 && zq == 2)
-            return size == kMiddle ? launch_product<1, 2, PA, QA, 128, 128, 2, 2, 64, 2>(P, Q, s, end, stream)
-                                   : launch_product<1, 2, PA, QA, 64, 64, 1, 2, 64, 3>(P, Q, s, end, stream);
-    if (zp != 1 || zq != 1) return hipErrorInvalidValue;
-    return size == kLarge    ? launch_product<1, 1, PA, QA, 256, 256, 4, 2, 64, 2>(P, Q, s, end, stream)
-           : size == kMiddle ? launch_product<1, 1, PA, QA, 128, 128, 2, 2, 64, 2>(P, Q, s, end, stream)
-                             : launch_product<1, 1, PA, QA, 64, 64, 1, 2, 64, 4>(P, Q, s, end, stream);
+    const Size size = tiling(s, Z, Z, 1).size;
+    return size == kLarge    ? launch_product<Large<Z, Z, false, false>>(w, h, s, o, stream)
+           : size == kMiddle ? launch_product<Middle<Z, Z, false, false>>(w, h, s, o, stream)
+                             : launch_product<Small<Z, Z, false, false>>(w, h, s, o, stream);
+}
+
+template <int ZP, int ZQ>
+hipError_t gradients_of(const Both& b, const GradEnd& he, const GradEnd& we, hipStream_t stream)
+{
+    const Size h = tiling(b.hs, ZP, ZQ, b.hs.slices).size, w = tiling(b.ws, ZP, ZQ, 1).size;
+    using HM = Middle<ZP, ZQ, true, false>;
+    using HS = Small<ZP, ZQ, true, false>;
+    using WM = Middle<ZP, ZQ, true, true>;
+    using WS = Small<ZP, ZQ, true, true>;
+    if (h != kLarge && w != kLarge)
+        return h == kMiddle ? (w == kMiddle ? launch_both<HM, WM>(b, he, we, stream) : launch_both<HM, WS>(b, he, we, stream))
+                            : (w == kMiddle ? launch_both<HS, WM>(b, he, we, stream) : launch_both<HS, WS>(b, he, we, stream));
+    if constexpr (ZP == ZQ) { // (1, 2) has no large shape
+        using HL = Large<ZP, ZQ, true, false>;
+        using WL = Large<ZP, ZQ, true, true>;
+        const hipError_t e = h == kLarge    ? launch_product<HL>(b.hp, b.hq, b.hs, he, stream)
+                             : h == kMiddle ? launch_product<HM>(b.hp, b.hq, b.hs, he, stream)
+                                            : launch_product<HS>(b.hp, b.hq, b.hs, he, stream);
+        if (e != hipSuccess) return e;
+        return w == kLarge    ? launch_product<WL>(b.wp, b.wq, b.ws, we, stream)
+               : w == kMiddle ? launch_product<WM>(b.wp, b.wq, b.ws, we, stream)
+                              : launch_product<WS>(b.wp, b.wq, b.ws, we, stream);
+    }
+    return hipErrorInvalidValue;
 }
 
 } // namespace
@@ -971,20 +1077,18 @@ hipError_t dispatch(const Operand& P, const Operand& Q, const ProductShape& s, u
 hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape& s, uint32_t planes,
                          const LogitsOut& o, hipStream_t stream)
 {
-    return dispatch<false, false>(w, h, s, planes, planes, tiling(s, planes, planes, 1).size, o, stream);
+    return planes == 3 ? logits_of<3>(w, h, s, o, stream) : logits_of<1>(w, h, s, o, stream);
 }
 
-hipError_t launch_d_hidden(const Operand& w, uint32_t zp, const Operand& dl, uint32_t zq, const ProductShape& s,
-                           const GradOut& o, hipStream_t stream)
+hipError_t launch_gradients(const Operand& w, const Operand& h, uint32_t zp, const Operand& dl, uint32_t zq,
+                            const ProductShape& dh, const GradOut& dho, const ProductShape& dw, const GradOut& dwo,
+                            hipStream_t stream)
 {
-    const Size size = tiling(s, zp, zq, s.slices).size;
-    return dispatch<true, false>(w, dl, s, zp, zq, size, GradEnd{o, s.p, s.q}, stream);
-}
-
-hipError_t launch_d_weight(const Operand& h, uint32_t zp, const Operand& dl, uint32_t zq, const ProductShape& s,
-                           const GradOut& o, hipStream_t stream)
-{
-    return dispatch<true, true>(h, dl, s, zp, zq, tiling(s, zp, zq, 1).size, GradEnd{o, s.p, s.q}, stream);
+    const Both b = {w, dl, h, dl, dh, dw, 0, 0};
+    const GradEnd he = {dho, dh.p, dh.q}, we = {dwo, dw.p, dw.q};
+    return zp == 3   ? gradients_of<3, 3>(b, he, we, stream)
+           : zq == 2 ? gradients_of<1, 2>(b, he, we, stream)
+                     : gradients_of<1, 1>(b, he, we, stream);
 }
 
 uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t zp, uint32_t zq, uint32_t most)

@@ -45,8 +45,19 @@ struct LogitsOut {
 constexpr uint32_t kPartWords = 64;
 constexpr uint32_t kE16Parts = 8192; // of a row held in fp16: their factors fit in LDS
 
+// Where the factor that all rows share and the loss come from when no launch
+// has made them (tokens == 0: one has).
+struct LossSums {
+    uint32_t tokens;
+    const float *row_weight, *token_loss, *grad_scale; // grad_scale or nullptr
+    float* loss;
+    bool mean;
+};
+
 // What becomes of a product that is a gradient (or a slice of one).
 struct GradOut {
+    LossSums sums;      // with tokens: the factor is made of these, not *scale
+    bool total;         // ... and the loss written
     const float* scale; // multiplies the sum; nullptr = 1
     const float* add;   // [q][add_ld] added to the product before the scale, or nullptr
     uint64_t add_ld;
@@ -57,13 +68,13 @@ struct GradOut {
 
 hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape& s, uint32_t planes,
                          const LogitsOut& o, hipStream_t stream);
+// Both gradients, in one launch where they are small:
+//   d_hidden: P = weight (k = words across rows), Q = d_logits (k contiguous)
+//   d_weight: P = hidden, Q = d_logits (both with k = tokens across rows)
 // zp, zq: planes of P and Q; (1, 1), (1, 2) or (3, 3).
-// d_hidden: P = weight (k = words across rows), Q = d_logits (k contiguous)
-hipError_t launch_d_hidden(const Operand& w, uint32_t zp, const Operand& dl, uint32_t zq, const ProductShape& s,
-                           const GradOut& o, hipStream_t stream);
-// d_weight: P = hidden, Q = d_logits (both with k = tokens across rows)
-hipError_t launch_d_weight(const Operand& h, uint32_t zp, const Operand& dl, uint32_t zq, const ProductShape& s,
-                           const GradOut& o, hipStream_t stream);
+hipError_t launch_gradients(const Operand& w, const Operand& h, uint32_t zp, const Operand& dl, uint32_t zq,
+                            const ProductShape& dh, const GradOut& dho, const ProductShape& dw, const GradOut& dwo,
+                            hipStream_t stream);
 // out = scale * sum of the n slices (fp32 [n][q][ld_s], `slice` apart; ld_s a multiple of 4)
 hipError_t launch_join(const float* slices, uint64_t slice, uint32_t ld_s, uint32_t n, uint32_t p, uint32_t q,
                        const GradOut& o, hipStream_t stream);
@@ -126,7 +137,8 @@ struct LossPiece {
     bool e16;
 };
 hipError_t launch_rows(const LossRows& r, const LossPiece& p, const RowCopy& copy, hipStream_t stream);
-// scale (from row_weight) and, if `total`, the loss.
+// scale (from row_weight) and, if `total`, the loss.  (launch_rows makes both of
+// one token.)
 hipError_t launch_finish(const LossRows& r, bool total, hipStream_t stream);
 
 // ---- optimizer (optim_kernels.hip) ----
