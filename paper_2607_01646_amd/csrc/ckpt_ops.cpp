@@ -399,6 +399,10 @@ extern "C" ckpt_status ckpt_grad_norm(const ckpt_tensor* grads, uint32_t n, uint
     static_assert(CKPT_GRAD_NORM_SCRATCH == kNormBlocks * 8, "one sum for each workgroup");
     NormArgs a;
     a.count = a.tiles = 0;
+    uint64_t total = 0;
+    for (uint32_t i = 0; i < n; ++i) total += grads[i].nbytes / e;
+    const bool few = n <= kNormFrags && total <= kNormFew;
+    const uint64_t tile = few ? kNormFewTile : kNormTile;
     bool fresh = true;
     const auto flush = [&] {
         const hipError_t err = launch_norm(a, e == 4, fresh, (double*)scratch, (hipStream_t)stream);
@@ -411,7 +415,7 @@ extern "C" ckpt_status ckpt_grad_norm(const ckpt_tensor* grads, uint32_t n, uint
         // A fragment of more tiles than a launch counts goes in runs.
         constexpr uint64_t kRun = (uint64_t)kNormTile << 30;
         for (uint64_t at = 0, all = grads[i].nbytes / e; at < all && err == hipSuccess; at += kRun) {
-            const uint64_t run = std::min(kRun, all - at), tiles = (run + kNormTile - 1) / kNormTile;
+            const uint64_t run = std::min(kRun, all - at), tiles = (run + tile - 1) / tile;
             if (a.count == kNormFrags || a.tiles + tiles > kMost) err = flush();
             a.f[a.count].ptr = (uint64_t)(uintptr_t)grads[i].dev_ptr + at * e;
             a.f[a.count].numel = run;
@@ -419,8 +423,9 @@ extern "C" ckpt_status ckpt_grad_norm(const ckpt_tensor* grads, uint32_t n, uint
             a.tiles += (uint32_t)tiles;
         }
     }
-    if (err == hipSuccess && (a.count || fresh)) err = flush();
-    if (err == hipSuccess) err = launch_norm_finish((const double*)scratch, max_norm, out, (hipStream_t)stream);
+    if (few && err == hipSuccess) err = launch_norm_few(a, e == 4, max_norm, out, (hipStream_t)stream);
+    if (!few && err == hipSuccess && (a.count || fresh)) err = flush();
+    if (!few && err == hipSuccess) err = launch_norm_finish((const double*)scratch, max_norm, out, (hipStream_t)stream);
     if (err != hipSuccess) return fail_free(CKPT_EHIP, "gradient norm: %s", hipGetErrorString(err));
     return CKPT_OK;
 }

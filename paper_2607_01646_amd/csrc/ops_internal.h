@@ -153,7 +153,7 @@ struct AdamArgs {
     float beta1, one_beta1, beta2, one_beta2, keep, lr, inv_bc1, inv_bc2, eps;
     const float* scale;
 };
-constexpr uint32_t kAdamTile = 2048;
+constexpr uint32_t kAdamTile = 1024;
 hipError_t launch_adamw(const AdamArgs& a, bool param_f32, bool grad_f32, hipStream_t stream);
 
 constexpr uint32_t kNormFrags = 160;
@@ -167,6 +167,10 @@ struct NormArgs {
 constexpr uint32_t kNormTile = 8192, kNormBlocks = 2048;
 // Adds the fragments' squares to part (kNormBlocks sums; `fresh`: stores them).
 hipError_t launch_norm(const NormArgs& a, bool f32, bool fresh, double* part, hipStream_t stream);
+// All of it, by one workgroup whose 16 waves take a tile of kNormFewTile each at a time: for so few elements that a
+// second launch takes longer.
+constexpr uint32_t kNormFewTile = 2048, kNormFew = 64 * kNormFewTile;
+hipError_t launch_norm_few(const NormArgs& a, bool f32, double max_norm, float* out, hipStream_t stream);
 hipError_t launch_norm_finish(const double* part, double max_norm, float* out, hipStream_t stream);
 
 } // namespace ckpt

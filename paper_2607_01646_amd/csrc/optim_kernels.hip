@@ -130,15 +130,14 @@ __device__ inline double block_sum(double x, double* s_wave)
     return x;
 }
 
-// Squares and sums are in 64 bits: the sum is exact to its last places for
-// any number of elements, no square overflows, and the kernel is bound by its
-// loads all the same.
-template <class G>
-__global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a, double* part, bool fresh)
+// The squares of tiles first, first + stride, ...: `lane` is one of LANES that share a tile of TILE elements.  Squares and
+// sums are in 64 bits: the sum is exact to its last places for any number of elements, no square overflows, and the
+// kernel is bound by its loads all the same.
+template <class G, int LANES, uint32_t TILE>
+__device__ inline double tile_squares(const NormArgs& a, uint32_t lane, uint32_t first, uint32_t stride)
 {
-    __shared__ double s_wave[kThreads / 64];
     double sum = 0;
-    for (uint32_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
+    for (uint32_t t = first; t < a.tiles; t += stride) {
         uint32_t f = 0;
         for (uint32_t base = 0; base < a.count; base += 64) {
             const uint32_t k = base + (threadIdx.x & 63);
@@ -146,29 +145,61 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a, double
             if (before) f = base + 63 - __builtin_clzll(before);
         }
         f = __builtin_amdgcn_readfirstlane(f);
-        const uint64_t n = a.f[f].numel, begin = (uint64_t)(t - a.first[f]) * kNormTile;
+        const uint64_t n = a.f[f].numel, begin = (uint64_t)(t - a.first[f]) * TILE;
         const G* g = (const G*)a.f[f].ptr + begin;
         const uint64_t left = n - begin;
-        if (left >= kNormTile) {
-            constexpr int kVecs = kNormTile / (4 * kThreads);
+        if (left >= TILE) {
+            constexpr int kVecs = TILE / (4 * LANES);
             f32x4 x[kVecs];
 #pragma unroll
-            for (int u = 0; u < kVecs; ++u) x[u] = load4(g + 4 * (u * kThreads + threadIdx.x));
+            for (int u = 0; u < kVecs; ++u) x[u] = load4(g + 4 * (u * LANES + lane));
 #pragma unroll
             for (int u = 0; u < kVecs; ++u)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum += (double)x[u][j] * (double)x[u][j];
         } else {
-            for (uint32_t at = threadIdx.x; at < left; at += kThreads) {
-                const double x = load1(g + at);
-                sum += x * x;
+            for (uint32_t at = 4 * lane; at < left; at += 4 * LANES) {
+                if (at + 4 <= left) {
+                    const f32x4 x = load4(g + at);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum += (double)x[j] * (double)x[j];
+                } else {
+                    for (uint32_t j = at; j < left; ++j) {
+                        const double x = load1(g + j);
+                        sum += x * x;
+                    }
+                }
             }
         }
     }
-    sum = block_sum(sum, s_wave);
+    return sum;
+}
+
+__device__ inline void write_norm(double sum, double max_norm, float* out)
+{
+    const double norm = sqrt(sum);
+    const double c = max_norm / (norm + 1e-6);
+    out[0] = (float)norm;
+    out[1] = max_norm <= 0 || c >= 1 ? 1.0f : (float)c; // a NaN norm gives NaN
+}
+
+template <class G>
+__global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a, double* part, bool fresh)
+{
+    __shared__ double s_wave[kThreads / 64];
+    const double sum = block_sum(tile_squares<G, kThreads, kNormTile>(a, threadIdx.x, blockIdx.x, gridDim.x), s_wave);
     if (threadIdx.x == 0) part[blockIdx.x] = fresh ? sum : part[blockIdx.x] + sum;
     if (fresh && blockIdx.x == 0) // workgroups that this launch does without
         for (uint32_t k = gridDim.x + threadIdx.x; k < kNormBlocks; k += kThreads) part[k] = 0;
+}
+
+template <class G>
+__global__ __launch_bounds__(1024) void norm_few_kernel(const NormArgs a, double max_norm, float* out)
+{
+    __shared__ double s_wave[16];
+    const double sum = block_sum(
+        tile_squares<G, 64, kNormFewTile>(a, threadIdx.x & 63, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 16), s_wave);
+    if (threadIdx.x == 0) write_norm(sum, max_norm, out);
 }
 
 __global__ __launch_bounds__(kThreads) void norm_finish_kernel(const double* part, double max_norm, float* out)
@@ -177,12 +208,7 @@ __global__ __launch_bounds__(kThreads) void norm_finish_kernel(const double* par
     double sum = 0;
     for (uint32_t k = threadIdx.x; k < kNormBlocks; k += kThreads) sum += part[k];
     sum = block_sum(sum, s_wave);
-    if (threadIdx.x == 0) {
-        const double norm = sqrt(sum);
-        const double c = max_norm / (norm + 1e-6);
-        out[0] = (float)norm;
-        out[1] = max_norm <= 0 || c >= 1 ? 1.0f : (float)c; // a NaN norm gives NaN
-    }
+    if (threadIdx.x == 0) write_norm(sum, max_norm, out);
 }
 
 } // namespace
@@ -210,6 +236,16 @@ hipError_t launch_norm(const NormArgs& a, bool f32, bool fresh, double* part, hi
         norm_kernel<float><<<grid, kThreads, 0, s>>>(a, part, fresh);
     else
         norm_kernel<uint16_t><<<grid, kThreads, 0, s>>>(a, part, fresh);
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_few(const NormArgs& a, bool f32, double max_norm, float* out, hipStream_t s)
+{
+    if (a.count > kNormFrags) return hipErrorInvalidValue;
+    if (f32)
+        norm_few_kernel<float><<<1, 1024, 0, s>>>(a, max_norm, out);
+    else
+        norm_few_kernel<uint16_t><<<1, 1024, 0, s>>>(a, max_norm, out);
     return hipGetLastError();
 }
 

@@ -54,6 +54,7 @@ class LinearLoss(NamedTuple):
 
 _lib = None
 _native = None
+_HERE = contextlib.nullcontext()
 
 
 def _module():
@@ -128,8 +129,12 @@ def _rows(t, what):
 def _on(stream):
     """The context in which the outputs and the workspace of work on `stream` are allocated."""
     if stream is None:
-        return contextlib.nullcontext()
+        return _HERE
     return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+
+
+def _listed(x):
+    return x if type(x) is list or type(x) is tuple else list(x)
 
 
 def _plain(t, what, dtype, n):
@@ -143,7 +148,7 @@ def _plain(t, what, dtype, n):
 
 def _linear_loss(hidden, weight, target, teacher, temperature, alpha, token_weight, ignore_index, reduction, grad,
                  grad_scale, piece_bytes, stream):
-    native, at = _module()
+    native, at = _native or _module()
     if native is not None and isinstance(hidden, torch.Tensor) and hidden.is_cuda and reduction in _REDUCTIONS:
         with _on(stream):
             got = native.linear_loss(at["ckpt_linear_loss_workspace"], at["ckpt_linear_loss"], hidden, weight, target,
@@ -238,10 +243,10 @@ def ckpt_grad_norm(grads, max_norm=0.0, stream=None):
     """fp32 [2]: the 2-norm of all gradients together (one type, bf16 or
     fp32), and the factor min(1, max_norm / (norm + 1e-6)) that clips them to
     max_norm (1 where max_norm is 0), for ckpt_adamw's grad_scale."""
-    grads = list(grads)
+    grads = _listed(grads)
     if not grads:
         raise ValueError("no gradients")
-    native, at = _module()
+    native, at = _native or _module()
     if native is not None and isinstance(grads[0], torch.Tensor) and grads[0].is_cuda:
         with _on(stream):
             got = native.grad_norm(at["ckpt_grad_norm"], grads, max_norm, _handle(stream, grads[0]))
@@ -270,19 +275,22 @@ def ckpt_adamw(params, masters, exp_avgs, exp_avg_sqs, grads, step, lr, beta1=0.
     moments, params (bf16, or fp32 in full precision) rounded from the masters,
     grads (bf16 or fp32).  One list of fragments may be a bucket, behind
     Checkpointer.wait_captured of the same range on the same stream."""
-    lists = [list(x) for x in (params, masters, exp_avgs, exp_avg_sqs, grads)]
+    params, masters, exp_avgs, exp_avg_sqs, grads = map(_listed, (params, masters, exp_avgs, exp_avg_sqs, grads))
+    native, at = _native or _module()
+    if native is not None and params and isinstance(params[0], torch.Tensor) and params[0].is_cuda:
+        rc = native.adamw(at["ckpt_adamw"], params, masters, exp_avgs, exp_avg_sqs, grads, step, lr, beta1, beta2, eps,
+                          weight_decay, grad_scale, _handle(stream, params[0]))
+        if rc is not None:
+            if rc != CKPT_OK:
+                _check(rc)
+            return
+    # Arguments that the native module leaves to this code, and those refused; every call where there is none.
+    lists = (params, masters, exp_avgs, exp_avg_sqs, grads)
     n = len(lists[0])
     if any(len(x) != n for x in lists):
         raise ValueError("lists of %s fragments" % ", ".join(str(len(x)) for x in lists))
     if n == 0:
         return
-    native, at = _module()
-    if native is not None and isinstance(lists[0][0], torch.Tensor) and lists[0][0].is_cuda:
-        rc = native.adamw(at["ckpt_adamw"], *lists, step, lr, beta1, beta2, eps, weight_decay, grad_scale,
-                          _handle(stream, lists[0][0]))
-        if rc is not None:
-            _check(rc)
-            return
     pt, gt = _type(lists[0][0], "param 0"), _type(lists[4][0], "grad 0")
     kinds = (pt, CKPT_TYPE_F32, CKPT_TYPE_F32, CKPT_TYPE_F32, gt)
     names = ("param", "master", "exp_avg", "exp_avg_sq", "grad")
