@@ -32,7 +32,7 @@ struct LossPlan {
     uint64_t piece = 0;       // tokens in a piece
     uint32_t pieces = 0;
     bool grad = false, teach = false, held = false; // held: a piece's logits are written,
-    bool e16 = false;                               // as exponentials in fp16 where d_logits goes
+    bool e16 = false;                               // as exponentials in 16 bits where d_logits goes
     bool copy_weight = false, copy_hidden = false, masked_hidden = false;
     bool two_sums = false; // the softmax at 1/temperature has sums of its own
     uint32_t parts = 0;

@@ -23,15 +23,12 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u16x4 u16x4_any __attribute__((aligned(2)));
 typedef u16x8 u16x8_any __attribute__((aligned(2)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kInf = __builtin_inff();
-constexpr float kE16 = 32768; // scale of the exponentials held in fp16
 
 __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 __device__ inline uint16_t bf16_of(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
@@ -161,6 +158,16 @@ __device__ inline uint2 bf16_run(f32x4 x)
     return __builtin_bit_cast(uint2, u16x4{bf16_of(x[0]), bf16_of(x[1]), bf16_of(x[2]), bf16_of(x[3])});
 }
 
+// Two values of [0, 1] in 16 bits each: the 7 exponent bits that fp32 has for them and 9 of the significand, to nearest.
+// The whole range of exp is kept, and the rounding is a quarter of bf16's.  (A NaN does not fit: it is known from the
+// sums.)
+__device__ inline uint32_t pack_e16(float a, float b)
+{
+    const uint32_t half = 1u << 13;
+    return (__float_as_uint(a) + half) >> 14 | ((__float_as_uint(b) + half) << 2 & 0xFFFF0000u);
+}
+__device__ inline float unpack_e16(uint16_t x) { return __uint_as_float((uint32_t)x << 14); }
+
 // What a lane reads for its epilogue ahead of the products.
 template <class End, int TQ>
 struct Early {
@@ -241,14 +248,11 @@ __device__ inline void finish(const LogitsOut& o, const Early<LogitsOut, TQ>& ea
                 if (o.part_t) o.part_t[at] = sum_t;
             }
             if (o.e16) {
-                // exp(l - top) 2^15, in 11 bits from 2^-29 on: its rounding is an eighth of d_logits' own
-                _Float16* row = (_Float16*)o.e16 + (uint64_t)q * o.ld + p0 + 8 * half;
+                uint16_t* row = o.e16 + (uint64_t)q * o.ld + p0 + 8 * half;
 #pragma unroll
                 for (int j = 0; j < kMine; j += 8) {
-                    f16x4 e[2];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) e[i / 4][i % 4] = (_Float16)(x[j + i] * kE16);
-                    const u16x8 v = pair_of(__builtin_bit_cast(uint2, e[0]), __builtin_bit_cast(uint2, e[1]));
+                    const u16x8 v = pair_of(make_uint2(pack_e16(x[j], x[j + 1]), pack_e16(x[j + 2], x[j + 3])),
+                                            make_uint2(pack_e16(x[j + 4], x[j + 5]), pack_e16(x[j + 6], x[j + 7])));
                     if (here) *(u16x8*)(row + 32 * (j / 16) + 8 * (j / 4 % 4)) = v;
                 }
             }
@@ -731,7 +735,7 @@ __device__ inline void only_row(const LossRows& r, float weight, float loss)
 // all of them.  Rounding d_logits to bf16 is what feeds the matrix cores; its errors are independent from word to word
 // and of the size of the gradients' own rounding.
 //
-// E16: the logits are held as exponentials in fp16 (cross entropy in bf16), in the place where d_logits goes, and
+// E16: the logits are held as exponentials in 16 bits (cross entropy in bf16), in the place where d_logits goes, and
 // the factors of the parts in LDS: 4 bytes of traffic a word, not 6.  Bound by HBM.
 template <int WAVES, bool E16>
 __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, const LossPiece p, const RowCopy copy)
@@ -818,13 +822,13 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
             r.lse[n] = lse;
             only_row(r, weight, loss);
         }
-        const float scale = weight * hard / (kE16 * sum);
+        const float scale = weight * hard / sum;
         for (uint32_t v = 8 * tid; v < p.dl_ld; v += 8 * kThreads) {
-            const f16x8 e = *(const f16x8*)(dl + v);
+            const u16x8 e = *(const u16x8*)(dl + v);
             const float f = v < r.vocab ? scale * s_more[v / kPartWords] : 0.0f;
             float g[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = f * (float)e[j];
+            for (int j = 0; j < 8; ++j) g[j] = f * unpack_e16(e[j]);
             if (target - v < 8) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)

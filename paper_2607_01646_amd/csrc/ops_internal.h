@@ -39,11 +39,11 @@ struct LogitsOut {
     float* part_t;         // the same sum at 1/temperature, or nullptr
     float inv_t;
     float* logits; // [tokens][ld], or nullptr
-    uint16_t* e16; // [tokens][ld] exp(l - its part's max) in fp16, or nullptr
+    uint16_t* e16; // [tokens][ld] exp(l - its part's max) in 16 bits, or nullptr
     uint64_t ld;   // a multiple of kPartWords
 };
 constexpr uint32_t kPartWords = 64;
-constexpr uint32_t kE16Parts = 8192; // of a row held in fp16: their factors fit in LDS
+constexpr uint32_t kE16Parts = 8192; // of a row held in 16 bits: their factors fit in LDS
 
 // Where the factor that all rows share and the loss come from when no launch
 // has made them (tokens == 0: one has).

@@ -18,6 +18,10 @@ SIZES = [(1, 64, 1), (1, 1, 1), (1, 128, 1000), (2, 63, 65), (31, 192, 129), (33
          (127, 200, 383), (129, 128, 128), (255, 8, 511), (257, 320, 1025), (300, 515, 2049), (700, 64, 300)]
 
 
+# sizes that take the larger tiles, products cut along the words, and both launches of the gradients
+LARGE = [(257, 2048, 8192), (1025, 512, 12001), (513, 1088, 4100), (2100, 640, 3000), (4097, 128, 20000), (700, 4096, 9000)]
+
+
 def bits(r):
     return [x.view(torch.int16) if x.dtype == BF else x.view(torch.int32) for x in r if x is not None]
 
@@ -31,6 +35,37 @@ def test_cross_entropy(tokens, dim, vocab, dtype):
     r = P.ckpt_linear_ce(x.hidden, x.weight, x.target)
     check(r, ref, grad=False)
     assert r.d_hidden is None and r.d_weight is None
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("tokens, dim, vocab", LARGE)
+def test_larger_sizes(tokens, dim, vocab, dtype):
+    x = inputs(tokens, dim, vocab, dtype, seed=tokens, masked=0.2, topk=5)
+    check(P.ckpt_linear_ce(x.hidden, x.weight, x.target, grad=True), definition(x.hidden, x.weight, x.target))
+    ref = definition(x.hidden, x.weight, x.target, x.teacher_index, x.teacher_logits, temperature=2.0, alpha=0.5)
+    check(P.ckpt_linear_distill(x.hidden, x.weight, x.teacher_index, x.teacher_logits, target=x.target, temperature=2.0,
+                                alpha=0.5, grad=True), ref)
+
+
+@pytest.mark.parametrize("tokens", [1, 40, 256])
+def test_few_tokens_gradients_are_as_exact_as_their_type(tokens):
+    """Up to 256 tokens the gradient of the logits keeps 16 bits: what is left is the outputs' own rounding."""
+    x = inputs(tokens, 256, 700, BF, seed=3, topk=5)
+    r = P.ckpt_linear_distill(x.hidden, x.weight, x.teacher_index, x.teacher_logits, target=x.target, temperature=2.0,
+                              alpha=0.5, grad=True)
+    ref = definition(x.hidden, x.weight, x.target, x.teacher_index, x.teacher_logits, temperature=2.0, alpha=0.5)
+    for got, want in ((r.d_hidden, ref.d_hidden), (r.d_weight, ref.d_weight)):
+        # half a unit of bf16, and 2^-13 of the tensor's size for two planes of 8 bits and the sums
+        assert ((got.double().reshape(want.shape) - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -13 * want.abs().max()).all()
+
+
+def test_a_wide_range_of_logits():
+    """Confident rows: logits hundreds apart, so that most probabilities vanish."""
+    for dtype in (BF, F32):
+        x = inputs(300, 128, 3000, dtype)
+        x.hidden *= 40
+        ref = definition(x.hidden, x.weight, x.target)
+        check(P.ckpt_linear_ce(x.hidden, x.weight, x.target, grad=True), ref)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
