@@ -33,6 +33,7 @@ struct LossPlan {
     uint32_t pieces = 0;
     bool grad = false, teach = false, held = false; // held: a piece's logits are written,
     bool e16 = false;                               // as exponentials in 16 bits where d_logits goes
+    bool dots = false;
     bool copy_weight = false, copy_hidden = false, masked_hidden = false;
     bool two_sums = false; // the softmax at 1/temperature has sums of its own
     uint32_t parts = 0;
@@ -84,11 +85,12 @@ LossPlan plan_loss(const ckpt_linear_loss_args* a)
     const auto direct = [&](const void* p, uint64_t ld) { // as it is fit for the loads of a product
         return !f32 && d % 64 == 0 && ld % 8 == 0 && ld <= kMostWidth && (uintptr_t)p % 16 == 0;
     };
-    l.copy_weight = !direct(a->weight, a->weight_stride);
+    l.dots = n <= kDotTokens; // the logits come from the operands as they are
+    l.copy_weight = !direct(a->weight, a->weight_stride) && !(l.dots && !l.grad);
     // With gradients the hidden states are copied so that those of rows that do not count are zero: the products over
     // the tokens multiply them by 0, and 0 * NaN is no 0.
     l.masked_hidden = l.grad && direct(a->hidden, a->hidden_stride); // by the row kernel
-    l.copy_hidden = !direct(a->hidden, a->hidden_stride);             // before the logits
+    l.copy_hidden = !direct(a->hidden, a->hidden_stride) && !(l.dots && !l.grad); // before the logits
     l.piece = n;
     if (l.held) {
         const uint64_t row = l.vocab_pad * ((l.e16 ? 0 : 4) + (l.grad ? 2 * l.dl_planes : 0));
@@ -255,8 +257,10 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
     r.mean = a->reduction == CKPT_LOSS_MEAN;
 
     hipError_t err = hipSuccess;
-#define CKPT_STEP(call, what) \
-    if ((err = (call)) != hipSuccess) return fail_free(CKPT_EHIP, "%s: %s", what, hipGetErrorString(err))
+#define CKPT_STEP(call, what)                                                                                      \
+    do {                                                                                                           \
+        if ((err = (call)) != hipSuccess) return fail_free(CKPT_EHIP, "%s: %s", what, hipGetErrorString(err));    \
+    } while (0)
 
     Operand W = {(const uint16_t*)a->weight, 0, a->weight_stride, (uint32_t)v, (uint32_t)d};
     if (l.copy_weight && n) {
@@ -294,7 +298,12 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
         lo.logits = l.held && !l.e16 ? (float*)(w + l.logits) : nullptr;
         lo.e16 = l.e16 ? (uint16_t*)(w + l.d_logits) : nullptr;
         lo.ld = l.vocab_pad;
-        CKPT_STEP(launch_logits(W, H, {(uint32_t)v, (uint32_t)rows, (uint32_t)l.dim_pad, 1}, l.planes, lo, s), "logits");
+        if (l.dots)
+            CKPT_STEP(launch_dots({a->weight, a->weight_stride}, {a->hidden, a->hidden_stride}, (uint32_t)d, f32, lo, s),
+                      "logits");
+        else
+            CKPT_STEP(launch_logits(W, H, {(uint32_t)v, (uint32_t)rows, (uint32_t)l.dim_pad, 1}, l.planes, lo, s),
+                      "logits");
 
         LossPiece p = {};
         p.row0 = (uint32_t)row0;

@@ -766,7 +766,19 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
     const float2* part = p.part + (uint64_t)row * p.parts;
     const float* part_t = p.part_t ? p.part_t + (uint64_t)row * p.parts : nullptr;
     float first[3] = {-kInf, -kInf, 0}; // the largest logit, the teacher's largest, the count of entries
-    for (uint32_t k = tid; k < p.parts; k += kThreads) first[0] = fmaxf(first[0], part[k].x);
+    // What does not wait for anything is asked for first: two parts a lane (the others of a larger vocabulary are read
+    // twice), the label's logit.
+    constexpr int kAhead = 2;
+    float2 ahead[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const uint32_t k = tid + u * kThreads;
+        ahead[u] = k < p.parts ? part[k] : make_float2(-kInf, 0);
+    }
+    const float target_logit = word ? r.target_logit[n] : 0.0f;
+    for (uint32_t k = tid + kAhead * kThreads; k < p.parts; k += kThreads) first[0] = fmaxf(first[0], part[k].x);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) first[0] = fmaxf(first[0], ahead[u].x);
     if (teach) {
         for (uint32_t k = tid; k < r.topk; k += kThreads) {
             int64_t at;
@@ -797,13 +809,16 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
     }
 
     float second[3] = {0, 0, 0}; // the sums of exponentials: the words', at the temperature, the teacher's
-    for (uint32_t k = tid; k < p.parts; k += kThreads) {
-        const float2 x = part[k];
+    auto add_part = [&](uint32_t k, float2 x) {
         const float f = x.x == -kInf ? (x.y == 0 ? 0.0f : x.y) : exp_of(x.x - low); // all words at -inf, or NaN
         second[0] += x.y * f;
         if (E16) s_more[k] = f;
         if (part_t && x.x != -kInf) second[1] += part_t[k] * exp_of((x.x - low) * inv_t);
-    }
+    };
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (tid + u * kThreads < p.parts) add_part(tid + u * kThreads, ahead[u]);
+    for (uint32_t k = tid + kAhead * kThreads; k < p.parts; k += kThreads) add_part(k, part[k]);
     if (teach)
         for (uint32_t k = tid; k < r.topk; k += kThreads) second[2] += exp_of((s_q[k] - t_top) * inv_t);
     block_reduce<WAVES, 0>(second, s_second);
@@ -814,7 +829,7 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
     float loss = 0, hard = 0;
     if (has_label) {
         hard = word ? 1 - r.alpha : __builtin_nanf(""); // the loss and the gradient show a label that is no word
-        loss = word ? hard * (lse - r.target_logit[n]) : hard;
+        loss = word ? hard * (lse - target_logit) : hard;
     }
     if constexpr (E16) {
         if (tid == 0) {
@@ -958,6 +973,134 @@ __global__ __launch_bounds__(1024) void finish_kernel(const LossRows r, bool tot
     if (total) *r.loss = (float)(loss * over);
 }
 
+// ---- logits of a few tokens ----
+//
+// For up to 4 tokens the head's rows are all that is read, and the matrix cores would wait for them: a workgroup takes
+// the 64 words of a part, each wave 16, and multiplies a run of 1 KiB of each row with the tokens' own on the vector
+// units, the next runs on their way.  No operand is copied or split first: any stride and alignment, and fp32 as it is.
+// Bound by HBM: one token against 32000 x 4096 in bf16.
+constexpr int kDotWords = 16;
+
+template <bool F32>
+struct Run { // a lane's values of one row
+    static constexpr int kValues = F32 ? 4 : 8;
+    uint4 raw;
+    __device__ inline float at(int j) const
+    {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        if (F32) return __uint_as_float(w[j]);
+        return __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+    }
+    // Values k.. of a row of dim, zeros past its end.
+    __device__ inline void load(const void* base, uint64_t row, uint64_t k, uint64_t dim)
+    {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        typedef u32x4 any __attribute__((aligned(2)));
+        if (k + kValues <= dim) {
+            const u32x4 x = __builtin_nontemporal_load((const any*)((const uint8_t*)base + (row + k) * (F32 ? 4 : 2)));
+            raw = {x[0], x[1], x[2], x[3]};
+            return;
+        }
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < kValues - 1; ++j) {
+            if (k + j >= dim) continue;
+            if (F32)
+                w[j] = ((const uint32_t*)base)[row + k + j];
+            else
+                w[j / 2] |= (uint32_t)((const uint16_t*)base)[row + k + j] << (j & 1 ? 16 : 0);
+        }
+        raw = {w[0], w[1], w[2], w[3]};
+    }
+};
+
+template <int N, bool F32>
+__global__ __launch_bounds__(256, 2) void dots_kernel(const DotOperand W, const DotOperand H, uint32_t dim, const LogitsOut o)
+{
+    constexpr uint32_t kRun = 64 * Run<F32>::kValues;
+    __shared__ float s_logit[N][kPartWords];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t p0 = blockIdx.x * kPartWords, mine = p0 + wave * kDotWords;
+    float acc[N][kDotWords];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < kDotWords; ++i) acc[n][i] = 0;
+    Run<F32> now[kDotWords], next[kDotWords], h[N], h_next[N];
+    auto load = [&](Run<F32>* w, Run<F32>* t, uint32_t k0) {
+#pragma unroll
+        for (int i = 0; i < kDotWords; ++i)
+            w[i].load(W.base, (uint64_t)min(mine + i, o.vocab - 1) * W.ld, k0 + Run<F32>::kValues * lane, dim);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            t[n].load(H.base, (uint64_t)min((uint32_t)n, o.tokens - 1) * H.ld, k0 + Run<F32>::kValues * lane, dim);
+    };
+    // Each wave begins at another run of its rows: rows lie a power of two apart for most heads, and waves at the same
+    // place in them would all wait for the same memory channels.
+    const uint32_t runs = (dim + kRun - 1) / kRun;
+    uint32_t at = (blockIdx.x * 4 + wave) % runs;
+    load(now, h, at * kRun);
+    for (uint32_t c = 0; c < runs; ++c) {
+        at = at + 1 == runs ? 0 : at + 1;
+        if (c + 1 < runs) load(next, h_next, at * kRun);
+#pragma unroll
+        for (int i = 0; i < kDotWords; ++i)
+#pragma unroll
+            for (int j = 0; j < Run<F32>::kValues; ++j)
+#pragma unroll
+                for (int n = 0; n < N; ++n) acc[n][i] = __builtin_fmaf(now[i].at(j), h[n].at(j), acc[n][i]);
+#pragma unroll
+        for (int i = 0; i < kDotWords; ++i) now[i] = next[i];
+#pragma unroll
+        for (int n = 0; n < N; ++n) h[n] = h_next[n];
+    }
+    // The lanes' sums: each exchange halves the words that a lane answers for.
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        int left = kDotWords;
+#pragma unroll
+        for (int step = 32; step > 2; step /= 2) {
+            left /= 2;
+            const bool high = lane & step;
+#pragma unroll
+            for (int i = 0; i < left; ++i) {
+                const float keep = high ? acc[n][i + left] : acc[n][i], give = high ? acc[n][i] : acc[n][i + left];
+                acc[n][i] = keep + __shfl_xor(give, step);
+            }
+        }
+        float x = acc[n][0];
+        x += __shfl_xor(x, 2);
+        x += __shfl_xor(x, 1);
+        const uint32_t word = (lane >> 5 & 1) * 8 + (lane >> 4 & 1) * 4 + (lane >> 3 & 1) * 2 + (lane >> 2 & 1);
+        if ((lane & 3) == 0) s_logit[n][wave * kDotWords + word] = x;
+    }
+    __syncthreads();
+    if (wave >= N || wave >= o.tokens) return;
+    const uint32_t q = wave, p = p0 + lane;
+    const float x = p < o.vocab ? s_logit[q < N ? q : 0][lane] : -kInf;
+    if (o.logits) o.logits[(uint64_t)q * o.ld + p] = x; // ld covers whole parts
+    if (o.target && o.target[q] == (int64_t)p && p < o.vocab) o.target_logit[q] = x;
+    const float top = wave_max(x), low = top == -kInf ? 0.0f : top;
+    const float sum = wave_sum(exp_of(x - low)), sum_t = o.part_t ? wave_sum(exp_of((x - low) * o.inv_t)) : 0.0f;
+    if (lane == 0) {
+        const uint64_t at = (uint64_t)q * o.parts + blockIdx.x;
+        o.part[at] = make_float2(top, sum);
+        if (o.part_t) o.part_t[at] = sum_t;
+    }
+}
+
+template <bool F32>
+hipError_t dots_of(const DotOperand& w, const DotOperand& h, uint32_t dim, const LogitsOut& o, hipStream_t stream)
+{
+    if (o.tokens == 1)
+        dots_kernel<1, F32><<<o.parts, 256, 0, stream>>>(w, h, dim, o);
+    else if (o.tokens == 2)
+        dots_kernel<2, F32><<<o.parts, 256, 0, stream>>>(w, h, dim, o);
+    else
+        dots_kernel<4, F32><<<o.parts, 256, 0, stream>>>(w, h, dim, o);
+    return hipGetLastError();
+}
+
 __global__ __launch_bounds__(256) void zero_kernel(void* out, uint32_t rows, uint32_t cols, uint64_t ld, bool f32)
 {
     for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x)
@@ -1082,6 +1225,13 @@ hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape&
                          const LogitsOut& o, hipStream_t stream)
 {
     return planes == 3 ? logits_of<3>(w, h, s, o, stream) : logits_of<1>(w, h, s, o, stream);
+}
+
+hipError_t launch_dots(const DotOperand& w, const DotOperand& h, uint32_t dim, bool f32, const LogitsOut& o,
+                       hipStream_t stream)
+{
+    if (o.tokens == 0 || o.tokens > kDotTokens || o.e16) return hipErrorInvalidValue;
+    return f32 ? dots_of<true>(w, h, dim, o, stream) : dots_of<false>(w, h, dim, o, stream);
 }
 
 hipError_t launch_gradients(const Operand& w, const Operand& h, uint32_t zp, const Operand& dl, uint32_t zq,

@@ -68,6 +68,15 @@ struct GradOut {
 
 hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape& s, uint32_t planes,
                          const LogitsOut& o, hipStream_t stream);
+// The same for at most kDotTokens tokens, from the caller's own operands (any
+// alignment of their elements).
+constexpr uint32_t kDotTokens = 4;
+struct DotOperand {
+    const void* base;
+    uint64_t ld;
+};
+hipError_t launch_dots(const DotOperand& w, const DotOperand& h, uint32_t dim, bool f32, const LogitsOut& o,
+                       hipStream_t stream);
 // Both gradients, in one launch where they are small:
 //   d_hidden: P = weight (k = words across rows), Q = d_logits (k contiguous)
 //   d_weight: P = hidden, Q = d_logits (both with k = tokens across rows)
