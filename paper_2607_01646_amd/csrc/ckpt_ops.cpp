@@ -19,6 +19,7 @@ constexpr uint64_t kDefaultPiece = 2ull << 30;
 constexpr uint64_t kFewTokens = 256;
 // So few tokens' weights are summed again by each workgroup that needs the sum.
 constexpr uint64_t kFewSums = 1024;
+constexpr uint64_t kAround = 64; // tokens of one small tile (a token's loss does not depend on how many are above that)
 constexpr uint64_t kSliceBytes = 256ull << 20; // of the partial sums of a product cut along k
 
 uint64_t up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
@@ -85,7 +86,7 @@ LossPlan plan_loss(const ckpt_linear_loss_args* a)
     const auto direct = [&](const void* p, uint64_t ld) { // as it is fit for the loads of a product
         return !f32 && d % 64 == 0 && ld % 8 == 0 && ld <= kMostWidth && (uintptr_t)p % 16 == 0;
     };
-    l.dots = n <= kDotTokens; // the logits come from the operands as they are
+    l.dots = n <= kDotTokens || (f32 && !l.grad && n <= kDotTokensF32); // the logits come from the operands as they are
     l.copy_weight = !direct(a->weight, a->weight_stride) && !(l.dots && !l.grad);
     // With gradients the hidden states are copied so that those of rows that do not count are zero: the products over
     // the tokens multiply them by 0, and 0 * NaN is no 0.
@@ -302,7 +303,7 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
             CKPT_STEP(launch_dots({a->weight, a->weight_stride}, {a->hidden, a->hidden_stride}, (uint32_t)d, f32, lo, s),
                       "logits");
         else
-            CKPT_STEP(launch_logits(W, H, {(uint32_t)v, (uint32_t)rows, (uint32_t)l.dim_pad, 1}, l.planes, lo, s),
+            CKPT_STEP(launch_logits(W, H, {(uint32_t)v, (uint32_t)rows, (uint32_t)l.dim_pad, 1, n <= kAround}, l.planes, lo, s),
                       "logits");
 
         LossPiece p = {};
@@ -356,8 +357,8 @@ extern "C" ckpt_status ckpt_linear_loss(const ckpt_linear_loss_args* a, int32_t 
             gh.slice = rows * l.dim_pad;
         }
         CKPT_STEP(launch_gradients(W, H, l.planes, dl_rows, l.dl_planes,
-                                   {(uint32_t)d, (uint32_t)rows, (uint32_t)l.vocab_pad, l.slices}, gh,
-                                   {(uint32_t)d, (uint32_t)v, (uint32_t)rows_pad, 1}, gw, s),
+                                   {(uint32_t)d, (uint32_t)rows, (uint32_t)l.vocab_pad, l.slices, false}, gh,
+                                   {(uint32_t)d, (uint32_t)v, (uint32_t)rows_pad, 1, false}, gw, s),
                   "gradients");
         if (l.slices > 1)
             CKPT_STEP(launch_join((const float*)gh.out, gh.slice, (uint32_t)l.dim_pad, l.slices, (uint32_t)d,

@@ -414,9 +414,12 @@ __device__ inline void product(const Operand& P, const Operand& Q, const Product
     // The wave's load `i` of a step's kLoads into buffer s; none past the last step.
     constexpr int kLoadsP = TileP::template loads<kThreads>(), kLoadsQ = TileQ::template loads<kThreads>();
     constexpr int kLoads = ZP * kLoadsP + ZQ * kLoadsQ;
+    // shape.around: each workgroup goes round its steps from another one.
+    const uint32_t round = last - first;
+    const uint32_t ahead = shape.around && round ? __builtin_amdgcn_readfirstlane(block % round) : 0;
     auto load = [&](uint16_t* s, uint32_t step, int i) {
         const bool any = step < last;
-        const uint32_t k0 = any ? step * BK : 0;
+        const uint32_t at = step + ahead, k0 = any ? (at < last ? at : at - round) * BK : 0;
         if (i < ZP * kLoadsP) {
             const int z = i % ZP, j = i / ZP;
             TileP::template load<kThreads>(P, P.base + z * P.plane, lane_p, p0, k0, any, j, s + z * TileP::kElems);
@@ -975,11 +978,11 @@ __global__ __launch_bounds__(1024) void finish_kernel(const LossRows r, bool tot
 
 // ---- logits of a few tokens ----
 //
-// For up to 4 tokens the head's rows are all that is read, and the matrix cores would wait for them: a workgroup takes
-// the 64 words of a part, each wave 16, and multiplies a run of 1 KiB of each row with the tokens' own on the vector
-// units, the next runs on their way.  No operand is copied or split first: any stride and alignment, and fp32 as it is.
-// Bound by HBM: one token against 32000 x 4096 in bf16.
-constexpr int kDotWords = 16;
+// For up to 4 tokens (fp32: some more, 8 at a time) the head's rows are all that is read, and the matrix cores would wait
+// for them: a workgroup takes the 64 words of a part, each wave 8, and multiplies a run of 1 KiB of each row with the
+// tokens' own on the vector units, the next runs on their way.  No operand is copied or split first: any stride and
+// alignment, and fp32 as it is.  Bound by HBM: one token against 32000 x 4096 in bf16 44 us, 5.9 TB/s.
+constexpr int kDotWords = 8, kDotWaves = kPartWords / kDotWords;
 
 template <bool F32>
 struct Run { // a lane's values of one row
@@ -1015,7 +1018,7 @@ struct Run { // a lane's values of one row
 };
 
 template <int N, bool F32>
-__global__ __launch_bounds__(256, 2) void dots_kernel(const DotOperand W, const DotOperand H, uint32_t dim, const LogitsOut o)
+__global__ __launch_bounds__(kDotWaves * 64, 2) void dots_kernel(const DotOperand W, const DotOperand H, uint32_t dim, const LogitsOut o)
 {
     constexpr uint32_t kRun = 64 * Run<F32>::kValues;
     __shared__ float s_logit[N][kPartWords];
@@ -1038,7 +1041,7 @@ __global__ __launch_bounds__(256, 2) void dots_kernel(const DotOperand W, const 
     // Each wave begins at another run of its rows: rows lie a power of two apart for most heads, and waves at the same
     // place in them would all wait for the same memory channels.
     const uint32_t runs = (dim + kRun - 1) / kRun;
-    uint32_t at = (blockIdx.x * 4 + wave) % runs;
+    uint32_t at = (blockIdx.x * kDotWaves + wave) % runs;
     load(now, h, at * kRun);
     for (uint32_t c = 0; c < runs; ++c) {
         at = at + 1 == runs ? 0 : at + 1;
@@ -1059,7 +1062,7 @@ __global__ __launch_bounds__(256, 2) void dots_kernel(const DotOperand W, const 
     for (int n = 0; n < N; ++n) {
         int left = kDotWords;
 #pragma unroll
-        for (int step = 32; step > 2; step /= 2) {
+        for (int step = 32; step > 4; step /= 2) {
             left /= 2;
             const bool high = lane & step;
 #pragma unroll
@@ -1069,10 +1072,9 @@ __global__ __launch_bounds__(256, 2) void dots_kernel(const DotOperand W, const 
             }
         }
         float x = acc[n][0];
-        x += __shfl_xor(x, 2);
-        x += __shfl_xor(x, 1);
-        const uint32_t word = (lane >> 5 & 1) * 8 + (lane >> 4 & 1) * 4 + (lane >> 3 & 1) * 2 + (lane >> 2 & 1);
-        if ((lane & 3) == 0) s_logit[n][wave * kDotWords + word] = x;
+        for (int step = 4; step; step /= 2) x += __shfl_xor(x, step);
+        const uint32_t word = (lane >> 5 & 1) * 4 + (lane >> 4 & 1) * 2 + (lane >> 3 & 1);
+        if ((lane & 7) == 0) s_logit[n][wave * kDotWords + word] = x;
     }
     __syncthreads();
     if (wave >= N || wave >= o.tokens) return;
@@ -1092,12 +1094,15 @@ __global__ __launch_bounds__(256, 2) void dots_kernel(const DotOperand W, const 
 template <bool F32>
 hipError_t dots_of(const DotOperand& w, const DotOperand& h, uint32_t dim, const LogitsOut& o, hipStream_t stream)
 {
+    constexpr uint32_t kThreads = kDotWaves * 64;
     if (o.tokens == 1)
-        dots_kernel<1, F32><<<o.parts, 256, 0, stream>>>(w, h, dim, o);
+        dots_kernel<1, F32><<<o.parts, kThreads, 0, stream>>>(w, h, dim, o);
     else if (o.tokens == 2)
-        dots_kernel<2, F32><<<o.parts, 256, 0, stream>>>(w, h, dim, o);
+        dots_kernel<2, F32><<<o.parts, kThreads, 0, stream>>>(w, h, dim, o);
+    else if (o.tokens <= 4)
+        dots_kernel<4, F32><<<o.parts, kThreads, 0, stream>>>(w, h, dim, o);
     else
-        dots_kernel<4, F32><<<o.parts, 256, 0, stream>>>(w, h, dim, o);
+        dots_kernel<8, F32><<<o.parts, kThreads, 0, stream>>>(w, h, dim, o);
     return hipGetLastError();
 }
 
@@ -1230,8 +1235,20 @@ hipError_t launch_logits(const Operand& w, const Operand& h, const ProductShape&
 hipError_t launch_dots(const DotOperand& w, const DotOperand& h, uint32_t dim, bool f32, const LogitsOut& o,
                        hipStream_t stream)
 {
-    if (o.tokens == 0 || o.tokens > kDotTokens || o.e16) return hipErrorInvalidValue;
-    return f32 ? dots_of<true>(w, h, dim, o, stream) : dots_of<false>(w, h, dim, o, stream);
+    if (o.e16) return hipErrorInvalidValue;
+    for (uint32_t n = 0; n < o.tokens; n += 8) { // the tokens of a launch
+        LogitsOut part = o;
+        part.tokens = std::min(8u, o.tokens - n);
+        part.target = o.target ? o.target + n : nullptr;
+        part.target_logit = o.target_logit + n;
+        part.part = o.part + (uint64_t)n * o.parts;
+        part.part_t = o.part_t ? o.part_t + (uint64_t)n * o.parts : nullptr;
+        part.logits = o.logits ? o.logits + (uint64_t)n * o.ld : nullptr;
+        const DotOperand rows = {(const uint8_t*)h.base + (uint64_t)n * h.ld * (f32 ? 4 : 2), h.ld};
+        const hipError_t e = f32 ? dots_of<true>(w, rows, dim, part, stream) : dots_of<false>(w, rows, dim, part, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_gradients(const Operand& w, const Operand& h, uint32_t zp, const Operand& dl, uint32_t zq,
@@ -1247,7 +1264,7 @@ hipError_t launch_gradients(const Operand& w, const Operand& h, uint32_t zp, con
 
 uint32_t d_hidden_slices(uint32_t p, uint32_t q, uint32_t k, uint32_t zp, uint32_t zq, uint32_t most)
 {
-    return tiling({p, q, k, 1}, zp, zq, std::max(1u, most)).slices;
+    return tiling({p, q, k, 1, false}, zp, zq, std::max(1u, most)).slices;
 }
 
 hipError_t launch_join(const float* slices, uint64_t slice, uint32_t ld_s, uint32_t n, uint32_t p, uint32_t q,
