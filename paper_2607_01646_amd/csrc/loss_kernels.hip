@@ -348,7 +348,7 @@ __device__ inline void finish(const GradEnd& e, const Early<GradEnd, TQ>& early,
 // Which tile a workgroup takes.  Workgroups go round the 8 XCDs, each with an L2 of its own: an XCD gets a run of
 // consecutive tiles, and runs go through bands of kBand tiles of q, so that the tiles which an XCD works on at a time
 // share their operands' rows.
-constexpr uint32_t kXcds = 8, kBand = 8;
+constexpr uint32_t kXcds = 8, kBand = 4;
 __device__ inline uint2 tile_of(uint32_t block, uint32_t np, uint32_t nq)
 {
     const uint32_t n = np * nq, each = n / kXcds, more = n % kXcds;
@@ -1183,8 +1183,9 @@ Tiling tiling(const ProductShape& s, uint32_t zp, uint32_t zq, uint32_t most)
 // The shapes.  The smaller two of gradients have 4 waves each, for one launch of both, and together no more LDS than
 // lets two workgroups share a unit (fp32: no such shapes).
 template <int ZP, int ZQ, bool PA, bool QA>
-using Large = std::conditional_t<ZP == 3, Shape<ZP, ZQ, PA, QA, 256, 128, 4, 2, 32, 2>,
-                                 Shape<ZP, ZQ, PA, QA, 256, 256, 4, 2, 64, 2>>;
+using Large = std::conditional_t<
+    ZP == 3, Shape<ZP, ZQ, PA, QA, 256, 128, 4, 2, 32, 2>,
+    std::conditional_t<PA, Shape<ZP, ZQ, PA, QA, 256, 256, 4, 2, 32, 4>, Shape<ZP, ZQ, PA, QA, 256, 256, 2, 4, 64, 2>>>;
 template <int ZP, int ZQ, bool PA, bool QA>
 using Middle = Shape<ZP, ZQ, PA, QA, 128, 128, 2, 2, ZP == 3 || ZQ == 2 ? 32 : 64, 2>;
 template <int ZP, int ZQ, bool PA, bool QA>
