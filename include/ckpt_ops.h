@@ -37,8 +37,8 @@ extern "C" {
 
 /* ---- Losses of the vocabulary head ----
  *
- * logits l = hidden weight^T are never held for more than one piece of the
- * tokens.  With w the token weight, lse = log sum_v exp l_v and y the target:
+ * The logits l = hidden weight^T are never held for more than one piece of the
+ * tokens; the cross entropy without gradients holds none.  With w the token weight, lse = log sum_v exp l_v and y the target:
  *   ce_n   = lse_n - l_n,y
  * and, with topk > 0, from a teacher's logits t_k at the words i_k:
  *   q      = softmax of t / T over the row's entries
@@ -76,7 +76,8 @@ typedef struct {
     uint64_t teacher_logits_stride;
     float temperature, alpha; /* T > 0, alpha in [0, 1] */
     const float* grad_scale;  /* device scalar or NULL (1) */
-    uint64_t piece_bytes;     /* bound on the logits held at a time, at least 256 rows of them; 0 = 2 GiB */
+    uint64_t piece_bytes;     /* bound on what is held for the tokens at a time (their logits most of all), at
+                                 least 256 tokens'; 0 = 2 GiB */
     /* outputs */
     float* loss;       /* scalar */
     float* token_loss; /* [tokens] loss_n, before the weight */

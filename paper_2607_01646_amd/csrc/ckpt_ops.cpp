@@ -14,6 +14,7 @@ namespace {
 constexpr uint64_t kMost = 0x7fffffffull;  // tokens
 constexpr uint64_t kMostWidth = 1ull << 22; // dim, vocab: a tile's rows of an operand stay within 31 bits of bytes
 constexpr uint64_t kDefaultPiece = 2ull << 30;
+constexpr uint64_t kMostPiece = 1ull << 22; // tokens: a workgroup a row stays below 2^32 lanes
 // For so few tokens d_logits has a second bf16 plane: the products are bound by the weight's bytes, and the gradients
 // of few terms have no others to average their rounding with.
 constexpr uint64_t kFewTokens = 256;
@@ -92,12 +93,11 @@ LossPlan plan_loss(const ckpt_linear_loss_args* a)
     // the tokens multiply them by 0, and 0 * NaN is no 0.
     l.masked_hidden = l.grad && direct(a->hidden, a->hidden_stride); // by the row kernel
     l.copy_hidden = !direct(a->hidden, a->hidden_stride) && !(l.dots && !l.grad); // before the logits
-    l.piece = n;
-    if (l.held) {
-        const uint64_t row = l.vocab_pad * ((l.e16 ? 0 : 4) + (l.grad ? 2 * l.dl_planes : 0));
-        const uint64_t most = std::max<uint64_t>(256, (a->piece_bytes ? a->piece_bytes : kDefaultPiece) / row / 64 * 64);
-        l.piece = std::min(n, most);
-    }
+    // What a token takes in the workspace: its logits and their gradient, its copy, its statistics.
+    const uint64_t row = l.vocab_pad * ((l.held && !l.e16 ? 4 : 0) + (l.grad ? 2 * l.dl_planes : 0)) +
+                         (l.copy_hidden || l.masked_hidden ? 2 * l.planes * l.dim_pad : 0) + (l.two_sums ? 12 : 8) * l.parts;
+    const uint64_t most = (a->piece_bytes ? a->piece_bytes : kDefaultPiece) / row / 64 * 64;
+    l.piece = std::min({n, std::max<uint64_t>(256, most), kMostPiece});
     l.pieces = n ? (uint32_t)((n + l.piece - 1) / l.piece) : 0;
     const uint64_t piece_pad = up(l.piece, 64);
 

@@ -1289,8 +1289,13 @@ hipError_t launch_zero(void* out, uint32_t rows, uint32_t cols, uint64_t ld, boo
 hipError_t launch_prepare(const LossRows* r, uint32_t row0, uint32_t rows, const RowCopy& c, hipStream_t stream)
 {
     const uint32_t all = c.src ? std::max(rows, c.dst_rows) : rows;
-    if (all == 0) return hipSuccess;
-    prepare_kernel<<<(all + 3) / 4, kRowThreads, 0, stream>>>(r ? *r : LossRows(), r != nullptr, row0, rows, c);
+    constexpr uint32_t kRows = 1u << 24; // of a launch, a wave each: 2^30 lanes
+    if (c.src && all > kRows) return hipErrorInvalidValue;
+    for (uint32_t at = 0; at < all; at += kRows) {
+        const uint32_t n = std::min(kRows, all - at);
+        prepare_kernel<<<(n + 3) / 4, kRowThreads, 0, stream>>>(r ? *r : LossRows(), r != nullptr, row0 + at,
+                                                               std::min(n, rows - std::min(rows, at)), c);
+    }
     return hipGetLastError();
 }
 

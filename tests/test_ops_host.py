@@ -2,10 +2,12 @@
 structures against the header's, argument checks that need no device, and the
 bound on the workspace (CPU only)."""
 import ctypes as C
+import functools
 import math
 import os
 import re
 import subprocess
+import tempfile
 
 import pytest
 import torch
@@ -58,6 +60,9 @@ def test_the_workspace_is_bounded_by_the_piece():
     # without gradients the cross entropy holds no logits at all
     rc, n = need(tokens=8192)
     assert rc == P.CKPT_OK and n < 8192 * 32000 // 4
+    # nor does what it keeps for its tokens grow beyond a piece, up to the most tokens there can be
+    sizes = [need(tokens=n, piece_bytes=64 << 20)[1] for n in (1 << 20, (1 << 31) - 1)]
+    assert sizes[1] - sizes[0] <= 4 * ((1 << 31) - (1 << 20)) + 256
 
 
 @pytest.mark.parametrize("kw", [
@@ -93,3 +98,60 @@ def test_host_tensors_are_refused():
         P.ckpt_adamw([h], [h], [h], [h], [h], step=1, lr=1e-3)
     with pytest.raises(ValueError, match="fragments"):
         P.ckpt_adamw([h], [h], [h], [h], [], step=1, lr=1e-3)
+
+
+@functools.lru_cache(None)
+def kernels(name):
+    """The gfx950 assembly of a kernel file."""
+    from paper_2607_01646_amd import build as B
+
+    with tempfile.TemporaryDirectory() as d:
+        return assembly(B, name, os.path.join(d, "k.s"))
+
+
+def assembly(B, name, out):
+    cmd = [B.HIPCC] + [f for f in B.DEVICE_FLAGS if f != "-fPIC"] + [
+        "-I", os.path.join(B.ROOT, "include"), "-I", B.CSRC, "--cuda-device-only", "-S", os.path.join(B.CSRC, name),
+        "-o", out]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    with open(out) as f:
+        return f.read()
+
+
+@pytest.mark.parametrize("name", ["loss_kernels.hip", "optim_kernels.hip"])
+def test_kernels_keep_their_registers_and_use_no_packed_fp32(name):
+    """No vector register goes to memory (the products' loops wait for their loads by count: a spill among them would
+    be waited for too), and no packed fp32 arithmetic is made."""
+    text = kernels(name)
+    spills = [int(x) for x in re.findall(r"\.vgpr_spill_count:\s*(\d+)", text)]
+    assert spills and not any(spills)
+    assert not re.search(r"\bv_pk_(add|mul|fma)_f32\b", text)
+
+
+def test_products_wait_for_no_load_that_is_to_stay_in_flight():
+    """In the loops of the largest products nothing but the barrier at which the waves meet waits for the loads made
+    since the last one; with four buffers not even that."""
+    text = kernels("loss_kernels.hip")
+    bodies = re.findall(r"^(_ZN4ckpt\w*product_kernel\w*Li256ELi256E\w*):\s(.*?)s_endpgm", text, re.S | re.M)
+    assert len(bodies) == 3
+    for name, body in bodies:
+        lines = [x.strip() for x in body.split("\n") if x.strip() and not x.strip().startswith(";")]
+        labels = {x.split(":")[0]: i for i, x in enumerate(lines) if x.startswith(".L")}
+        loops = []
+        for i, x in enumerate(lines):
+            m = re.match(r"s_c?branch\w*\s+(\.L\w+)", x)
+            if m and labels.get(m.group(1), i) < i:
+                loops.append(lines[labels[m.group(1)]:i])
+        loop = max(loops, key=lambda l: sum("mfma" in x for x in l))
+        assert sum("mfma" in x for x in loop) >= 64
+        flying = waits = 0
+        for x, after in zip(loop + loop, loop[1:] + loop + loop[:1]):
+            if x.startswith("buffer_load") and x.endswith("lds"):
+                flying += 1
+            elif x.startswith("s_waitcnt") and "vmcnt(0)" in x:
+                waits += 1
+                assert "Li32ELi4E" not in name and (flying == 0 or after.startswith("s_barrier")), (name, x, after)
+            elif x.startswith("s_barrier"):
+                flying = 0
+        assert waits or "Li32ELi4E" in name
