@@ -1173,7 +1173,7 @@ Tiling tiling(const ProductShape& s, uint32_t zp, uint32_t zq, uint32_t most)
             const double steps = (double)((s.k / 64 + n - 1) / n);
             const double t = pairs * (steps * both + 3) +
                              (left == 0 ? 0 : left <= 256 ? steps * alone + 3 : steps * both + 3) +
-                             (n > 1 ? 3 + 8.0 * s.p * s.q * n / 4e6 : 0);
+                             (n > 1 ? 3 + 0.8 * n + 8.0 * s.p * s.q * n / 6e6 : 0);
             if (t < least) least = t, best = {(Size)size, n};
         }
     }
