@@ -105,6 +105,8 @@ struct Tile {
     {
         static_assert(kChunks % THREADS == 0, "every wave has the same loads");
         const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        // The last values of k may lie past the operand altogether (k runs to a multiple of 64, BK may be less).
+        if constexpr (ACROSS) k0 = min(k0, o.rows - 1);
         const uint16_t* from = base + (ACROSS ? (uint64_t)k0 * o.ld : (uint64_t)row0 * o.ld + k0);
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
             (void*)from, 0, __builtin_amdgcn_readfirstlane(any ? -1 : 0), 0x00020000);

@@ -194,6 +194,18 @@ def test_strides_offsets_and_leading_dimensions(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("tokens, dim, vocab", [(40, 256, 8200), (256, 1024, 8209), (2048, 2048, 8224), (2048, 2048, 8193)])
+def test_nothing_beyond_the_vocabulary_is_read(tokens, dim, vocab, dtype):
+    """A head whose rows are the first of a larger buffer, and whose words leave most of the products' last 64 values
+    of k without a row: the rows behind it are NaN, which no zero of d_logits would take out of d_hidden."""
+    x = inputs(tokens, dim, vocab, dtype, seed=vocab, masked=0.1)
+    big = torch.full((vocab + 64, dim), math.nan, dtype=dtype, device="cuda")
+    big[:vocab] = x.weight
+    r = P.ckpt_linear_ce(x.hidden, big[:vocab], x.target, grad=True)
+    check(r, definition(x.hidden, x.weight, x.target))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_sum_scale_and_weights(dtype):
     x = inputs(130, 72, 200, dtype, masked=0.2)
     w = torch.rand(130, device="cuda") * 3
