@@ -126,11 +126,12 @@ def _rows(t, what):
     return rows, cols, t.stride(dims[-1])
 
 
-def _on(stream):
-    """The context in which the outputs and the workspace of work on `stream` are allocated."""
+def _on(stream, tensor):
+    """The context in which the outputs and the workspace of work on `stream` are allocated.  A handle is a stream of
+    the tensor's device, which need not be the current one."""
     if stream is None:
         return _HERE
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, tensor.device) if isinstance(stream, int) else stream)
 
 
 def _listed(x):
@@ -150,7 +151,7 @@ def _linear_loss(hidden, weight, target, teacher, temperature, alpha, token_weig
                  grad_scale, piece_bytes, stream):
     native, at = _native or _module()
     if native is not None and isinstance(hidden, torch.Tensor) and hidden.is_cuda and reduction in _REDUCTIONS:
-        with _on(stream):
+        with _on(stream, hidden):
             got = native.linear_loss(at["ckpt_linear_loss_workspace"], at["ckpt_linear_loss"], hidden, weight, target,
                                      None if teacher is None else teacher[0], None if teacher is None else teacher[1],
                                      temperature, alpha, token_weight, ignore_index, _REDUCTIONS[reduction], grad,
@@ -197,7 +198,7 @@ def _linear_loss(hidden, weight, target, teacher, temperature, alpha, token_weig
         a.grad_scale = _plain(grad_scale, "grad_scale", torch.float32, 1)
     a.piece_bytes = piece_bytes
     d_hidden = d_weight = None
-    with _on(stream):
+    with _on(stream, hidden):
         out = torch.empty(2 * n + 1, dtype=torch.float32, device=hidden.device)
         a.loss = out.data_ptr()
         a.token_loss = a.loss + 4
@@ -248,7 +249,7 @@ def ckpt_grad_norm(grads, max_norm=0.0, stream=None):
         raise ValueError("no gradients")
     native, at = _native or _module()
     if native is not None and isinstance(grads[0], torch.Tensor) and grads[0].is_cuda:
-        with _on(stream):
+        with _on(stream, grads[0]):
             got = native.grad_norm(at["ckpt_grad_norm"], grads, max_norm, _handle(stream, grads[0]))
         if got is not None:
             _check(got[0])
@@ -261,7 +262,7 @@ def ckpt_grad_norm(grads, max_norm=0.0, stream=None):
         arr[i].nbytes = tensor_bytes(t)
         arr[i].dev_ptr = t.data_ptr() if arr[i].nbytes else None
     device = grads[0].device
-    with _on(stream):
+    with _on(stream, grads[0]):
         out = torch.empty(2, dtype=torch.float32, device=device)
         scratch = torch.empty(CKPT_GRAD_NORM_SCRATCH, dtype=torch.uint8, device=device)
         _check(_ops().ckpt_grad_norm(arr, len(grads), kind, max_norm, out.data_ptr(), scratch.data_ptr(), device.index,

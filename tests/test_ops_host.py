@@ -100,6 +100,20 @@ def test_host_tensors_are_refused():
         P.ckpt_adamw([h], [h], [h], [h], [], step=1, lr=1e-3)
 
 
+def test_a_stream_handle_belongs_to_the_tensors_device(monkeypatch):
+    """What is allocated for work on a stream given as a handle comes from that stream's pool, on the tensor's device,
+    whichever device is current."""
+    seen = []
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: seen.append((handle, device)) or "s")
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: s)
+
+    class On1:
+        device = torch.device("cuda", 1)
+
+    assert ops._on(1234, On1()) == "s" and seen == [(1234, torch.device("cuda", 1))]
+    assert ops._on("a stream", On1()) == "a stream" and ops._on(None, On1()) is ops._HERE
+
+
 @functools.lru_cache(None)
 def kernels(name):
     """The gfx950 assembly of a kernel file."""
