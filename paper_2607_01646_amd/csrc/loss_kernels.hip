@@ -815,10 +815,12 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(const LossRows r, cons
 
     float second[3] = {0, 0, 0}; // the sums of exponentials: the words', at the temperature, the teacher's
     auto add_part = [&](uint32_t k, float2 x) {
-        const float f = x.x == -kInf ? (x.y == 0 ? 0.0f : x.y) : exp_of(x.x - low); // all words at -inf, or NaN
+        // A maximum of -inf: all words at -inf and sums of 0, or NaN among them, which a maximum passes by and the sums show.
+        const bool none = x.x == -kInf;
+        const float f = none ? x.y : exp_of(x.x - low);
         second[0] += x.y * f;
         if (E16) s_more[k] = f;
-        if (part_t && x.x != -kInf) second[1] += part_t[k] * exp_of((x.x - low) * inv_t);
+        if (part_t) second[1] += part_t[k] * (none ? x.y : exp_of((x.x - low) * inv_t));
     };
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)

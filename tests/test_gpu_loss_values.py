@@ -1,0 +1,57 @@
+"""The vocabulary head's losses at values that are no numbers, against the
+definition in 64 bits (needs an MI355X; through the C ABI)."""
+import math
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from ops_util import check, definition, inputs
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    import paper_2607_01646_amd as P
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def distill(x, **kw):
+    return P.ckpt_linear_distill(x.hidden, x.weight, x.teacher_index, x.teacher_logits, target=x.target, **kw)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("temperature, alpha", [(1.0, 1.0), (2.0, 1.0), (2.0, 0.5), (0.5, 1.0)])
+@pytest.mark.parametrize("tokens", [3, 70, 300])
+def test_nan_in_a_hidden_state_shows_in_distillation(tokens, temperature, alpha, grad, dtype):
+    x = inputs(tokens, 64, 300, dtype, seed=tokens, topk=5)
+    x.hidden[1, 7] = math.nan
+    kw = dict(temperature=temperature, alpha=alpha)
+    r = distill(x, grad=grad, **kw)
+    odd = torch.arange(tokens, device="cuda") == 1
+    assert torch.equal(r.lse.isnan(), odd) and torch.equal(r.token_loss.isnan(), odd) and r.loss.isnan()
+    if grad:
+        assert torch.equal(r.d_hidden.isnan().all(1), odd) and torch.equal(r.d_hidden.isnan().any(1), odd)
+        assert r.d_weight.isnan().all()
+    y = SimpleNamespace(**{k: t if k == "weight" else t[~odd] for k, t in vars(x).items()})
+    ref = definition(y.hidden, y.weight, y.target, y.teacher_index, y.teacher_logits, **kw)
+    check(P.LinearLoss(ref.loss, r.token_loss[~odd], r.lse[~odd], None, None), ref, grad=False)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("temperature, alpha", [(1.0, 1.0), (2.0, 1.0), (2.0, 0.5), (0.5, 1.0)])
+@pytest.mark.parametrize("tokens", [3, 70, 300])
+@pytest.mark.parametrize("vocab, first, last", [(65, 64, 65), (300, 64, 128)])
+def test_words_that_are_nan_show_in_every_row(vocab, first, last, tokens, temperature, alpha, grad, dtype):
+    """A whole run of words whose statistics are joined (64, or what the vocabulary's end leaves) is NaN, and neither a
+    label nor a teacher's word is among them."""
+    x = inputs(tokens, 64, vocab, dtype, seed=vocab, topk=5)
+    x.weight[first:last] = math.nan
+    x.target %= 64
+    x.teacher_index %= 64
+    r = distill(x, grad=grad, temperature=temperature, alpha=alpha)
+    assert r.lse.isnan().all() and r.token_loss.isnan().all() and r.loss.isnan()
+    if grad:
+        assert r.d_hidden.isnan().all() and r.d_weight.isnan().all()
