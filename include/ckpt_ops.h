@@ -88,7 +88,9 @@ typedef struct {
     uint64_t d_weight_stride;
 } ckpt_linear_loss_args;
 
-/* Device memory the call works in.  Errors: EINVAL. */
+/* Device memory the call works in, for these sizes, strides and pointers (an
+ * operand's alignment decides whether it is copied).  Errors: EINVAL (sizes,
+ * numbers, strides whose rows lie beyond 64 bits of bytes). */
 ckpt_status ckpt_linear_loss_workspace(const ckpt_linear_loss_args* a, uint64_t* bytes);
 
 /* The loss and, where d_hidden and d_weight are given, its gradients.

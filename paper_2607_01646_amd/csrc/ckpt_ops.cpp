@@ -44,6 +44,15 @@ struct LossPlan {
              d_logits = 0, sum = 0, join = 0, bytes = 0;
 };
 
+// The bytes of a [rows, cols] operand with rows `ld` elements apart; false where 64 bits do not count them.
+bool extent(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t elem, uint64_t* bytes)
+{
+    *bytes = 0;
+    uint64_t last;
+    return rows == 0 || (!__builtin_mul_overflow(rows - 1, ld, &last) && !__builtin_add_overflow(last, cols, &last) &&
+                         !__builtin_mul_overflow(last, elem, bytes));
+}
+
 ckpt_status check_loss(const ckpt_linear_loss_args* a)
 {
     if (!a) return fail_free(CKPT_EINVAL, "null argument");
@@ -66,6 +75,22 @@ ckpt_status check_loss(const ckpt_linear_loss_args* a)
         return fail_free(CKPT_EINVAL, "no targets for the cross entropy");
     if (!a->d_hidden != !a->d_weight && a->tokens)
         return fail_free(CKPT_EINVAL, "both gradients or neither");
+    const uint64_t e = a->dtype == CKPT_TYPE_F32 ? 4 : 2, te = a->teacher_dtype == CKPT_TYPE_F32 ? 4 : 2;
+    const struct {
+        uint64_t rows, cols, ld, elem;
+        const char* what;
+    } each[] = {{a->tokens, a->dim, a->hidden_stride, e, "hidden"},
+                {a->vocab, a->dim, a->weight_stride, e, "weight"},
+                {a->topk ? a->tokens : 0, a->topk, a->teacher_index_stride, 8, "teacher_index"},
+                {a->topk ? a->tokens : 0, a->topk, a->teacher_logits_stride, te, "teacher_logits"},
+                {a->d_hidden ? a->tokens : 0, a->dim, a->d_hidden_stride, e, "d_hidden"},
+                {a->d_weight ? a->vocab : 0, a->dim, a->d_weight_stride, e, "d_weight"}};
+    for (const auto& x : each) {
+        uint64_t bytes;
+        if (!extent(x.rows, x.cols, x.ld, x.elem, &bytes))
+            return fail_free(CKPT_EINVAL, "%s: %llu rows, %llu elements apart, are beyond 64 bits", x.what,
+                             (unsigned long long)x.rows, (unsigned long long)x.ld);
+    }
     return CKPT_OK;
 }
 
@@ -128,12 +153,6 @@ LossPlan plan_loss(const ckpt_linear_loss_args* a)
     return l;
 }
 
-// A [rows, cols] operand with rows `ld` elements apart, in bytes.
-uint64_t extent(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t elem)
-{
-    return rows ? ((rows - 1) * ld + cols) * elem : 0;
-}
-
 // Allocations that this call has met: most of its pointers share a few (a
 // flat buffer's fragments, a caching allocator's segments), and asking the
 // runtime about one takes a microsecond.
@@ -172,7 +191,9 @@ ckpt_status check_given(const Given& g, int device, Known& known)
         return fail_free(CKPT_EINVAL, "%s: rows of %llu elements are %llu apart", g.what, (unsigned long long)g.cols,
                          (unsigned long long)g.ld);
     if (g.ld > (1ull << 40)) return fail_free(CKPT_EINVAL, "%s: a stride of %llu", g.what, (unsigned long long)g.ld);
-    const uint64_t p = (uint64_t)(uintptr_t)g.p, bytes = extent(g.rows, g.cols, g.ld, g.elem);
+    const uint64_t p = (uint64_t)(uintptr_t)g.p;
+    uint64_t bytes;
+    if (!extent(g.rows, g.cols, g.ld, g.elem, &bytes)) return fail_free(CKPT_EINVAL, "%s: too large", g.what);
     if (known.holds(p, bytes)) return CKPT_OK;
     if (ckpt_status st = check_range(g.p, bytes, device, g.what)) return st;
     hipDeviceptr_t base = nullptr;

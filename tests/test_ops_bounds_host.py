@@ -1,0 +1,50 @@
+"""What the training-step operators check and bound on the host, without a GPU
+(CPU only)."""
+import ctypes as C
+
+import pytest
+
+import paper_2607_01646_amd as P
+from paper_2607_01646_amd import ops
+
+
+def need(**kw):
+    """Status and workspace bytes of a call."""
+    a = ops.ckpt_linear_loss_args(dtype=P.CKPT_TYPE_BF16, tokens=8192, dim=4096, vocab=32000, hidden_stride=4096,
+                                  weight_stride=4096, target=256, temperature=1, alpha=1)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    n = C.c_uint64()
+    return ops._ops().ckpt_linear_loss_workspace(C.byref(a), C.byref(n)), n.value
+
+
+TEACHER = dict(topk=4, teacher_dtype=P.CKPT_TYPE_F32, teacher_index_stride=4, teacher_logits_stride=4)
+GRADS = dict(d_hidden=256, d_weight=256, d_hidden_stride=4096, d_weight_stride=4096)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(tokens=(1 << 23) + 1, hidden_stride=1 << 40),  # 2^64 bytes to the last row: its own bytes would be left
+    dict(tokens=(1 << 25) + 1, hidden_stride=1 << 38),
+    dict(tokens=(1 << 22) + 1, hidden_stride=1 << 40, dtype=P.CKPT_TYPE_F32),
+    dict(tokens=(1 << 30) + 1, hidden_stride=(1 << 33) + 1),
+    dict(hidden_stride=1 << 63),
+    dict(weight_stride=1 << 60),
+    dict(tokens=(1 << 21) + 1, **{**TEACHER, "teacher_index_stride": 1 << 40}),
+    dict(tokens=(1 << 22) + 1, **{**TEACHER, "teacher_logits_stride": 1 << 40}),
+    dict(tokens=(1 << 23) + 1, **{**GRADS, "d_hidden_stride": 1 << 40}),
+    dict(**{**GRADS, "d_weight_stride": 1 << 60}),
+])
+def test_strides_that_wrap_are_refused(kw):
+    """Rows so far apart that their distance in bytes does not fit 64 bits: what is left of it must not be taken for the
+    operand's size."""
+    rc, _ = need(**kw)
+    assert rc == P.CKPT_EINVAL and "rows" in P.ckpt_last_error(None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(tokens=(1 << 23) - 1, hidden_stride=1 << 40), dict(tokens=(1 << 31) - 1, hidden_stride=1 << 20),
+    dict(tokens=1, hidden_stride=1 << 63), dict(tokens=0, hidden_stride=1 << 63), dict(vocab=1, weight_stride=1 << 63),
+    dict(vocab=1 << 22, dim=1 << 22, weight_stride=1 << 22), dict(d_hidden_stride=1 << 63, d_weight_stride=1 << 63),
+    dict(teacher_index_stride=1 << 63), dict(**TEACHER, **GRADS)])
+def test_strides_that_do_not_wrap_or_are_not_used_are_not(kw):
+    assert need(**kw)[0] == P.CKPT_OK
