@@ -118,11 +118,30 @@ LossPlan plan_loss(const ckpt_linear_loss_args* a)
     // the tokens multiply them by 0, and 0 * NaN is no 0.
     l.masked_hidden = l.grad && direct(a->hidden, a->hidden_stride); // by the row kernel
     l.copy_hidden = !direct(a->hidden, a->hidden_stride) && !(l.dots && !l.grad); // before the logits
-    // What a token takes in the workspace: its logits and their gradient, its copy, its statistics.
+    // What a token takes in the workspace: its logits and their gradient, its copy, its statistics, its label's logit.
     const uint64_t row = l.vocab_pad * ((l.held && !l.e16 ? 4 : 0) + (l.grad ? 2 * l.dl_planes : 0)) +
-                         (l.copy_hidden || l.masked_hidden ? 2 * l.planes * l.dim_pad : 0) + (l.two_sums ? 12 : 8) * l.parts;
-    const uint64_t most = (a->piece_bytes ? a->piece_bytes : kDefaultPiece) / row / 64 * 64;
-    l.piece = std::min({n, std::max<uint64_t>(256, most), kMostPiece});
+                         (l.copy_hidden || l.masked_hidden ? 2 * l.planes * l.dim_pad : 0) +
+                         (l.two_sums ? 12 : 8) * l.parts + 4;
+    const uint64_t budget = a->piece_bytes ? a->piece_bytes : kDefaultPiece;
+    const auto fit = [&](uint64_t bytes) { // tokens, in whole tiles
+        return std::min({n, std::max<uint64_t>(256, bytes / row / 64 * 64), kMostPiece});
+    };
+    l.piece = fit(budget);
+    if (l.grad && n) {
+        // The sums of d_hidden's runs are held for a piece's tokens too: room for those that all the tokens that fit would
+        // have comes off the piece, at most a quarter of it, and what is left when it is cut bounds them.
+        const auto runs = [&](uint64_t bytes) {
+            return d_hidden_slices((uint32_t)d, (uint32_t)l.piece, (uint32_t)l.vocab_pad, l.planes, l.dl_planes,
+                                   (uint32_t)std::min<uint64_t>(bytes / (4 * l.piece * l.dim_pad), 1u << 20));
+        };
+        const uint64_t most = std::min(kSliceBytes, budget / 4);
+        l.slices = runs(most);
+        const uint64_t sums = l.slices > 1 ? 4 * l.piece * l.dim_pad * l.slices : 0;
+        if (sums && l.piece * row + sums > budget) {
+            l.piece = fit(budget - sums);
+            l.slices = runs(std::min(most, budget - std::min(budget, l.piece * row)));
+        }
+    }
     l.pieces = n ? (uint32_t)((n + l.piece - 1) / l.piece) : 0;
     const uint64_t piece_pad = up(l.piece, 64);
 
@@ -143,11 +162,7 @@ LossPlan plan_loss(const ckpt_linear_loss_args* a)
     if (l.grad) {
         l.d_logits = take(2ull * l.dl_planes * piece_pad * l.vocab_pad);
         if (l.pieces > 1) l.sum = take(4 * v * d);
-        const uint64_t one = 4 * l.piece * l.dim_pad;
-        l.slices = n ? d_hidden_slices((uint32_t)d, (uint32_t)l.piece, (uint32_t)l.vocab_pad, l.planes, l.dl_planes,
-                                       (uint32_t)std::min<uint64_t>(kSliceBytes / one, 1u << 20))
-                     : 1;
-        if (l.slices > 1) l.join = take(one * l.slices);
+        if (l.slices > 1) l.join = take(4 * l.piece * l.dim_pad * l.slices);
     }
     l.bytes = at;
     return l;

@@ -48,3 +48,34 @@ def test_strides_that_wrap_are_refused(kw):
     dict(teacher_index_stride=1 << 63), dict(**TEACHER, **GRADS)])
 def test_strides_that_do_not_wrap_or_are_not_used_are_not(kw):
     assert need(**kw)[0] == P.CKPT_OK
+
+
+def up(x, a):
+    return (x + a - 1) // a * a
+
+
+KINDS = {"ce": {}, "distill": TEACHER, "distill at 2": dict(TEACHER, temperature=2)}
+
+
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("dtype", [P.CKPT_TYPE_BF16, P.CKPT_TYPE_F32])
+@pytest.mark.parametrize("dim, vocab", [(8192, 32000), (2048, 8192), (1024, 32000), (512, 8192), (640, 50304), (4096, 128256),
+                                        (64, 256)])
+@pytest.mark.parametrize("tokens", [300, 2047, 8192, 65536])
+def test_what_is_held_for_the_tokens_is_within_the_piece(tokens, dim, vocab, dtype, kind):
+    """Everything but the head's copy and the sum of its gradient, and a weight a token, is within piece_bytes, or what
+    256 tokens take where that is more (with gradients)."""
+    kw = dict(KINDS[kind], tokens=tokens, dim=dim, vocab=vocab, hidden_stride=dim, weight_stride=dim, dtype=dtype,
+              d_hidden=256, d_weight=256, d_hidden_stride=dim, d_weight_stride=dim)
+    fp32 = dtype == P.CKPT_TYPE_F32
+    planes = 3 if fp32 else 1
+    words = up(vocab, 64)
+    token = 2 * planes * (words + dim) + (0 if kind == "ce" and not fp32 else 4 * words) + 12 * (words // 64) + 4
+    for piece in (1, 1 << 20, 16 << 20, 64 << 20, 256 << 20, 1 << 30, 0):
+        rc, total = need(piece_bytes=piece, **kw)
+        assert rc == P.CKPT_OK
+        head = (6 * vocab * dim if fp32 else 0) + 4 * tokens
+        held = max(piece or 2 << 30, 256 * token)
+        if total - head > held + 16 * 256:  # more than one piece: the head's gradient is summed over them
+            head += 4 * vocab * dim
+        assert total - head <= held + 16 * 256, (piece, total - head, held)
