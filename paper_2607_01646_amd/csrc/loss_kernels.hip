@@ -33,20 +33,22 @@ constexpr float kInf = __builtin_inff();
 __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 __device__ inline uint16_t bf16_of(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
-// An fp32 value as the sum of 3 bf16: each takes the next 8 bits of the
-// significand, cut off, not rounded, so the rests are exact and all 24 bits are
-// kept.  A value that is not finite is its first plane alone (a NaN whose bits
-// would all be cut off keeps one).
+// An fp32 value as the sum of 3 bf16: each rounds what the ones before it leave, which is exact: 24 bits, less 8 and a
+// sign each time.  Rounded and not cut off, so that the second is at most 2^-8 and the third 2^-17 of the leading power of
+// two, of either sign: that is what the products below leave out.  A value whose rounding would be infinite is cut off
+// instead.  One that is not finite is its first plane alone (a NaN whose bits would all be cut off keeps one).
 __device__ inline void split3(float x, uint16_t (&p)[3])
 {
-    const uint32_t u = __float_as_uint(x), a = u & 0xFFFF0000u;
-    const bool finite = (u & 0x7F800000u) != 0x7F800000u, nan = !finite && (u & 0x007FFFFFu) != 0;
-    const float r = x - __uint_as_float(a);
-    const uint32_t b = __float_as_uint(r) & 0xFFFF0000u;
-    const uint32_t c = __float_as_uint(r - __uint_as_float(b));
-    p[0] = (uint16_t)((a >> 16) | (nan ? 0x40 : 0));
-    p[1] = finite ? (uint16_t)(b >> 16) : 0;
-    p[2] = finite ? (uint16_t)(c >> 16) : 0;
+    const uint32_t u = __float_as_uint(x);
+    if ((u & 0x7F800000u) == 0x7F800000u) {
+        p[0] = (uint16_t)((u >> 16) | ((u & 0x007FFFFFu) ? 0x40 : 0));
+        p[1] = p[2] = 0;
+        return;
+    }
+    p[0] = (u & 0x7FFFFFFFu) >= 0x7F7F8000u ? (uint16_t)(u >> 16) : bf16_of(x);
+    const float r = x - __uint_as_float((uint32_t)p[0] << 16);
+    p[1] = bf16_of(r);
+    p[2] = bf16_of(r - __uint_as_float((uint32_t)p[1] << 16));
 }
 
 // ---- tiles of an operand in LDS ----
@@ -365,7 +367,8 @@ __device__ inline uint2 tile_of(uint32_t block, uint32_t np, uint32_t nq)
 // A workgroup of NWP x NWQ waves makes a BP x BQ tile of out[q][p] = sum_k P(p, k) Q(q, k), each wave a part of it in
 // registers.  Two buffers in LDS: while one is multiplied the loads of the next BK values of k write the other one.
 // ZP and ZQ planes an operand.  3 and 3: fp32 operands as 3 bf16 planes; of the 9 products of planes the 6 whose sum of
-// indexes is at most 2 are made (the others are below 2^-24 of the value), smallest first.
+// indexes is at most 2 are made, smallest first.  The others are at most 2 * 2^-8 * 2^-17 + 2^-34 of the value, 2^-24, of
+// either sign (2^-23 within 2^-8 of fp32's largest value).
 template <int ZP_, int ZQ_, bool PA_, bool QA_, int BP_, int BQ_, int NWP_, int NWQ_, int BK_, int BUFS_>
 struct Shape {
     static constexpr int ZP = ZP_, ZQ = ZQ_, BP = BP_, BQ = BQ_, NWP = NWP_, NWQ = NWQ_, BK = BK_, BUFS = BUFS_;

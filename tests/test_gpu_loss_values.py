@@ -1,12 +1,13 @@
-"""The vocabulary head's losses at values that are no numbers, against the
-definition in 64 bits (needs an MI355X; through the C ABI)."""
+"""The vocabulary head's losses at values that are no numbers and at the ends
+of fp32's planes, against the definition in 64 bits (needs an MI355X; through
+the C ABI)."""
 import math
 from types import SimpleNamespace
 
 import pytest
 import torch
 
-from ops_util import check, definition, inputs
+from ops_util import check, definition, inputs, within
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +56,32 @@ def test_words_that_are_nan_show_in_every_row(vocab, first, last, tokens, temper
     assert r.lse.isnan().all() and r.token_loss.isnan().all() and r.loss.isnan()
     if grad:
         assert r.d_hidden.isnan().all() and r.d_weight.isnan().all()
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_fp32_products_drop_no_more_than_they_say(sign):
+    """One product a logit, of values with many ones in their significand, as three bf16 planes each.  The products of
+    planes left out are 2^-24 (1 + 2^-9) of the value at most; the others are added from the smallest, so what their
+    sums round is a unit in the last place of the largest, 2^-23, and 2^-8 of that for the next.  With one word the
+    log-sum-exp is the logit."""
+    g = torch.Generator().manual_seed(0)
+    bits = (0x3F800000 + torch.randint(0, 1 << 23, (300,), generator=g)).int()
+    bits[:8] = torch.tensor([0x3F80FFFF, 0x3F817FFF, 0x3F818000, 0x3F80FF80, 0x3FFFFFFF, 0x3F807F7F, 0x3F80FEFF, 0x3F800001])
+    values = bits.view(F32).cuda()
+    hidden = (sign * values)[:, None]
+    for w in values[:8].tolist():
+        r = P.ckpt_linear_ce(hidden, torch.full((1, 1), w, device="cuda"), torch.zeros(300, dtype=torch.int64, device="cuda"))
+        want = hidden[:, 0].double() * w
+        within(r.lse, want, 4 * 2.0 ** -24 * want.abs(), "logits")
+
+
+def test_fp32_operands_near_the_ends_of_their_range():
+    """Values whose rounding to bf16 would be beyond fp32, and small ones: the same bound (below it a product's smaller
+    planes are no normal numbers)."""
+    most = torch.finfo(F32).max
+    hidden = torch.tensor([most, -most, most * (1 - 2.0 ** -9), 3.39e38, 1e-30, -1e-30, 1.0], device="cuda").repeat(10)[:, None]
+    target = torch.zeros(70, dtype=torch.int64, device="cuda")
+    for w in (0.4999, 2.0 ** -60, 2.0 ** -100 * 1.7):
+        r = P.ckpt_linear_ce(hidden, torch.full((1, 1), w, device="cuda"), target)
+        want = hidden[:, 0].double() * torch.tensor(w, device="cuda").double()
+        within(r.lse, want, 8 * 2.0 ** -24 * want.abs() + 2.0 ** -126, "logits")
