@@ -36,13 +36,18 @@ __device__ inline uint16_t bf16_of(float x) { return __builtin_bit_cast(uint16_t
 // An fp32 value as the sum of 3 bf16: each rounds what the ones before it leave, which is exact: 24 bits, less 8 and a
 // sign each time.  Rounded and not cut off, so that the second is at most 2^-8 and the third 2^-17 of the leading power of
 // two, of either sign: that is what the products below leave out.  A value whose rounding would be infinite is cut off
-// instead.  One that is not finite is its first plane alone (a NaN whose bits would all be cut off keeps one).
+// instead.  An infinity is its third plane alone: that one meets only the other operand's first, so the product is infinity
+// times the value; as a first plane it would meet all three, and a 0 among them gives NaN.  (Where both operands are infinite
+// it is NaN; all logits of such a token are infinite or NaN, and its loss is no number either way.)  A NaN is its first plane
+// (one whose bits would all be cut off keeps one).
 __device__ inline void split3(float x, uint16_t (&p)[3])
 {
     const uint32_t u = __float_as_uint(x);
     if ((u & 0x7F800000u) == 0x7F800000u) {
-        p[0] = (uint16_t)((u >> 16) | ((u & 0x007FFFFFu) ? 0x40 : 0));
-        p[1] = p[2] = 0;
+        const bool nan = (u & 0x007FFFFFu) != 0;
+        p[0] = nan ? (uint16_t)(u >> 16 | 0x40) : 0;
+        p[1] = 0;
+        p[2] = nan ? 0 : (uint16_t)(u >> 16);
         return;
     }
     p[0] = (u & 0x7FFFFFFFu) >= 0x7F7F8000u ? (uint16_t)(u >> 16) : bf16_of(x);

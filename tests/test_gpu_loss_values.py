@@ -58,6 +58,42 @@ def test_words_that_are_nan_show_in_every_row(vocab, first, last, tokens, temper
         assert r.d_hidden.isnan().all() and r.d_weight.isnan().all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("tokens", [3, 24, 25, 70, 300])
+@pytest.mark.parametrize("kind", ["ce", "distill"])
+def test_words_left_out_by_an_infinite_weight(kind, tokens, dtype):
+    """Entries of -inf against a positive coordinate of every hidden state, and of +inf against a negative one: logits of
+    -inf, whatever the type and the number of tokens, and the loss and gradients of the other words."""
+    x = inputs(tokens, 64, 300, dtype, seed=tokens, topk=5)
+    x.hidden[:, 0] = x.hidden[:, 0].abs() + 0.5
+    x.hidden[::2, 0] = 1.0
+    x.hidden[:, 1] = -x.hidden[:, 1].abs() - 0.5
+    out = torch.zeros(300, dtype=torch.bool, device="cuda")
+    out[64:128] = True  # a whole run
+    out[[5, 130, 299]] = True
+    keep = (~out).nonzero().flatten()
+    x.weight[out, 0] = -math.inf
+    x.weight[299, :2] = torch.tensor([0.25, math.inf], device="cuda").to(dtype)
+    y = SimpleNamespace(hidden=x.hidden, weight=x.weight[keep], target=x.target % keep.numel())
+    x.target = keep[y.target]
+    kw = dict(temperature=2.0, alpha=0.5) if kind == "distill" else {}
+    if kind == "distill":
+        y.teacher_index, y.teacher_logits = x.teacher_index % keep.numel(), x.teacher_logits
+        x.teacher_index = keep[y.teacher_index]
+        ref = definition(y.hidden, y.weight, y.target, y.teacher_index, y.teacher_logits, **kw)
+        call = lambda grad: distill(x, grad=grad, **kw)  # noqa: E731
+    else:
+        ref = definition(y.hidden, y.weight, y.target)
+        call = lambda grad: P.ckpt_linear_ce(x.hidden, x.weight, x.target, grad=grad)  # noqa: E731
+    check(call(False), ref, grad=False)
+    r = call(True)
+    check(r, ref, grad=False)
+    # 0 times the infinite entries: coordinates 0 and 1 of d_hidden are NaN by the formula
+    within(r.d_hidden[:, 2:], ref.d_hidden[:, 2:], ref.b_d_hidden[:, 2:], "d_hidden")
+    within(r.d_weight[keep], ref.d_weight, ref.b_d_weight, "d_weight")
+    assert not r.d_weight[out].any()
+
+
 @pytest.mark.parametrize("sign", [1, -1])
 def test_fp32_products_drop_no_more_than_they_say(sign):
     """One product a logit, of values with many ones in their significand, as three bf16 planes each.  The products of
