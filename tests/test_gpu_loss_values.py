@@ -1,6 +1,6 @@
-"""The vocabulary head's losses at values that are no numbers and at the ends
-of fp32's planes, against the definition in 64 bits (needs an MI355X; through
-the C ABI)."""
+"""The vocabulary head's losses at values that are no numbers, at the ends of
+fp32's planes and over large vocabularies, against the definition in 64 bits
+(needs an MI355X; through the C ABI)."""
 import math
 from types import SimpleNamespace
 
@@ -121,3 +121,30 @@ def test_fp32_operands_near_the_ends_of_their_range():
         r = P.ckpt_linear_ce(hidden, torch.full((1, 1), w, device="cuda"), target)
         want = hidden[:, 0].double() * torch.tensor(w, device="cuda").double()
         within(r.lse, want, 8 * 2.0 ** -24 * want.abs() + 2.0 ** -126, "logits")
+
+
+# More than the statistics that a row's workgroup keeps in registers (512 runs of 64 words), and more than it keeps
+# factors of (8192): the words of the runs behind those are the likely ones.
+@pytest.mark.parametrize("tokens, dim, vocab", [(300, 64, 32769), (300, 64, 50301), (70, 64, 50301), (260, 64, 524289)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_large_vocabularies(tokens, dim, vocab, dtype):
+    if dtype == F32 and vocab > 60000:
+        pytest.skip("the number of words changes nothing more in fp32")
+    x = inputs(tokens, dim, vocab, dtype, seed=vocab, masked=0.1)
+    x.weight[32768:] *= 8 if vocab > 32769 else 30
+    x.weight[524288:] *= 4
+    ref = definition(x.hidden, x.weight, x.target)
+    tail = (ref.lse - torch.logsumexp(x.hidden.double() @ x.weight[:32768].double().t(), 1))[ref.lse != 0]
+    assert (tail > 1).sum() > tail.numel() // 4  # they matter
+    check(P.ckpt_linear_ce(x.hidden, x.weight, x.target, grad=True), ref)
+
+
+@pytest.mark.parametrize("tokens", [70, 300])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_distillation_over_a_large_vocabulary(tokens, dtype):
+    x = inputs(tokens, 64, 50301, dtype, seed=7, topk=9, masked=0.1)
+    x.weight[32768:] *= 8
+    kw = dict(temperature=2.0, alpha=0.5)
+    ref = definition(x.hidden, x.weight, x.target, x.teacher_index, x.teacher_logits, **kw)
+    check(distill(x, grad=True, **kw), ref)
+    check(distill(x, **kw), ref, grad=False)
