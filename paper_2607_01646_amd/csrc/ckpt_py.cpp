@@ -286,7 +286,9 @@ PyObject* linear_loss(PyObject*, PyObject* const* args, Py_ssize_t n_args)
         for (const auto& x : each) {
             if (x.o == Py_None) continue;
             const at::Tensor* t = plain(x.o);
-            if (!t || t->scalar_type() != x.type || (uint64_t)t->numel() != a.tokens || !t->is_contiguous()) Py_RETURN_NONE;
+            if (!t || t->scalar_type() != x.type || (uint64_t)t->numel() != a.tokens || !t->is_contiguous() ||
+                (t->dim() != 1 && t->sizes() != shape))
+                Py_RETURN_NONE;
             *x.to = a.tokens ? t->data_ptr() : nullptr;
         }
         if (args[5] != Py_None) {

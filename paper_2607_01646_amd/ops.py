@@ -147,6 +147,14 @@ def _plain(t, what, dtype, n):
     return t.data_ptr() if n else None
 
 
+def _each_token(t, what, dtype, shape):
+    """A value for each token: of the tokens' shape, or flat.  Another shape of as many values may be another order."""
+    p = _plain(t, what, dtype, shape.numel())
+    if t.dim() != 1 and [k for k in t.shape if k != 1] != [k for k in shape if k != 1]:
+        raise ValueError("%s %s for tokens %s" % (what, tuple(t.shape), tuple(shape)))
+    return p
+
+
 def _linear_loss(hidden, weight, target, teacher, temperature, alpha, token_weight, ignore_index, reduction, grad,
                  grad_scale, piece_bytes, stream):
     native, at = _native or _module()
@@ -178,10 +186,10 @@ def _linear_loss(hidden, weight, target, teacher, temperature, alpha, token_weig
     a.vocab, _, a.weight_stride = _rows(weight, "weight")
     a.hidden, a.weight = hidden.data_ptr(), weight.data_ptr()
     if target is not None:
-        a.target = _plain(target, "target", torch.int64, n)
+        a.target = _each_token(target, "target", torch.int64, shape)
     a.ignore_index = ignore_index
     if token_weight is not None:
-        a.token_weight = _plain(token_weight, "token_weight", torch.float32, n)
+        a.token_weight = _each_token(token_weight, "token_weight", torch.float32, shape)
     a.temperature, a.alpha = temperature, alpha
     if teacher is not None:
         index, logits = teacher
