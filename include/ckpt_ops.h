@@ -74,7 +74,7 @@ typedef struct {
     uint64_t teacher_index_stride;
     const void* teacher_logits; /* [tokens, topk] */
     uint64_t teacher_logits_stride;
-    float temperature, alpha; /* T > 0, alpha in [0, 1] */
+    float temperature, alpha; /* T > 0, 1/T and T^2 within fp32; alpha in [0, 1] */
     const float* grad_scale;  /* device scalar or NULL (1) */
     uint64_t piece_bytes;     /* bound on what is held for the tokens at a time (their logits most of all), at
                                  least 256 tokens'; 0 = 2 GiB */

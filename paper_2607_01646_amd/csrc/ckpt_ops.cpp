@@ -65,8 +65,9 @@ ckpt_status check_loss(const ckpt_linear_loss_args* a)
                          (unsigned long long)a->tokens, (unsigned long long)a->dim, (unsigned long long)a->vocab);
     if (a->topk > 1024) return fail_free(CKPT_EINVAL, "%u teacher entries: at most 1024", a->topk);
     if (a->topk) {
-        if (!(a->temperature > 0) || !std::isfinite(a->temperature))
-            return fail_free(CKPT_EINVAL, "temperature %g", (double)a->temperature);
+        // The kernels multiply by 1 / T, and by T twice.
+        if (!(a->temperature > 0) || !std::isfinite(1 / a->temperature) || !std::isfinite(a->temperature * a->temperature))
+            return fail_free(CKPT_EINVAL, "temperature %g: its inverse and its square are fp32 numbers", (double)a->temperature);
         if (!(a->alpha >= 0 && a->alpha <= 1)) return fail_free(CKPT_EINVAL, "alpha %g is not in [0, 1]", (double)a->alpha);
         if (a->teacher_dtype != CKPT_TYPE_BF16 && a->teacher_dtype != CKPT_TYPE_F32)
             return fail_free(CKPT_EINVAL, "teacher logits are bf16 or fp32, not type %u", a->teacher_dtype);

@@ -79,3 +79,14 @@ def test_what_is_held_for_the_tokens_is_within_the_piece(tokens, dim, vocab, dty
         if total - head > held + 16 * 256:  # more than one piece: the head's gradient is summed over them
             head += 4 * vocab * dim
         assert total - head <= held + 16 * 256, (piece, total - head, held)
+
+
+@pytest.mark.parametrize("temperature", [1e-39, 2.9e-39, 1e-45, 1.9e19, 1e30, 3.4e38])
+def test_temperatures_whose_inverse_or_square_is_infinite_are_refused(temperature):
+    """0 times an infinite 1/T, or an infinite T^2 times 0, would make a finite row NaN."""
+    assert need(**dict(TEACHER, temperature=temperature))[0] == P.CKPT_EINVAL
+
+
+@pytest.mark.parametrize("temperature", [3e-39, 1e-30, 0.01, 1.0, 1e4, 1.8e19])
+def test_other_temperatures_are_not(temperature):
+    assert need(**dict(TEACHER, temperature=temperature))[0] == P.CKPT_OK
