@@ -17,6 +17,10 @@ import torch
 
 from .ckpt import CKPT_OK, CkptError, _native_module, ckpt_tensor, lib, tensor_bytes
 
+__all__ = ["CKPT_GRAD_NORM_SCRATCH", "CKPT_LOSS_MEAN", "CKPT_LOSS_SUM", "CKPT_TYPE_BF16", "CKPT_TYPE_F32", "LinearLoss",
+           "ckpt_adamw", "ckpt_adamw_fragment", "ckpt_grad_norm", "ckpt_linear_ce", "ckpt_linear_distill",
+           "ckpt_linear_loss_args"]
+
 CKPT_TYPE_BF16 = 1
 CKPT_TYPE_F32 = 2
 CKPT_LOSS_MEAN = 0

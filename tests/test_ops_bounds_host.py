@@ -90,3 +90,12 @@ def test_temperatures_whose_inverse_or_square_is_infinite_are_refused(temperatur
 @pytest.mark.parametrize("temperature", [3e-39, 1e-30, 0.01, 1.0, 1e4, 1.8e19])
 def test_other_temperatures_are_not(temperature):
     assert need(**dict(TEACHER, temperature=temperature))[0] == P.CKPT_OK
+
+
+def test_the_package_takes_the_operators_names_and_no_others():
+    """What ops.py imports for itself (typing, contextlib) is not the package's."""
+    assert not any(hasattr(P, name) for name in ("NamedTuple", "Optional", "contextlib"))
+    assert all(hasattr(P, name) for name in ops.__all__)
+    public = {k for k, x in vars(ops).items() if k.startswith(("ckpt_", "CKPT_")) and getattr(x, "__module__", ops.__name__) == ops.__name__}
+    from paper_2607_01646_amd import ckpt
+    assert public - set(vars(ckpt)) <= set(ops.__all__)
