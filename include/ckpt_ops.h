@@ -15,9 +15,10 @@
  * thrown, and ckpt_last_error(NULL) for the text of this thread's last
  * failure.  A call enqueues its work on `stream` and returns without waiting;
  * it allocates nothing, keeps nothing between calls, and records no memset or
- * copy node (it may be captured into a HIP graph).  Device pointers are
- * checked on the host against their allocations; what device memory holds
- * (targets, indices) is not.
+ * copy node (it may be captured into a HIP graph).  What its pointers name has
+ * to stay until that work has run.  Device pointers are checked on the host
+ * against their allocations; what device memory holds (targets, indices) is
+ * not.
  */
 #ifndef CKPT_OPS_H
 #define CKPT_OPS_H
@@ -40,17 +41,18 @@ extern "C" {
  * The logits l = hidden weight^T are never held for more than one piece of the
  * tokens; the cross entropy without gradients holds none.  With w the token weight, lse = log sum_v exp l_v and y the target:
  *   ce_n   = lse_n - l_n,y
- * and, with topk > 0, from a teacher's logits t_k at the words i_k:
+ * and, with topk > 0 and alpha > 0, from a teacher's logits t_k at the words i_k:
  *   q      = softmax of t / T over the row's entries
  *   kd_n   = T^2 sum_k q_k (log q_k - l_n,i_k / T + lse^T_n),  lse^T = log sum_v exp(l_v / T)
  *   loss_n = alpha kd_n + (1 - alpha) ce_n
- * (loss_n = ce_n with topk == 0).  The loss is sum_n w_n loss_n, divided by
+ * (loss_n = ce_n with topk == 0 or alpha == 0: the teacher's entries are then
+ * not read).  The loss is sum_n w_n loss_n, divided by
  * the sum of w_n over the rows that count for CKPT_LOSS_MEAN (0 where none
  * does).  The gradients are those of grad_scale * loss.
  *
  * Which rows count: one whose target is not ignore_index (where the cross
- * entropy has a share: topk == 0 or alpha < 1), or that has a teacher entry;
- * never one of weight 0.  Rows that do not count are not read: whatever
+ * entropy has a share: topk == 0 or alpha < 1), or that has a teacher entry
+ * (where the teacher has one: topk > 0 and alpha > 0); never one of weight 0.  Rows that do not count are not read: whatever
  * `hidden` holds there, NaN included, their loss, log-sum-exp and gradient
  * are 0.  A target outside [0, vocab) other than ignore_index, or a teacher
  * index >= vocab, makes the row's loss and gradient NaN.  A teacher index below 0 marks an
@@ -76,12 +78,14 @@ typedef struct {
     uint64_t teacher_logits_stride;
     float temperature, alpha; /* T > 0, 1/T and T^2 within fp32; alpha in [0, 1] */
     const float* grad_scale;  /* device scalar or NULL (1) */
-    uint64_t piece_bytes;     /* bound on what is held for the tokens at a time (their logits most of all), at
-                                 least 256 tokens'; 0 = 2 GiB */
+    uint64_t piece_bytes;     /* bound on what is held for the tokens at a time: their logits and the logits'
+                                 gradient, their copy and statistics, the sums of d_hidden where it is cut; at least
+                                 what 256 tokens take without the last; 0 = 2 GiB.  Not in it: 4 bytes a token, copies
+                                 of weight, the running d_weight of several pieces */
     /* outputs */
     float* loss;       /* scalar */
     float* token_loss; /* [tokens] loss_n, before the weight */
-    float* lse;        /* [tokens] lse (topk > 0: lse^T) */
+    float* lse;        /* [tokens] lse (topk > 0 and alpha > 0: lse^T) */
     void* d_hidden;    /* [tokens, dim]; both gradients or neither (NULL) */
     uint64_t d_hidden_stride;
     void* d_weight; /* [vocab, dim] */

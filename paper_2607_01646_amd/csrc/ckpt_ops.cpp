@@ -15,8 +15,8 @@ constexpr uint64_t kMost = 0x7fffffffull;  // tokens
 constexpr uint64_t kMostWidth = 1ull << 22; // dim, vocab: a tile's rows of an operand stay within 31 bits of bytes
 constexpr uint64_t kDefaultPiece = 2ull << 30;
 constexpr uint64_t kMostPiece = 1ull << 22; // tokens: a workgroup a row stays below 2^32 lanes
-// For so few tokens d_logits has a second bf16 plane: the products are bound by the weight's bytes, and the gradients
-// of few terms have no others to average their rounding with.
+// For so few tokens d_logits has a second bf16 plane: gradients of few terms have no others to average their rounding
+// with.  It doubles the gradients' products, in smaller tiles (256 x 4096 x 32000 0.45 ms; 512 tokens with one plane 0.49).
 constexpr uint64_t kFewTokens = 256;
 // So few tokens' weights are summed again by each workgroup that needs the sum.
 constexpr uint64_t kFewSums = 1024;

@@ -2,7 +2,7 @@
 // norm and AdamW over a rank's fragments.
 //
 // Both are bound by HBM: AdamW moves 28 bytes a parameter (bf16 parameter and
-// gradient; 36 in full precision) for some 60 instructions, the norm 2 or 4.
+// gradient; 32 in full precision) for some 60 instructions, the norm 2 or 4.
 // A launch takes the fragments of up to 64 (the norm: 160) parameters as
 // kernel arguments, so nothing is allocated or copied for a table; a workgroup
 // finds the fragment of its tile with one load per lane and a ballot.

@@ -1,7 +1,11 @@
 """Python binding of the training-step operators (include/ckpt_ops.h): the
 vocabulary head's losses with their gradients, and the clipped AdamW step over
-a rank's fragments.  Argument marshalling only, as in `ckpt`; workspaces come
-from torch's caching allocator, on the stream that the work runs on.
+a rank's fragments.  Argument marshalling only, as in `ckpt`; workspaces and
+results come from torch's caching allocator, on the stream that the work runs
+on.  With `stream` the allocator does not learn that the call's tensors are
+used there: inputs have to be ready for that stream and to live until its work
+has run, and results are another stream's only behind it (`wait_stream`,
+`record_stream`), as for any work on a stream of its own.
 
     r = ckpt_linear_ce(hidden, lm_head, targets, grad=True)
     hidden.backward(r.d_hidden)                      # the rest of the model
@@ -51,7 +55,7 @@ class ckpt_adamw_fragment(C.Structure):
 class LinearLoss(NamedTuple):
     loss: torch.Tensor  # scalar, fp32
     token_loss: torch.Tensor  # fp32, the tokens' shape; 0 where a token does not count
-    lse: torch.Tensor  # fp32 log-sum-exp (distillation: at the temperature)
+    lse: torch.Tensor  # fp32 log-sum-exp (distillation, alpha > 0: at the temperature)
     d_hidden: Optional[torch.Tensor]
     d_weight: Optional[torch.Tensor]
 
@@ -232,7 +236,8 @@ def ckpt_linear_ce(hidden, weight, target, token_weight=None, ignore_index=-100,
                    grad_scale=None, piece_bytes=0, stream=None):
     """Softmax cross entropy of hidden [..., dim] weight^T [vocab, dim]
     against target [...] (int64), without holding the logits of more tokens
-    than piece_bytes allows (0 = 2 GiB).  bf16 or fp32.  grad: also d_hidden
+    than piece_bytes allows (0 = 2 GiB).  target and token_weight (fp32) have
+    the tokens' shape or are flat.  bf16 or fp32.  grad: also d_hidden
     and d_weight, of grad_scale (a device scalar; None = 1) times the loss.
     A token counts unless its target is ignore_index or its token_weight 0;
     hidden is not read where it does not."""
@@ -247,7 +252,8 @@ def ckpt_linear_distill(hidden, weight, teacher_index, teacher_logits, target=No
     (1 - alpha) cross entropy, q the softmax of teacher_logits [..., topk] / T
     over the words teacher_index [..., topk] (int64; below 0 = absent), p^T
     the student's over the whole vocabulary.  target is needed where alpha <
-    1.  The other arguments are ckpt_linear_ce's."""
+    1; lse is that of p^T (alpha = 0: as ckpt_linear_ce's, which the call then
+    is).  The other arguments are ckpt_linear_ce's."""
     return _linear_loss(hidden, weight, target, (teacher_index, teacher_logits), temperature, alpha, token_weight,
                         ignore_index, reduction, grad, grad_scale, piece_bytes, stream)
 
