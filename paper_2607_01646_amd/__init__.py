@@ -11,5 +11,7 @@ analytic models and replica placement are in `disruption` and `placement`.
 """
 from .ckpt import *  # noqa: F401,F403
 from .ckpt import Checkpointer, CkptError, Peer, PeerError, lib  # noqa: F401
+from .muon import *  # noqa: F401,F403
+from .muon import ckpt_muon, ckpt_orthogonalize  # noqa: F401
 from .ops import *  # noqa: F401,F403
 from .ops import LinearLoss, ckpt_adamw, ckpt_grad_norm, ckpt_linear_ce, ckpt_linear_distill  # noqa: F401

@@ -1,0 +1,341 @@
+// ckpt_muon.cpp -- entry points of the orthogonalised optimizer step
+// (include/ckpt_muon.h): argument checks, groups of matrices that the
+// workspace holds, the order of launches.  Nothing is allocated but lists on
+// the host, and nothing outlives a call.
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "../../include/ckpt_muon.h"
+#include "ops_host.h"
+#include "ops_internal.h"
+
+namespace ckpt {
+namespace {
+
+constexpr uint64_t kDefaultPiece = 2ull << 30;
+
+ckpt_status check_ns(const ckpt_newton_schulz& ns)
+{
+    if (ns.steps < 1 || ns.steps > 64) return fail_free(CKPT_EINVAL, "%u steps: 1 to 64", ns.steps);
+    if (ns.reserved) return fail_free(CKPT_EINVAL, "reserved is not 0");
+    if (!(ns.eps >= 1e-30 && ns.eps <= 1)) return fail_free(CKPT_EINVAL, "eps %g is not in [1e-30, 1]", ns.eps);
+    // Singular values begin in [0, 1].  The operands' scale has room for 16, and the polynomial's coefficient of a value for 15.
+    constexpr int kGrid = 512;
+    bool fine = std::isfinite(ns.a) && std::isfinite(ns.b) && std::isfinite(ns.c);
+    for (int k = 0; fine && k <= kGrid; ++k) {
+        double x = (double)k / kGrid;
+        for (uint32_t i = 0; fine && i < ns.steps; ++i) {
+            const double s = x * x, factor = ns.a + s * (ns.b + s * ns.c);
+            x *= factor;
+            fine = std::fabs(x) <= 2 && std::fabs(factor) <= 8;
+        }
+    }
+    if (!fine)
+        return fail_free(CKPT_EINVAL, "the polynomial %g x + %g x^3 + %g x^5 leaves [-2, 2], or multiplies a value by more than 8",
+                         ns.a, ns.b, ns.c);
+    return CKPT_OK;
+}
+
+// A matrix of the call, whichever entry point it is of.
+struct Job {
+    MuonMatrix m;
+    uint64_t s, l;
+    uint64_t x, y, a, b, part; // offsets in the workspace
+};
+
+// Lays the operands of a matrix out from `at` on; false where 64 bits do not count them.
+bool lay_out(Job& j, uint64_t rows, uint64_t cols, uint64_t& at)
+{
+    j.s = std::min(rows, cols);
+    j.l = std::max(rows, cols);
+    const uint64_t x = up(4 * j.s * up(j.l, 64), 256), a = up(4 * j.s * up(j.s, 64), 256); // at most 2^46 each
+    const uint64_t tiles = ((rows + kMuonRows - 1) / kMuonRows) * ((cols + kMuonCols - 1) / kMuonCols);
+    j.x = at;
+    j.y = j.x + x;
+    j.a = j.y + x;
+    j.b = j.a + a;
+    j.part = j.b + a;
+    at = j.part + up(8 * tiles, 256);
+    j.m.rows = (uint32_t)rows;
+    j.m.cols = (uint32_t)cols;
+    j.m.part_n = (uint32_t)tiles;
+    return tiles <= (1u << 23);
+}
+
+// Cuts the matrices into groups: calls `run(first, last)` for each, and finds the bytes that the largest takes.
+template <class F>
+ckpt_status grouped(std::vector<Job>& jobs, uint64_t piece_bytes, uint64_t* most, F run)
+{
+    const uint64_t budget = piece_bytes ? piece_bytes : kDefaultPiece;
+    *most = 0;
+    for (size_t i = 0; i < jobs.size();) {
+        uint64_t at = 0, tiles = 0;
+        size_t k = i;
+        for (; k < jobs.size() && k - i < kMuonMats; ++k) {
+            uint64_t next = at;
+            Job j = jobs[k];
+            if (!lay_out(j, j.m.rows, j.m.cols, next))
+                return fail_free(CKPT_EINVAL, "matrix of %u x %u: too many elements", j.m.rows, j.m.cols);
+            tiles += std::max<uint64_t>(j.m.part_n, (j.s + 63) / 64 * ((j.l + 63) / 64)); // of any launch, at most
+            if (k > i && (next > budget || tiles > (1u << 23))) break;
+            if (tiles > (1u << 23)) return fail_free(CKPT_EINVAL, "matrix of %u x %u: too many elements", j.m.rows, j.m.cols);
+            jobs[k] = j;
+            at = next;
+        }
+        *most = std::max(*most, at);
+        if (ckpt_status st = run(i, k)) return st;
+        i = k;
+    }
+    return CKPT_OK;
+}
+
+ckpt_status nothing(size_t, size_t) { return CKPT_OK; }
+
+ckpt_status sizes(uint64_t rows, uint64_t cols, uint32_t i)
+{
+    if (rows > kMostWidth || cols > kMostWidth)
+        return fail_free(CKPT_EINVAL, "matrix %u: %llu x %llu: at most 2^22 each", i, (unsigned long long)rows,
+                         (unsigned long long)cols);
+    return CKPT_OK;
+}
+
+void add_job(std::vector<Job>& jobs, uint64_t rows, uint64_t cols)
+{
+    Job j = {};
+    j.m.rows = (uint32_t)rows;
+    j.m.cols = (uint32_t)cols;
+    jobs.push_back(j);
+}
+
+// The launches of all groups.  `a`: what they share.
+ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schulz& ns, void* workspace,
+                    uint64_t workspace_bytes, hipStream_t s)
+{
+    uint64_t need = 0;
+    if (ckpt_status st = grouped(jobs, ns.piece_bytes, &need, nothing)) return st;
+    if (need > workspace_bytes)
+        return fail_free(CKPT_EINVAL, "workspace of %llu bytes needs %llu", (unsigned long long)workspace_bytes,
+                         (unsigned long long)need);
+    a.ca = (float)ns.a;
+    a.cb = (float)ns.b;
+    a.cc = (float)ns.c;
+    a.eps = ns.eps;
+    const uint64_t w = (uint64_t)(uintptr_t)workspace;
+    return grouped(jobs, ns.piece_bytes, &need, [&](size_t first, size_t last) {
+        a.count = (uint32_t)(last - first);
+        for (size_t k = first; k < last; ++k) {
+            MuonMatrix& m = a.m[k - first] = jobs[k].m;
+            m.x = w + jobs[k].x;
+            m.y = w + jobs[k].y;
+            m.a = w + jobs[k].a;
+            m.b = w + jobs[k].b;
+            m.part = w + jobs[k].part;
+        }
+        hipError_t err = launch_muon_first(a, s);
+        if (err == hipSuccess) err = launch_muon_pack(a, s);
+        for (uint32_t step = 0; step < ns.steps && err == hipSuccess; ++step) {
+            err = launch_muon_gram(a, false, s);
+            if (err == hipSuccess) err = launch_muon_gram(a, true, s);
+            if (err == hipSuccess) err = launch_muon_apply(a, step + 1 == ns.steps, s);
+            for (uint32_t k = 0; k < a.count; ++k) std::swap(a.m[k].x, a.m[k].y);
+        }
+        return err == hipSuccess ? CKPT_OK : fail_free(CKPT_EHIP, "orthogonalisation: %s", hipGetErrorString(err));
+    });
+}
+
+struct Span {
+    uint64_t lo, hi;
+    bool written;
+};
+
+// Whether something written lies where something else does.
+bool overlap(std::vector<Span>& spans)
+{
+    std::sort(spans.begin(), spans.end(), [](const Span& x, const Span& y) { return x.lo < y.lo; });
+    uint64_t any = 0, written = 0;
+    for (const Span& x : spans) {
+        if (x.lo < (x.written ? any : written)) return true;
+        any = std::max(any, x.hi);
+        if (x.written) written = std::max(written, x.hi);
+    }
+    return false;
+}
+
+ckpt_status check_workspace(void* workspace, uint64_t bytes, int device, Known& known)
+{
+    if (!workspace || (uintptr_t)workspace % 256) return fail_free(CKPT_EINVAL, "workspace: null or not 256-byte aligned");
+    return check_given({workspace, 1, bytes, bytes, 1, "workspace"}, device, known);
+}
+
+ckpt_status orthogonalize_jobs(const ckpt_matrix* m, uint32_t n, const ckpt_newton_schulz* ns, std::vector<Job>& jobs)
+{
+    if (!ns || (n && !m)) return fail_free(CKPT_EINVAL, "null argument");
+    if (ckpt_status st = check_ns(*ns)) return st;
+    for (uint32_t i = 0; i < n; ++i) {
+        if (ckpt_status st = sizes(m[i].rows, m[i].cols, i)) return st;
+        if (m[i].rows && m[i].cols) add_job(jobs, m[i].rows, m[i].cols);
+    }
+    return CKPT_OK;
+}
+
+ckpt_status muon_jobs(const ckpt_muon_matrix* m, uint32_t n, const ckpt_muon_args* args, std::vector<Job>& jobs)
+{
+    if (!args || (n && !m)) return fail_free(CKPT_EINVAL, "null argument");
+    uint64_t e;
+    if (!type_bytes(args->param_dtype, &e) || !type_bytes(args->grad_dtype, &e))
+        return fail_free(CKPT_EINVAL, "parameters and gradients are bf16 or fp32, not types %u and %u", args->param_dtype,
+                         args->grad_dtype);
+    if (args->nesterov > 1 || args->reserved) return fail_free(CKPT_EINVAL, "nesterov is 0 or 1, reserved 0");
+    if (!(args->momentum >= 0 && args->momentum < 1)) return fail_free(CKPT_EINVAL, "momentum %g is not in [0, 1)", args->momentum);
+    if (!std::isfinite(args->lr) || !std::isfinite(args->weight_decay))
+        return fail_free(CKPT_EINVAL, "lr %g, weight_decay %g", args->lr, args->weight_decay);
+    if (ckpt_status st = check_ns(args->ns)) return st;
+    for (uint32_t i = 0; i < n; ++i) {
+        if (ckpt_status st = sizes(m[i].rows, m[i].cols, i)) return st;
+        if (!std::isfinite(m[i].scale)) return fail_free(CKPT_EINVAL, "matrix %u: scale %g", i, m[i].scale);
+        if (m[i].rows && m[i].cols) add_job(jobs, m[i].rows, m[i].cols);
+    }
+    return CKPT_OK;
+}
+
+// Nothing is thrown past an entry point.
+template <class F>
+ckpt_status guarded(F f)
+{
+    clear_free_error();
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        return fail_free(CKPT_EINVAL, "no host memory for the list of matrices");
+    }
+}
+
+} // namespace
+} // namespace ckpt
+
+using namespace ckpt;
+
+extern "C" ckpt_status ckpt_orthogonalize_workspace(const ckpt_matrix* m, uint32_t n, const ckpt_newton_schulz* ns,
+                                                    uint64_t* bytes)
+{
+    return guarded([&]() -> ckpt_status {
+        std::vector<Job> jobs;
+        if (!bytes) return fail_free(CKPT_EINVAL, "null argument");
+        if (ckpt_status st = orthogonalize_jobs(m, n, ns, jobs)) return st;
+        return grouped(jobs, ns->piece_bytes, bytes, nothing);
+    });
+}
+
+extern "C" ckpt_status ckpt_orthogonalize(const ckpt_matrix* m, uint32_t n, uint32_t dtype, const ckpt_newton_schulz* ns,
+                                          int32_t device, void* workspace, uint64_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> ckpt_status {
+        std::vector<Job> jobs;
+        uint64_t e = 0;
+        if (!type_bytes(dtype, &e)) return fail_free(CKPT_EINVAL, "matrices are bf16 or fp32, not type %u", dtype);
+        if (ckpt_status st = orthogonalize_jobs(m, n, ns, jobs)) return st;
+        DeviceGuard dg;
+        if (ckpt_status st = enter_device(device, dg)) return st;
+        Known known;
+        std::vector<Span> spans;
+        size_t at = 0;
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint64_t rows = m[i].rows, cols = m[i].cols;
+            if (!rows || !cols) continue;
+            char what[48];
+            snprintf(what, sizeof what, "matrix %u", i);
+            if (ckpt_status st = check_given({m[i].in, rows, cols, m[i].in_stride, e, what}, device, known)) return st;
+            snprintf(what, sizeof what, "matrix %u, its result", i);
+            if (ckpt_status st = check_given({m[i].out, rows, cols, m[i].out_stride, e, what}, device, known)) return st;
+            const auto span = [&](const void* p, uint64_t ld, bool written) {
+                if (rows > 1 && ld != cols) return; // rows of others may lie between them
+                spans.push_back({(uint64_t)(uintptr_t)p, (uint64_t)(uintptr_t)p + rows * cols * e, written});
+            };
+            span(m[i].out, m[i].out_stride, true);
+            if (m[i].in != m[i].out || (rows > 1 && m[i].in_stride != m[i].out_stride)) span(m[i].in, m[i].in_stride, false);
+            MuonMatrix& to = jobs[at++].m;
+            to.in = (uint64_t)(uintptr_t)m[i].in;
+            to.in_ld = m[i].in_stride;
+            to.out = (uint64_t)(uintptr_t)m[i].out;
+            to.out_ld = m[i].out_stride;
+        }
+        if (jobs.empty()) return CKPT_OK;
+        if (overlap(spans)) return fail_free(CKPT_EINVAL, "a result overlaps another matrix");
+        if (ckpt_status st = check_workspace(workspace, workspace_bytes, device, known)) return st;
+        MuonArgs a = {};
+        a.in_f32 = a.out_f32 = e == 4;
+        return run_all(jobs, a, *ns, workspace, workspace_bytes, (hipStream_t)stream);
+    });
+}
+
+extern "C" ckpt_status ckpt_muon_workspace(const ckpt_muon_matrix* m, uint32_t n, const ckpt_muon_args* args, uint64_t* bytes)
+{
+    return guarded([&]() -> ckpt_status {
+        std::vector<Job> jobs;
+        if (!bytes) return fail_free(CKPT_EINVAL, "null argument");
+        if (ckpt_status st = muon_jobs(m, n, args, jobs)) return st;
+        return grouped(jobs, args->ns.piece_bytes, bytes, nothing);
+    });
+}
+
+extern "C" ckpt_status ckpt_muon(const ckpt_muon_matrix* m, uint32_t n, const ckpt_muon_args* args, int32_t device,
+                                 void* workspace, uint64_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> ckpt_status {
+        std::vector<Job> jobs;
+        if (ckpt_status st = muon_jobs(m, n, args, jobs)) return st;
+        uint64_t pe = 0, ge = 0;
+        type_bytes(args->param_dtype, &pe);
+        type_bytes(args->grad_dtype, &ge);
+        DeviceGuard dg;
+        if (ckpt_status st = enter_device(device, dg)) return st;
+        Known known;
+        if (args->grad_scale)
+            if (ckpt_status st = check_given({args->grad_scale, 1, 1, 1, 4, "grad_scale"}, device, known)) return st;
+        std::vector<Span> spans;
+        size_t at = 0;
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint64_t all = m[i].rows * m[i].cols;
+            if (!all) continue;
+            const struct {
+                const void* p;
+                uint64_t e;
+                bool written;
+                const char* name;
+            } part[] = {{m[i].param, pe, true, "param"}, {m[i].master, 4, true, "master"},
+                        {m[i].momentum, 4, true, "momentum"}, {m[i].grad, ge, false, "grad"}};
+            for (const auto& x : part) {
+                const uint64_t p = (uint64_t)(uintptr_t)x.p;
+                if (p % x.e || !known.holds(p, all * x.e)) {
+                    char what[48];
+                    snprintf(what, sizeof what, "matrix %u, %s", i, x.name);
+                    if (ckpt_status st = check_given({x.p, 1, all, all, x.e, what}, device, known)) return st;
+                }
+                // A parameter in full precision may be its own master copy.
+                if (&x == part && m[i].param == (void*)m[i].master && pe == 4) continue;
+                spans.push_back({p, p + all * x.e, x.written});
+            }
+            MuonMatrix& to = jobs[at++].m;
+            to.in = (uint64_t)(uintptr_t)m[i].grad;
+            to.momentum = (uint64_t)(uintptr_t)m[i].momentum;
+            to.master = (uint64_t)(uintptr_t)m[i].master;
+            to.out = (uint64_t)(uintptr_t)m[i].param;
+            to.in_ld = to.out_ld = m[i].cols;
+            to.scale = (float)(args->lr * m[i].scale);
+        }
+        if (jobs.empty()) return CKPT_OK;
+        if (overlap(spans)) return fail_free(CKPT_EINVAL, "fragments overlap");
+        if (ckpt_status st = check_workspace(workspace, workspace_bytes, device, known)) return st;
+        MuonArgs a = {};
+        a.beta = (float)args->momentum;
+        a.one_beta = (float)(1 - args->momentum);
+        a.keep = (float)(1 - args->lr * args->weight_decay);
+        a.grad_scale = args->grad_scale;
+        a.nesterov = args->nesterov != 0;
+        a.in_f32 = ge == 4;
+        a.out_f32 = pe == 4;
+        return run_all(jobs, a, args->ns, workspace, workspace_bytes, (hipStream_t)stream);
+    });
+}

@@ -187,4 +187,36 @@ constexpr uint32_t kNormFewTile = 2048, kNormFew = 64 * kNormFewTile;
 hipError_t launch_norm_few(const NormArgs& a, bool f32, double max_norm, float* out, hipStream_t stream);
 hipError_t launch_norm_finish(const double* part, double max_norm, float* out, hipStream_t stream);
 
+// ---- orthogonalised updates (muon_kernels.hip) ----
+
+// A matrix of s x l values, s the shorter side, is held as two planes of fp16 (22 bits) that are 2^12 times its values, in
+// rows of up(l, 64) with zeros behind them: x and y in turn, and a and b, s x s in rows of up(s, 64).
+constexpr uint32_t kMuonMats = 32; // per launch: kernel arguments stay below 4 KiB
+struct MuonMatrix {
+    uint64_t x, y, a, b;
+    uint64_t in, momentum, master, out; // momentum == 0: `in` is orthogonalised, and out is the result's; else out is the parameter's
+    uint64_t in_ld, out_ld;
+    uint64_t part; // double [part_n]: sums of squares, a tile's each
+    uint32_t part_n, rows, cols, first;
+    float scale; // lr times the matrix's scale
+};
+struct MuonArgs {
+    MuonMatrix m[kMuonMats];
+    uint32_t count, tiles; // tiles: of this launch, m[].first the first of each matrix
+    float beta, one_beta, keep, ca, cb, cc;
+    double eps;
+    const float* grad_scale;
+    bool nesterov, in_f32, out_f32;
+};
+// Elements of the tiles of the launches that are not products.
+constexpr uint32_t kMuonRows = 16, kMuonCols = 256, kMuonTurn = 64;
+// Momentum, and the squares of the update.
+hipError_t launch_muon_first(MuonArgs& a, hipStream_t stream);
+// The update over its norm into x.
+hipError_t launch_muon_pack(MuonArgs& a, hipStream_t stream);
+// a = x x^T, b = ca I + cb a + cc a a.
+hipError_t launch_muon_gram(MuonArgs& a, bool poly, hipStream_t stream);
+// y = b x; `last`: into the master copy and the parameter, or the result.
+hipError_t launch_muon_apply(MuonArgs& a, bool last, hipStream_t stream);
+
 } // namespace ckpt
