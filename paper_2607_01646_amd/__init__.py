@@ -11,6 +11,8 @@ analytic models and replica placement are in `disruption` and `placement`.
 """
 from .ckpt import *  # noqa: F401,F403
 from .ckpt import Checkpointer, CkptError, Peer, PeerError, lib  # noqa: F401
+from .embed import *  # noqa: F401,F403
+from .embed import ckpt_embedding, ckpt_embedding_grad  # noqa: F401
 from .muon import *  # noqa: F401,F403
 from .muon import ckpt_muon, ckpt_orthogonalize  # noqa: F401
 from .ops import *  # noqa: F401,F403

@@ -23,8 +23,9 @@ DEVICE_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC",
 HOST_CXX = os.environ.get("CXX_HOST", "g++")
 HOST_SOURCES = ["ckpt_runtime.cpp", "ckpt_snapshot.cpp", "ckpt_check.cpp", "ckpt_bounce.cpp", "ckpt_file.cpp",
                 "ckpt_h2h.cpp", "ckpt_peer.cpp", "ckpt_recover.cpp", "ckpt_noalloc.cpp"]
-OPS_SOURCES = ["ckpt_ops.cpp", "ckpt_muon.cpp"]  # the training-step operators: with their kernels only, apart from the runtime
-KERNEL_SOURCES = ["ckpt_kernels.hip", "loss_kernels.hip", "optim_kernels.hip", "muon_kernels.hip"]
+OPS_SOURCES = ["ckpt_ops.cpp", "ckpt_muon.cpp", "ckpt_embed.cpp"]  # the training-step operators: with their kernels only, apart from the runtime
+KERNEL_SOURCES = ["ckpt_kernels.hip", "loss_kernels.hip", "optim_kernels.hip", "muon_kernels.hip",
+                  "embed_kernels.hip"]
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-pthread", "-Wall", "-Wextra", "-D__HIP_PLATFORM_AMD__",
               "-I", "/opt/rocm/include"]
 

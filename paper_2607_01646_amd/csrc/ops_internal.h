@@ -219,4 +219,29 @@ hipError_t launch_muon_gram(MuonArgs& a, bool poly, hipStream_t stream);
 // y = b x; `last`: into the master copy and the parameter, or the result.
 hipError_t launch_muon_apply(MuonArgs& a, bool last, hipStream_t stream);
 
+// ---- the vocabulary table (embed_kernels.hip) ----
+
+struct EmbedArgs {
+    const int64_t* ids;
+    int64_t ignore_index;
+    uint32_t tokens, dim, vocab;
+    float scale;
+    void* rows;
+    uint64_t rows_ld;
+    void* table;
+    uint64_t table_ld;
+    bool rows_f32, table_f32, add;
+    // the gradient's workspace
+    uint32_t range, chunk; // words of a sorting workgroup; sorted tokens that are summed together
+    uint32_t* start;       // [vocab + 1]: the first of each word's tokens in their order
+    uint32_t *order, *word; // [tokens]: the tokens by word, and their words
+    float* part;            // [2][chunks][part_ld]: sums of words that a chunk shares with the one before it, and with the one behind it
+    uint64_t part_ld;
+};
+// Counters of a sorting workgroup's waves fit in LDS.
+constexpr uint32_t kSortWaves = 16, kSortRange = 1000;
+hipError_t launch_lookup(const EmbedArgs& a, hipStream_t stream);
+hipError_t launch_sort(const EmbedArgs& a, hipStream_t stream);
+hipError_t launch_table_sums(const EmbedArgs& a, hipStream_t stream);
+
 } // namespace ckpt
