@@ -38,11 +38,30 @@ ckpt_status check_ns(const ckpt_newton_schulz& ns)
     return CKPT_OK;
 }
 
+// Whether two steps are made from one Gram matrix: X's next is B A B (all are polynomials of A), and X is multiplied once,
+// by the product of both factors.  Of the products with the long side that leaves 9 for 5 steps instead of 15, in units of
+// s^2 l, and of those of the short side 11 instead of 5, in units of s^3.  It is as exact as step by step (a Gram matrix of
+// X itself sets every other step right; with three from one, what is rounded off beside the large singular values grows in
+// the small ones' place until it is all there is).  The product of both factors has to fit the operands' scale.
+bool in_twos(const ckpt_newton_schulz& ns)
+{
+    constexpr int kGrid = 512;
+    for (int k = 0; k <= kGrid; ++k) {
+        double x = (double)k / kGrid, before = 0;
+        for (uint32_t i = 0; i < ns.steps; ++i) {
+            const double s = x * x, factor = ns.a + s * (ns.b + s * ns.c);
+            if (std::fabs(before * factor) > 14) return false;
+            x *= before = factor;
+        }
+    }
+    return true;
+}
+
 // A matrix of the call, whichever entry point it is of.
 struct Job {
     MuonMatrix m;
     uint64_t s, l;
-    uint64_t x, y, a, b, part; // offsets in the workspace
+    uint64_t x, y, a, b, c, part; // offsets in the workspace
 };
 
 // Lays the operands of a matrix out from `at` on; false where 64 bits do not count them.
@@ -56,7 +75,8 @@ bool lay_out(Job& j, uint64_t rows, uint64_t cols, uint64_t& at)
     j.y = j.x + x;
     j.a = j.y + x;
     j.b = j.a + a;
-    j.part = j.b + a;
+    j.c = j.b + a;
+    j.part = j.c + a;
     at = j.part + up(8 * tiles, 256);
     j.m.rows = (uint32_t)rows;
     j.m.cols = (uint32_t)cols;
@@ -118,28 +138,56 @@ ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schul
     if (need > workspace_bytes)
         return fail_free(CKPT_EINVAL, "workspace of %llu bytes needs %llu", (unsigned long long)workspace_bytes,
                          (unsigned long long)need);
-    a.ca = (float)ns.a;
-    a.cb = (float)ns.b;
-    a.cc = (float)ns.c;
     a.eps = ns.eps;
+    const bool twos = in_twos(ns);
     const uint64_t w = (uint64_t)(uintptr_t)workspace;
     return grouped(jobs, ns.piece_bytes, &need, [&](size_t first, size_t last) {
         a.count = (uint32_t)(last - first);
         for (size_t k = first; k < last; ++k) {
-            MuonMatrix& m = a.m[k - first] = jobs[k].m;
-            m.x = w + jobs[k].x;
-            m.y = w + jobs[k].y;
-            m.a = w + jobs[k].a;
-            m.b = w + jobs[k].b;
-            m.part = w + jobs[k].part;
+            a.m[k - first] = jobs[k].m;
+            a.m[k - first].part = w + jobs[k].part;
+            a.m[k - first].x = w + jobs[k].x;
         }
         hipError_t err = launch_muon_first(a, s);
         if (err == hipSuccess) err = launch_muon_pack(a, s);
-        for (uint32_t step = 0; step < ns.steps && err == hipSuccess; ++step) {
-            err = launch_muon_gram(a, false, s);
-            if (err == hipSuccess) err = launch_muon_gram(a, true, s);
-            if (err == hipSuccess) err = launch_muon_apply(a, step + 1 == ns.steps, s);
-            for (uint32_t k = 0; k < a.count; ++k) std::swap(a.m[k].x, a.m[k].y);
+        // out = cb c + cc p q of all matrices, and with `poly` ca I in it.
+        const auto tri = [&](uint64_t Job::*p, uint64_t Job::*q, uint64_t Job::*out, bool poly) {
+            if (err != hipSuccess) return;
+            TriArgs t = {};
+            t.count = a.count;
+            t.ca = (float)ns.a;
+            t.cb = (float)ns.b;
+            t.cc = poly ? (float)ns.c : 1.0f;
+            for (size_t k = first; k < last; ++k) {
+                const Job& j = jobs[k];
+                t.m[k - first] = {w + j.*p, w + j.*q, poly ? w + j.*p : 0, w + j.*out, (uint32_t)j.s,
+                                  (uint32_t)up(p == &Job::x || p == &Job::y ? j.l : j.s, 64), 0, 0};
+            }
+            err = launch_muon_tri(t, s);
+        };
+        uint64_t Job::*x = &Job::x, Job::*y = &Job::y, Job::*f;
+        for (uint32_t step = 0; step < ns.steps && err == hipSuccess; std::swap(x, y)) {
+            tri(x, x, &Job::a, false);
+            tri(&Job::a, &Job::a, &Job::b, true);
+            f = &Job::b;
+            step += 1;
+            if (twos && step < ns.steps) { // the next Gram matrix is B A B, and both factors are one
+                tri(&Job::a, &Job::b, &Job::c, false);
+                tri(&Job::c, &Job::b, &Job::a, false);
+                tri(&Job::a, &Job::a, &Job::c, true);
+                tri(&Job::c, &Job::b, &Job::a, false);
+                f = &Job::a;
+                step += 1;
+            }
+            if (err != hipSuccess) break;
+            for (size_t k = first; k < last; ++k) {
+                MuonMatrix& m = a.m[k - first];
+                m = jobs[k].m;
+                m.x = w + jobs[k].*x;
+                m.y = w + jobs[k].*y;
+                m.f = w + jobs[k].*f;
+            }
+            err = launch_muon_apply(a, step == ns.steps, s);
         }
         return err == hipSuccess ? CKPT_OK : fail_free(CKPT_EHIP, "orthogonalisation: %s", hipGetErrorString(err));
     });

@@ -219,21 +219,19 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const MuonArgs a)
 
 // ---- the products ----
 
-// A tile of A or B, and its mirror image: only the tiles on and below the diagonal are made, and of those only values on and
-// below it are used.  So both are symmetric to the last bit, and a value does not depend on the size of the tiles: the
-// matrices of a call do not change each other's results.
-struct GramEnd {
-    uint16_t* out;
-    const uint16_t* in; // A, for B
-    uint64_t plane;
-    uint32_t s, ld;
-    float ca, cb, cc;
-    bool poly;
+// Two planes of a run of 4 values of a row.
+struct Planes {
+    uint2 hi, lo;
+    __device__ inline void load(const uint16_t* p, uint64_t plane)
+    {
+        hi = *(const uint2*)p;
+        lo = *(const uint2*)(p + plane);
+    }
+    __device__ inline float at(int j) const
+    {
+        return (float)__builtin_bit_cast(f16x4, hi)[j] + (float)__builtin_bit_cast(f16x4, lo)[j];
+    }
 };
-
-// Another mapping of a 32 x 32 tile's values: row p of q.  One wave's, through its own LDS.
-constexpr uint32_t kTurnLd = 40;
-constexpr uint32_t kTurnWave = 32 * kTurnLd;
 
 // What the lanes of this wave have written to LDS is there for its others.
 __device__ inline void same_wave()
@@ -242,9 +240,23 @@ __device__ inline void same_wave()
     __builtin_amdgcn_wave_barrier();
 }
 
+// A tile of a symmetric product, out = ca I + cb C + cc P Q, and its mirror image: only the tiles on and below the diagonal
+// are made, and of those only values on and below it are used.  So the result is symmetric to the last bit, and a value
+// does not depend on the size of the tiles: the matrices of a call do not change each other's results.
+struct TriEnd {
+    uint16_t* out;
+    const uint16_t* c; // or nullptr
+    uint64_t plane;
+    uint32_t s, ld;
+    float ca, cb, cc;
+};
+
+// Where a wave turns a 32 x 32 tile: rows of p, q across.
+constexpr uint32_t kTurnLd = 40, kTurnWave = 32 * kTurnLd;
+
 template <int TP, int TQ>
-struct Finish<GramEnd, TP, TQ> {
-    static __device__ inline void run(const GramEnd& e, const Early<GramEnd, TQ>&, f32x16 (&acc)[TP][TQ], uint32_t p0,
+struct Finish<TriEnd, TP, TQ> {
+    static __device__ inline void run(const TriEnd& e, const Early<TriEnd, TQ>&, f32x16 (&acc)[TP][TQ], uint32_t p0,
                                       uint32_t q0, uint32_t, uint16_t* lds)
     {
         const uint32_t lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -257,44 +269,54 @@ struct Finish<GramEnd, TP, TQ> {
                 const uint32_t ps = p0 + 32 * tp, qs = q0 + 32 * tq, q = qs + (lane & 31);
                 if (ps > qs || qs >= e.ld) continue; // ld covers whole tiles of 32
                 uint2 hi[4], lo[4];
+                {
+                    Planes c[4];
+                    if (e.c) {
+                        const uint16_t* row = e.c + (uint64_t)min(q, e.s - 1) * e.ld + ps + 4 * half;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t p = ps + 8 * r + 4 * half;
-                    f32x4 v;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = acc[tp][tq][4 * r + j] * kDown;
-                    if (e.poly) {
-                        f16x4 ah = {0, 0, 0, 0}, al = ah;
-                        if (q < e.s) {
-                            ah = *(const f16x4*)(e.in + (uint64_t)q * e.ld + p);
-                            al = *(const f16x4*)(e.in + e.plane + (uint64_t)q * e.ld + p);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            v[j] = e.cc * v[j] + e.cb * ((float)ah[j] + (float)al[j]) + (p + j == q ? e.ca * kUp : 0.0f);
+                        for (int r = 0; r < 4; ++r) c[r].load(row + 8 * r, e.plane);
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = p + j < e.s && q < e.s ? v[j] : 0.0f;
-                    split2(v, hi[r], lo[r]);
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t p = ps + 8 * r + 4 * half;
+                        f32x4 v;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = e.cc * (acc[tp][tq][4 * r + j] * kDown);
+                        if (e.c) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) v[j] += e.cb * c[r].at(j) + (p + j == q ? e.ca * kUp : 0.0f);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = p + j < e.s && q < e.s ? v[j] : 0.0f;
+                        split2(v, hi[r], lo[r]);
+                    }
                 }
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
                     const uint2* w = z ? lo : hi;
                     uint16_t* out = e.out + z * e.plane;
-                    const u16x8 a = pair_of(w[0], w[1]), b = pair_of(w[2], w[3]);
-                    if (ps < qs && q < e.s) {
-                        uint16_t* row = out + (uint64_t)q * e.ld + ps + 8 * half;
-                        *(u16x8*)row = a;
-                        *(u16x8*)(row + 16) = b;
-                    }
+                    if (ps < qs) {
+                        const u16x8 a = pair_of(w[0], w[1]), b = pair_of(w[2], w[3]);
+                        if (q < e.s) {
+                            uint16_t* row = out + (uint64_t)q * e.ld + ps + 8 * half;
+                            *(u16x8*)row = a;
+                            *(u16x8*)(row + 16) = b;
+                        }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const u16x4 u = __builtin_bit_cast(u16x4, w[r]);
+                        for (int r = 0; r < 4; ++r) {
+                            const u16x4 u = __builtin_bit_cast(u16x4, w[r]);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t p = 8 * r + 4 * half + j;
-                            if (ps < qs || p <= (lane & 31)) turn[p * kTurnLd + (lane & 31)] = u[j];
-                            if (ps == qs && p <= (lane & 31)) turn[(lane & 31) * kTurnLd + p] = u[j];
+                            for (int j = 0; j < 4; ++j) turn[(8 * r + 4 * half + j) * kTurnLd + (lane & 31)] = u[j];
+                        }
+                    } else { // on the diagonal: below it, and its image
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const u16x4 u = __builtin_bit_cast(u16x4, w[r]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint32_t p = 8 * r + 4 * half + j;
+                                if (p <= (lane & 31)) turn[p * kTurnLd + (lane & 31)] = turn[(lane & 31) * kTurnLd + p] = u[j];
+                            }
                         }
                     }
                     same_wave();
@@ -368,98 +390,114 @@ struct Finish<LastEnd, TP, TQ> {
         for (int tq = 0; tq < TQ; ++tq)
 #pragma unroll
             for (int tp = 0; tp < TP; ++tp) {
-                const uint32_t q = q0 + 32 * tq + (lane & 31);
-                if (q >= e.q) continue;
+                const uint32_t ps = p0 + 32 * tp, q = q0 + 32 * tq + (lane & 31), p = ps + 4 * half;
+                f32x4 v[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t p = p0 + 32 * tp + 8 * r + 4 * half;
-                    f32x4 v;
+                for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = acc[tp][tq][4 * r + j] * (kDown * kDown);
-                    if (p + 4 <= e.p) {
-                        if (e.master) {
-                            float* w = e.master + (uint64_t)q * e.p + p;
-                            v = load4(w) * e.keep - v * e.lr;
-                            *(f32x4_any*)w = v;
-                        }
-                        if (e.f32)
-                            *(f32x4_any*)((float*)e.out + (uint64_t)q * e.out_ld + p) = v;
-                        else
-                            *(u16x4_any*)((uint16_t*)e.out + (uint64_t)q * e.out_ld + p) =
-                                u16x4{bf16_of(v[0]), bf16_of(v[1]), bf16_of(v[2]), bf16_of(v[3])};
-                    } else {
+                    for (int j = 0; j < 4; ++j) v[r][j] = acc[tp][tq][4 * r + j] * (kDown * kDown);
+                if (q >= e.q || ps >= e.p) continue;
+                float* w = e.master ? e.master + (uint64_t)q * e.p + p : nullptr;
+                const uint64_t to = (uint64_t)q * e.out_ld + p;
+                if (ps + 32 <= e.p) {
+                    if (w) {
+                        f32x4 old[4];
 #pragma unroll
-                        for (uint32_t j = 0; j < 3; ++j) {
-                            if (p + j >= e.p) continue;
-                            float y = v[j];
-                            if (e.master) {
-                                float* w = e.master + (uint64_t)q * e.p + p + j;
-                                y = *w * e.keep - y * e.lr;
-                                *w = y;
-                            }
-                            if (e.f32)
-                                ((float*)e.out)[(uint64_t)q * e.out_ld + p + j] = y;
-                            else
-                                ((uint16_t*)e.out)[(uint64_t)q * e.out_ld + p + j] = bf16_of(y);
+                        for (int r = 0; r < 4; ++r) old[r] = load4(w + 8 * r);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            v[r] = old[r] * e.keep - v[r] * e.lr;
+                            *(f32x4_any*)(w + 8 * r) = v[r];
                         }
                     }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (e.f32)
+                            *(f32x4_any*)((float*)e.out + to + 8 * r) = v[r];
+                        else
+                            *(u16x4_any*)((uint16_t*)e.out + to + 8 * r) =
+                                u16x4{bf16_of(v[r][0]), bf16_of(v[r][1]), bf16_of(v[r][2]), bf16_of(v[r][3])};
+                    continue;
                 }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) {
+                        if (p + 8 * r + j >= e.p) continue;
+                        float y = v[r][j];
+                        if (w) {
+                            y = w[8 * r + j] * e.keep - y * e.lr;
+                            w[8 * r + j] = y;
+                        }
+                        if (e.f32)
+                            ((float*)e.out)[to + 8 * r + j] = y;
+                        else
+                            ((uint16_t*)e.out)[to + 8 * r + j] = bf16_of(y);
+                    }
             }
     }
 };
 
-// An XCD gets a run of consecutive tiles.
-__device__ inline uint32_t run_of(uint32_t block, uint32_t n)
+// The tile of workgroup `block` of the `n` tiles of a matrix, whose workgroups are a multiple of 8 and begin at one:
+// workgroups go round the XCDs, and each XCD gets a run of consecutive tiles of every matrix.  False: none.
+__device__ inline bool run_of(uint32_t block, uint32_t n, uint32_t& tile)
 {
-    const uint32_t each = n / kXcds, more = n % kXcds, xcd = block % kXcds;
-    return xcd * each + min(xcd, more) + block / kXcds;
+    const uint32_t each = n / kXcds, more = n % kXcds, xcd = block % kXcds, at = block / kXcds;
+    tile = xcd * each + min(xcd, more) + at;
+    return at < each + (xcd < more);
 }
 
 template <class S>
-__global__ __launch_bounds__(S::kThreads, S::kThreads >= 512 ? 2 : 1) void gram_kernel(const MuonArgs a, bool poly)
+__global__ __launch_bounds__(S::kThreads, S::kThreads >= 512 ? 2 : 1) void tri_kernel(const TriArgs a)
 {
     CKPT_BUFFERS(S, S);
     static_assert(S::BP == S::BQ && S::kThreads / 64 * kTurnWave <= S::kBuffer, "");
-    const uint32_t t0 = run_of(blockIdx.x, gridDim.x), f = matrix_of(a, t0), t = t0 - a.m[f].first;
-    const uint32_t rows = a.m[f].rows, cols = a.m[f].cols, s = min(rows, cols);
-    const uint32_t ldx = up64(max(rows, cols)), lda = up64(s), ld = poly ? lda : ldx;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t before = __ballot(lane < a.count && a.m[lane < kMuonMats ? lane : 0].first <= blockIdx.x);
+    const TriMatrix m = a.m[__builtin_amdgcn_readfirstlane(63 - __builtin_clzll(before))];
+    const uint32_t n = (m.s + S::BP - 1) / S::BP;
+    uint32_t t;
+    if (!run_of(blockIdx.x - m.first, n * (n + 1) / 2, t)) return;
     // Row i of the triangle begins at tile i (i + 1) / 2.
     uint32_t i = (uint32_t)((__builtin_sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
     while (i * (i + 1) / 2 > t) --i;
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
     const uint32_t j = t - i * (i + 1) / 2;
-    const Operand X = {(const uint16_t*)(poly ? a.m[f].a : a.m[f].x), (uint64_t)s * ld, ld, s, ld};
-    const GramEnd end = {(uint16_t*)(poly ? a.m[f].b : a.m[f].a), (const uint16_t*)a.m[f].a, (uint64_t)s * lda, s, lda,
-                         a.ca, a.cb, a.cc, poly};
-    product<S>(X, X, {s, s, ld, 1, false}, end, make_uint2(__builtin_amdgcn_readfirstlane(j), __builtin_amdgcn_readfirstlane(i)),
+    const Operand P = {(const uint16_t*)m.p, (uint64_t)m.s * m.k, m.k, m.s, m.k};
+    const Operand Q = {(const uint16_t*)m.q, (uint64_t)m.s * m.k, m.k, m.s, m.k};
+    const uint32_t ld = up64(m.s);
+    const TriEnd end = {(uint16_t*)m.out, (const uint16_t*)m.c, (uint64_t)m.s * ld, m.s, ld, a.ca, a.cb, a.cc};
+    product<S>(P, Q, {m.s, m.s, m.k, 1, false}, end, make_uint2(__builtin_amdgcn_readfirstlane(j), __builtin_amdgcn_readfirstlane(i)),
                t, 0, s0, s1, s2, s3);
 }
 
-// WIDE: [q][p] is [short][long]; else [long][short], where the last product of a tall matrix leaves it as it lies.
-template <class End>
-__device__ inline End apply_end(const MuonArgs& a, uint32_t f)
+// [q][p] is [short][long]; for the last X of a tall matrix [long][short], as it lies.  W: the shape of the one, T: of the other.
+template <class W, class T, class End>
+__global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply_kernel(const MuonArgs a)
 {
+    CKPT_BUFFERS(W, T);
+    const uint32_t f = matrix_of(a, blockIdx.x);
     const MuonMatrix& m = a.m[f];
-    const uint32_t s = min(m.rows, m.cols), ldx = up64(max(m.rows, m.cols));
-    if constexpr (std::is_same_v<End, NextEnd>)
-        return {(uint16_t*)m.y, (uint64_t)s * ldx, s, ldx};
-    else
-        return {(float*)m.master, (void*)m.out, m.out_ld, m.cols, m.rows, a.keep, m.scale, a.out_f32};
-}
-template <class S, class End>
-__global__ __launch_bounds__(S::kThreads, S::kThreads >= 512 ? 2 : 1) void apply_kernel(const MuonArgs a)
-{
-    CKPT_BUFFERS(S, S);
-    constexpr bool WIDE = S::PA;
-    const uint32_t t0 = run_of(blockIdx.x, gridDim.x), f = matrix_of(a, t0), t = t0 - a.m[f].first;
-    const uint32_t rows = a.m[f].rows, cols = a.m[f].cols, s = min(rows, cols), l = max(rows, cols);
-    const uint32_t ldx = up64(l), lda = up64(s);
-    const Operand X = {(const uint16_t*)a.m[f].x, (uint64_t)s * ldx, ldx, s, ldx};
-    const Operand B = {(const uint16_t*)a.m[f].b, (uint64_t)s * lda, lda, s, lda};
-    const uint32_t p = WIDE ? l : s, q = WIDE ? s : l, np = (p + S::BP - 1) / S::BP, nq = (q + S::BQ - 1) / S::BQ;
+    const uint32_t s = min(m.rows, m.cols), l = max(m.rows, m.cols), ldx = up64(l), lda = up64(s);
+    const uint32_t ns = (s + W::BP - 1) / W::BP, nl = (l + W::BP - 1) / W::BP;
+    const bool wide = std::is_same_v<End, NextEnd> || m.rows <= m.cols;
+    const uint32_t p = wide ? l : s, q = wide ? s : l, np = wide ? nl : ns, nq = wide ? ns : nl;
+    uint32_t t;
+    if (!run_of(blockIdx.x - m.first, ns * nl, t)) return;
     const uint32_t band = t / (kBand * np), in = t % (kBand * np), width = min(kBand, nq - band * kBand);
     const uint2 tile = make_uint2(in / width, band * kBand + in % width);
-    product<S>(WIDE ? X : B, WIDE ? B : X, {p, q, lda, 1, false}, apply_end<End>(a, f), tile, t, 0, s0, s1, s2, s3);
+    const Operand X = {(const uint16_t*)m.x, (uint64_t)s * ldx, ldx, s, ldx};
+    const Operand B = {(const uint16_t*)m.f, (uint64_t)s * lda, lda, s, lda};
+    if constexpr (std::is_same_v<End, NextEnd>) {
+        const NextEnd end = {(uint16_t*)m.y, (uint64_t)s * ldx, s, ldx};
+        product<W>(X, B, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3);
+    } else {
+        const LastEnd end = {(float*)m.master, (void*)m.out, m.out_ld, p, q, a.keep, m.scale, a.out_f32};
+        if (wide)
+            product<W>(X, B, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3);
+        else
+            product<T>(B, X, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3);
+    }
 }
 
 // ---- shapes ----
@@ -474,25 +512,23 @@ using Middle = Shape<2, 2, PA, QA, 128, 128, 2, 2, 32, 2, true>;
 template <bool PA, bool QA>
 using Small = Shape<2, 2, PA, QA, 64, 64, 2, 1, 32, 3, true>;
 
-uint32_t blocks(uint64_t x, uint32_t side) { return (uint32_t)((x + side - 1) / side); }
-uint64_t triangle(uint64_t n) { return n * (n + 1) / 2; }
+uint64_t blocks(uint64_t x, uint32_t side) { return (x + side - 1) / side; }
 
-// Numbers the tiles of each matrix that `tiles` gives it, and returns all.
-template <class F>
-uint64_t number(MuonArgs& a, F tiles)
+// Numbers the tiles of each matrix that `tiles` gives it, `round` of them at a time, and returns all.
+template <class A, class F>
+uint64_t number(A& a, uint32_t round, F tiles)
 {
     uint64_t all = 0;
     for (uint32_t i = 0; i < a.count; ++i) {
         a.m[i].first = (uint32_t)std::min<uint64_t>(all, 0xffffffffu);
-        all += tiles(a.m[i]);
+        all += (tiles(a.m[i]) + round - 1) / round * round;
     }
-    a.tiles = (uint32_t)std::min<uint64_t>(all, 0xffffffffu);
     return all;
 }
 
-// The largest tiles that still give each compute unit one.
-template <class F>
-Size size_of(MuonArgs& a, F tiles)
+// The size of tiles that is done first, of products that have `tiles(m, side)` with `steps(m)` of 64 values of k each.
+template <class A, class T, class K>
+Size size_of(const A& a, T tiles, K steps)
 {
     for (int s = kLarge; s > kSmall; --s) {
         uint64_t all = 0;
@@ -502,84 +538,70 @@ Size size_of(MuonArgs& a, F tiles)
     return kSmall;
 }
 
-template <class S>
-hipError_t gram(const MuonArgs& a, bool poly, hipStream_t stream)
+template <class K>
+hipError_t launch_tiles(K kernel, const void* args, uint64_t tiles, uint32_t threads, hipStream_t stream)
 {
-    if ((uint64_t)a.tiles * S::kThreads > 0xffffffffu) return hipErrorInvalidValue;
-    gram_kernel<S><<<a.tiles, S::kThreads, 0, stream>>>(a, poly);
-    return hipGetLastError();
+    if (tiles == 0 || tiles * threads > 0xffffffffu) return hipErrorInvalidValue;
+    void* list[] = {const_cast<void*>(args)};
+    return hipLaunchKernel((const void*)kernel, dim3((uint32_t)tiles), dim3(threads), list, 0, stream);
 }
-template <class S, class End>
-hipError_t apply(const MuonArgs& a, hipStream_t stream)
+
+template <class End>
+hipError_t apply(MuonArgs& a, hipStream_t stream)
 {
-    if ((uint64_t)a.tiles * S::kThreads > 0xffffffffu) return hipErrorInvalidValue;
-    apply_kernel<S, End><<<a.tiles, S::kThreads, 0, stream>>>(a);
-    return hipGetLastError();
-}
-template <bool WIDE, class End>
-hipError_t apply_sized(MuonArgs& a, hipStream_t stream)
-{
+    constexpr bool kNext = std::is_same_v<End, NextEnd>;
     const auto tiles = [](const MuonMatrix& m, uint32_t side) {
-        return (uint64_t)blocks(std::min(m.rows, m.cols), side) * blocks(std::max(m.rows, m.cols), side);
+        return blocks(std::min(m.rows, m.cols), side) * blocks(std::max(m.rows, m.cols), side);
     };
-    const Size size = size_of(a, tiles);
-    number(a, [&](const MuonMatrix& m) { return tiles(m, kSide[size]); });
-    return size == kLarge    ? apply<Large<WIDE, !WIDE>, End>(a, stream)
-           : size == kMiddle ? apply<Middle<WIDE, !WIDE>, End>(a, stream)
-                             : apply<Small<WIDE, !WIDE>, End>(a, stream);
+    const auto steps = [](const MuonMatrix& m) { return blocks(std::min(m.rows, m.cols), 64); };
+    std::stable_sort(a.m, a.m + a.count, [&](const MuonMatrix& x, const MuonMatrix& y) { return steps(x) > steps(y); });
+    const Size size = size_of(a, tiles, steps);
+    const uint64_t all = number(a, kXcds, [&](const MuonMatrix& m) { return tiles(m, kSide[size]); });
+    using LT = std::conditional_t<kNext, Large<true, false>, Large<false, true>>;
+    using MT = std::conditional_t<kNext, Middle<true, false>, Middle<false, true>>;
+    using ST = std::conditional_t<kNext, Small<true, false>, Small<false, true>>;
+    return size == kLarge    ? launch_tiles(apply_kernel<Large<true, false>, LT, End>, &a, all, LT::kThreads, stream)
+           : size == kMiddle ? launch_tiles(apply_kernel<Middle<true, false>, MT, End>, &a, all, MT::kThreads, stream)
+                             : launch_tiles(apply_kernel<Small<true, false>, ST, End>, &a, all, ST::kThreads, stream);
 }
 
 } // namespace
 
 hipError_t launch_muon_first(MuonArgs& a, hipStream_t stream)
 {
-    number(a, [](const MuonMatrix& m) { return (uint64_t)m.part_n; });
-    if (a.tiles == 0 || (uint64_t)a.tiles * kThreads > 0xffffffffu) return hipErrorInvalidValue;
-    if (a.in_f32)
-        first_kernel<float><<<a.tiles, kThreads, 0, stream>>>(a);
-    else
-        first_kernel<uint16_t><<<a.tiles, kThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    const uint64_t tiles = number(a, 1, [](const MuonMatrix& m) { return (uint64_t)m.part_n; });
+    return a.in_f32 ? launch_tiles(first_kernel<float>, &a, tiles, kThreads, stream)
+                    : launch_tiles(first_kernel<uint16_t>, &a, tiles, kThreads, stream);
 }
 
 hipError_t launch_muon_pack(MuonArgs& a, hipStream_t stream)
 {
-    number(a, [](const MuonMatrix& m) {
-        return m.rows <= m.cols ? (uint64_t)blocks(m.rows, kMuonRows) * blocks(((uint64_t)m.cols + 63) / 64 * 64, kMuonCols)
-                                : (uint64_t)blocks(m.rows, kMuonTurn) * blocks(m.cols, kMuonTurn);
+    const uint64_t tiles = number(a, 1, [](const MuonMatrix& m) {
+        return m.rows <= m.cols ? blocks(m.rows, kMuonRows) * blocks(((uint64_t)m.cols + 63) / 64 * 64, kMuonCols)
+                                : blocks(m.rows, kMuonTurn) * blocks(m.cols, kMuonTurn);
     });
-    if (a.tiles == 0 || (uint64_t)a.tiles * kThreads > 0xffffffffu) return hipErrorInvalidValue;
-    if (a.in_f32)
-        pack_kernel<float><<<a.tiles, kThreads, 0, stream>>>(a);
-    else
-        pack_kernel<uint16_t><<<a.tiles, kThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    return a.in_f32 ? launch_tiles(pack_kernel<float>, &a, tiles, kThreads, stream)
+                    : launch_tiles(pack_kernel<uint16_t>, &a, tiles, kThreads, stream);
 }
 
-hipError_t launch_muon_gram(MuonArgs& a, bool poly, hipStream_t stream)
+hipError_t launch_muon_tri(TriArgs& a, hipStream_t stream)
 {
-    const auto tiles = [](const MuonMatrix& m, uint32_t side) { return triangle(blocks(std::min(m.rows, m.cols), side)); };
-    const Size size = size_of(a, tiles);
-    number(a, [&](const MuonMatrix& m) { return tiles(m, kSide[size]); });
-    return size == kLarge    ? gram<Large<false, false>>(a, poly, stream)
-           : size == kMiddle ? gram<Middle<false, false>>(a, poly, stream)
-                             : gram<Small<false, false>>(a, poly, stream);
+    const auto tiles = [](const TriMatrix& m, uint32_t side) {
+        const uint64_t n = blocks(m.s, side);
+        return n * (n + 1) / 2;
+    };
+    const auto steps = [](const TriMatrix& m) { return (uint64_t)m.k / 64; };
+    std::stable_sort(a.m, a.m + a.count, [&](const TriMatrix& x, const TriMatrix& y) { return x.k > y.k; });
+    const Size size = size_of(a, tiles, steps);
+    const uint64_t all = number(a, kXcds, [&](const TriMatrix& m) { return tiles(m, kSide[size]); });
+    return size == kLarge    ? launch_tiles(tri_kernel<Large<false, false>>, &a, all, Large<false, false>::kThreads, stream)
+           : size == kMiddle ? launch_tiles(tri_kernel<Middle<false, false>>, &a, all, Middle<false, false>::kThreads, stream)
+                             : launch_tiles(tri_kernel<Small<false, false>>, &a, all, Small<false, false>::kThreads, stream);
 }
 
 hipError_t launch_muon_apply(MuonArgs& a, bool last, hipStream_t stream)
 {
-    if (!last) return apply_sized<true, NextEnd>(a, stream);
-    // Wide and tall matrices end with products of their own.
-    MuonArgs some = a;
-    for (const bool wide : {true, false}) {
-        some.count = 0;
-        for (uint32_t i = 0; i < a.count; ++i)
-            if ((a.m[i].rows <= a.m[i].cols) == wide) some.m[some.count++] = a.m[i];
-        if (some.count == 0) continue;
-        const hipError_t e = wide ? apply_sized<true, LastEnd>(some, stream) : apply_sized<false, LastEnd>(some, stream);
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    return last ? apply<LastEnd>(a, stream) : apply<NextEnd>(a, stream);
 }
 
 } // namespace ckpt

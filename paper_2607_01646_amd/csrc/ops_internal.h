@@ -190,10 +190,10 @@ hipError_t launch_norm_finish(const double* part, double max_norm, float* out, h
 // ---- orthogonalised updates (muon_kernels.hip) ----
 
 // A matrix of s x l values, s the shorter side, is held as two planes of fp16 (22 bits) that are 2^12 times its values, in
-// rows of up(l, 64) with zeros behind them: x and y in turn, and a and b, s x s in rows of up(s, 64).
+// rows of up(l, 64) with zeros behind them; its Gram matrix and polynomials of that are s x s in rows of up(s, 64).
 constexpr uint32_t kMuonMats = 32; // per launch: kernel arguments stay below 4 KiB
 struct MuonMatrix {
-    uint64_t x, y, a, b;
+    uint64_t x, y, f; // launch_muon_apply: y (or the result) = f x
     uint64_t in, momentum, master, out; // momentum == 0: `in` is orthogonalised, and out is the result's; else out is the parameter's
     uint64_t in_ld, out_ld;
     uint64_t part; // double [part_n]: sums of squares, a tile's each
@@ -201,12 +201,22 @@ struct MuonMatrix {
     float scale; // lr times the matrix's scale
 };
 struct MuonArgs {
-    MuonMatrix m[kMuonMats];
-    uint32_t count, tiles; // tiles: of this launch, m[].first the first of each matrix
-    float beta, one_beta, keep, ca, cb, cc;
+    MuonMatrix m[kMuonMats]; // launches may put them in another order
+    uint32_t count;
+    float beta, one_beta, keep;
     double eps;
     const float* grad_scale;
     bool nesterov, in_f32, out_f32;
+};
+// Symmetric products out = ca I + cb c + cc p q, p q^T of rows of k values; c == 0: cc p q alone.
+struct TriMatrix {
+    uint64_t p, q, c, out;
+    uint32_t s, k, first, unused;
+};
+struct TriArgs {
+    TriMatrix m[kMuonMats];
+    uint32_t count;
+    float ca, cb, cc;
 };
 // Elements of the tiles of the launches that are not products.
 constexpr uint32_t kMuonRows = 16, kMuonCols = 256, kMuonTurn = 64;
@@ -214,9 +224,8 @@ constexpr uint32_t kMuonRows = 16, kMuonCols = 256, kMuonTurn = 64;
 hipError_t launch_muon_first(MuonArgs& a, hipStream_t stream);
 // The update over its norm into x.
 hipError_t launch_muon_pack(MuonArgs& a, hipStream_t stream);
-// a = x x^T, b = ca I + cb a + cc a a.
-hipError_t launch_muon_gram(MuonArgs& a, bool poly, hipStream_t stream);
-// y = b x; `last`: into the master copy and the parameter, or the result.
+hipError_t launch_muon_tri(TriArgs& a, hipStream_t stream);
+// The next X, or the last: into the master copy and the parameter, or the result.
 hipError_t launch_muon_apply(MuonArgs& a, bool last, hipStream_t stream);
 
 // ---- the vocabulary table (embed_kernels.hip) ----
