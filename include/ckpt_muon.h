@@ -34,7 +34,7 @@ typedef struct {
     double a, b, c;       /* the polynomial, and all its iterates, stay within [-2, 2] on [0, 1] */
     double eps;           /* > 0 */
     uint64_t piece_bytes; /* bound on the workspace: matrices are taken in groups that fit (at least one);
-                             0 = 2 GiB */
+                             0 = 4 GiB */
 } ckpt_newton_schulz;
 
 typedef struct {
@@ -47,7 +47,7 @@ typedef struct {
 
 /* Orthogonalises n matrices of one type (CKPT_TYPE_*).  `workspace`: 256-byte
  * aligned device memory of at least the bytes that _workspace says, the call's
- * own until its work on `stream` has run.
+ * own until its work on `stream` has run (NULL where that is 0).
  * Errors: EINVAL (sizes, numbers, pointers, outputs that overlap), EHIP. */
 ckpt_status ckpt_orthogonalize_workspace(const ckpt_matrix* m, uint32_t n, const ckpt_newton_schulz* ns,
                                          uint64_t* bytes);

@@ -4,6 +4,7 @@
 // the host, and nothing outlives a call.
 #include <algorithm>
 #include <cmath>
+#include <iterator>
 #include <new>
 #include <vector>
 
@@ -14,7 +15,7 @@
 namespace ckpt {
 namespace {
 
-constexpr uint64_t kDefaultPiece = 2ull << 30;
+constexpr uint64_t kDefaultPiece = 4ull << 30; // the matrices of a layer of 4096 x 11008, in one group
 
 ckpt_status check_ns(const ckpt_newton_schulz& ns)
 {
@@ -84,6 +85,18 @@ bool lay_out(Job& j, uint64_t rows, uint64_t cols, uint64_t& at)
     return tiles <= (1u << 23);
 }
 
+// Takes the matrices out that need no workspace: by their own sides, so that a matrix's result does not depend on others.
+std::vector<Job> take_tiny(std::vector<Job>& jobs)
+{
+    std::vector<Job> tiny;
+    const auto small = [](const Job& j) {
+        return std::min(j.m.rows, j.m.cols) <= kTinyShort && std::max(j.m.rows, j.m.cols) <= kTinyLong;
+    };
+    std::copy_if(jobs.begin(), jobs.end(), std::back_inserter(tiny), small);
+    jobs.erase(std::remove_if(jobs.begin(), jobs.end(), small), jobs.end());
+    return tiny;
+}
+
 // Cuts the matrices into groups: calls `run(first, last)` for each, and finds the bytes that the largest takes.
 template <class F>
 ckpt_status grouped(std::vector<Job>& jobs, uint64_t piece_bytes, uint64_t* most, F run)
@@ -134,11 +147,18 @@ ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schul
                     uint64_t workspace_bytes, hipStream_t s)
 {
     uint64_t need = 0;
+    const std::vector<Job> tiny = take_tiny(jobs);
     if (ckpt_status st = grouped(jobs, ns.piece_bytes, &need, nothing)) return st;
     if (need > workspace_bytes)
         return fail_free(CKPT_EINVAL, "workspace of %llu bytes needs %llu", (unsigned long long)workspace_bytes,
                          (unsigned long long)need);
     a.eps = ns.eps;
+    for (size_t i = 0; i < tiny.size(); i += kMuonMats) {
+        a.count = (uint32_t)std::min<size_t>(kMuonMats, tiny.size() - i);
+        for (uint32_t k = 0; k < a.count; ++k) a.m[k] = tiny[i + k].m;
+        const hipError_t err = launch_muon_tiny(a, {(float)ns.a, (float)ns.b, (float)ns.c, ns.steps}, s);
+        if (err != hipSuccess) return fail_free(CKPT_EHIP, "orthogonalisation: %s", hipGetErrorString(err));
+    }
     const bool twos = in_twos(ns);
     const uint64_t w = (uint64_t)(uintptr_t)workspace;
     return grouped(jobs, ns.piece_bytes, &need, [&](size_t first, size_t last) {
@@ -272,6 +292,7 @@ extern "C" ckpt_status ckpt_orthogonalize_workspace(const ckpt_matrix* m, uint32
         std::vector<Job> jobs;
         if (!bytes) return fail_free(CKPT_EINVAL, "null argument");
         if (ckpt_status st = orthogonalize_jobs(m, n, ns, jobs)) return st;
+        take_tiny(jobs);
         return grouped(jobs, ns->piece_bytes, bytes, nothing);
     });
 }
@@ -311,7 +332,8 @@ extern "C" ckpt_status ckpt_orthogonalize(const ckpt_matrix* m, uint32_t n, uint
         }
         if (jobs.empty()) return CKPT_OK;
         if (overlap(spans)) return fail_free(CKPT_EINVAL, "a result overlaps another matrix");
-        if (ckpt_status st = check_workspace(workspace, workspace_bytes, device, known)) return st;
+        if (workspace_bytes)
+            if (ckpt_status st = check_workspace(workspace, workspace_bytes, device, known)) return st;
         MuonArgs a = {};
         a.in_f32 = a.out_f32 = e == 4;
         return run_all(jobs, a, *ns, workspace, workspace_bytes, (hipStream_t)stream);
@@ -324,6 +346,7 @@ extern "C" ckpt_status ckpt_muon_workspace(const ckpt_muon_matrix* m, uint32_t n
         std::vector<Job> jobs;
         if (!bytes) return fail_free(CKPT_EINVAL, "null argument");
         if (ckpt_status st = muon_jobs(m, n, args, jobs)) return st;
+        take_tiny(jobs);
         return grouped(jobs, args->ns.piece_bytes, bytes, nothing);
     });
 }
@@ -375,7 +398,8 @@ extern "C" ckpt_status ckpt_muon(const ckpt_muon_matrix* m, uint32_t n, const ck
         }
         if (jobs.empty()) return CKPT_OK;
         if (overlap(spans)) return fail_free(CKPT_EINVAL, "fragments overlap");
-        if (ckpt_status st = check_workspace(workspace, workspace_bytes, device, known)) return st;
+        if (workspace_bytes)
+            if (ckpt_status st = check_workspace(workspace, workspace_bytes, device, known)) return st;
         MuonArgs a = {};
         a.beta = (float)args->momentum;
         a.one_beta = (float)(1 - args->momentum);

@@ -79,13 +79,14 @@ __device__ inline double wave_sum(double x)
     return x;
 }
 // The workgroup's sum in every lane, the waves' in their order.
+template <int THREADS = kThreads>
 __device__ inline double block_sum(double x, double* s_wave)
 {
     x = wave_sum(x);
     if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = x;
     __syncthreads();
     x = s_wave[0];
-    for (int w = 1; w < kThreads / 64; ++w) x += s_wave[w];
+    for (int w = 1; w < THREADS / 64; ++w) x += s_wave[w];
     return x;
 }
 
@@ -438,13 +439,23 @@ struct Finish<LastEnd, TP, TQ> {
     }
 };
 
-// The tile of workgroup `block` of the `n` tiles of a matrix, whose workgroups are a multiple of 8 and begin at one:
-// workgroups go round the XCDs, and each XCD gets a run of consecutive tiles of every matrix.  False: none.
-__device__ inline bool run_of(uint32_t block, uint32_t n, uint32_t& tile)
+// Workgroups go round the XCDs, each with an L2 of its own.  Where all tiles take the same time an XCD gets a run of them,
+// so that it reads few matrices (A of 7 of 1024 x 8192, tiles of 128: 187 us,
+// with shares 331); else it gets a share of each
+// matrix, a run too, and the longest first: a run of all would leave it only long ones or only short ones.
+// shares: the workgroups of a matrix are a multiple of 8 and begin at one.
+__device__ inline uint32_t run_begin(uint32_t n, uint32_t xcd) { return xcd * (n / kXcds) + min(xcd, n % kXcds); }
+__device__ inline uint32_t nth_tile(bool shares, uint32_t n) // of n in all
 {
-    const uint32_t each = n / kXcds, more = n % kXcds, xcd = block % kXcds, at = block / kXcds;
-    tile = xcd * each + min(xcd, more) + at;
-    return at < each + (xcd < more);
+    return shares ? blockIdx.x : run_begin(n, blockIdx.x % kXcds) + blockIdx.x / kXcds;
+}
+__device__ inline bool tile_in(bool shares, uint32_t at, uint32_t n, uint32_t& tile) // at-th of a matrix's n
+{
+    tile = at;
+    if (!shares) return true;
+    const uint32_t xcd = at % kXcds;
+    tile = run_begin(n, xcd) + at / kXcds;
+    return tile < run_begin(n, xcd + 1);
 }
 
 template <class S>
@@ -453,11 +464,12 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads >= 512 ? 2 : 1) void tri_k
     CKPT_BUFFERS(S, S);
     static_assert(S::BP == S::BQ && S::kThreads / 64 * kTurnWave <= S::kBuffer, "");
     const uint32_t lane = threadIdx.x & 63;
-    const uint64_t before = __ballot(lane < a.count && a.m[lane < kMuonMats ? lane : 0].first <= blockIdx.x);
+    const uint32_t at = nth_tile(a.shares, gridDim.x);
+    const uint64_t before = __ballot(lane < a.count && a.m[lane < kMuonMats ? lane : 0].first <= at);
     const TriMatrix m = a.m[__builtin_amdgcn_readfirstlane(63 - __builtin_clzll(before))];
     const uint32_t n = (m.s + S::BP - 1) / S::BP;
     uint32_t t;
-    if (!run_of(blockIdx.x - m.first, n * (n + 1) / 2, t)) return;
+    if (!tile_in(a.shares, at - m.first, n * (n + 1) / 2, t)) return;
     // Row i of the triangle begins at tile i (i + 1) / 2.
     uint32_t i = (uint32_t)((__builtin_sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
     while (i * (i + 1) / 2 > t) --i;
@@ -476,14 +488,14 @@ template <class W, class T, class End>
 __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply_kernel(const MuonArgs a)
 {
     CKPT_BUFFERS(W, T);
-    const uint32_t f = matrix_of(a, blockIdx.x);
-    const MuonMatrix& m = a.m[f];
+    const uint32_t at = nth_tile(a.shares, gridDim.x);
+    const MuonMatrix& m = a.m[matrix_of(a, at)];
     const uint32_t s = min(m.rows, m.cols), l = max(m.rows, m.cols), ldx = up64(l), lda = up64(s);
     const uint32_t ns = (s + W::BP - 1) / W::BP, nl = (l + W::BP - 1) / W::BP;
     const bool wide = std::is_same_v<End, NextEnd> || m.rows <= m.cols;
     const uint32_t p = wide ? l : s, q = wide ? s : l, np = wide ? nl : ns, nq = wide ? ns : nl;
     uint32_t t;
-    if (!run_of(blockIdx.x - m.first, ns * nl, t)) return;
+    if (!tile_in(a.shares, at - m.first, ns * nl, t)) return;
     const uint32_t band = t / (kBand * np), in = t % (kBand * np), width = min(kBand, nq - band * kBand);
     const uint2 tile = make_uint2(in / width, band * kBand + in % width);
     const Operand X = {(const uint16_t*)m.x, (uint64_t)s * ldx, ldx, s, ldx};
@@ -500,17 +512,225 @@ __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply
     }
 }
 
+// ---- small matrices ----
+//
+// Up to 64 x 256: a workgroup makes all of a matrix's step, X, A and B in LDS, in the time that the launches' latencies
+// would take many times over (4 matrices of 64 x 64 to 256: XXX us, XXX by the kernels above).  The same sums of the same
+// operands, but step by step.  X is padded with zeros to 64 rows and a multiple of 32 columns; rows lie 16 bytes further
+// apart than they are long, which spreads the 16 rows that a quarter of a wave reads over the banks.
+constexpr int kTinyThreads = 512, kTinyX = kTinyLong + 8, kTinyA = kTinyShort + 8;
+
+// The lane's 8 values of rows [r0, r0 + 32), k [k0, k0 + 16).
+__device__ inline f16x8 row_part(const uint16_t* m, uint32_t ld, uint32_t r0, uint32_t k0)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    return *(const f16x8*)(m + (r0 + (lane & 31)) * ld + k0 + 8 * (lane >> 5));
+}
+// The same of columns [c0, c0 + 32), k down the rows: 16 lanes name 4 rows of 16 values and each receives a column of them.
+__device__ inline f16x8 column_part(const uint16_t* m, uint32_t ld, uint32_t c0, uint32_t k0)
+{
+    typedef __attribute__((address_space(3))) i16x4* Ptr;
+    const uint32_t lane = threadIdx.x & 63;
+    i16x4 h[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint32_t k = k0 + 8 * (lane >> 5) + 4 * u + ((lane >> 2) & 3);
+        h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(m + k * ld + c0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)));
+    }
+    return __builtin_bit_cast(f16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+}
+__device__ inline void multiply2(f32x16& acc, const f16x8 (&a)[2], const f16x8 (&b)[2])
+{
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[1], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1], b[0], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[0], acc, 0, 0, 0);
+}
+__device__ inline f32x16 zeros()
+{
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0;
+    return z;
+}
+
+template <class G>
+__global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, const MuonPolynomial n)
+{
+    constexpr uint32_t kXPlane = kTinyShort * kTinyX, kAPlane = kTinyShort * kTinyA;
+    __shared__ __attribute__((aligned(16))) uint16_t s_x[2 * kXPlane], s_a[2 * kAPlane], s_b[2 * kAPlane];
+    __shared__ double s_wave[kTinyThreads / 64];
+    const MuonMatrix& m = a.m[blockIdx.x];
+    const uint32_t rows = m.rows, cols = m.cols, l32 = (max(rows, cols) + 31) & ~31u;
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool wide = rows <= cols;
+
+    // The update, in registers until its norm is known.
+    constexpr uint32_t kMost = kTinyShort * kTinyLong / 4 / kTinyThreads;
+    const uint32_t in_row = (cols + 3) / 4, all = rows * in_row;
+    const G* in = (const G*)m.in;
+    float* momentum = (float*)m.momentum;
+    const float cs = a.grad_scale ? *a.grad_scale : 1.0f;
+    f32x4 g[kMost], u[kMost];
+#pragma unroll
+    for (uint32_t i = 0; i < kMost; ++i) {
+        const uint32_t at = min(i * kTinyThreads + threadIdx.x, all - 1), row = at / in_row, c = at % in_row * 4;
+        g[i] = load_row(in + row * m.in_ld, c, cols);
+        if (momentum) u[i] = load_row(momentum + row * cols, c, cols);
+    }
+    for (uint32_t k = threadIdx.x; k < 2 * kXPlane / 8; k += kTinyThreads) ((uint4*)s_x)[k] = make_uint4(0, 0, 0, 0);
+    double sum = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kMost; ++i) {
+        const uint32_t at = i * kTinyThreads + threadIdx.x, row = at / in_row, c = at % in_row * 4;
+        if (at >= all) continue;
+        if (momentum) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float cg = cs * g[i][j];
+                u[i][j] = a.beta * u[i][j] + a.one_beta * cg;
+                g[i][j] = update(a, u[i][j], cg);
+            }
+            float* to = momentum + row * cols + c;
+            if (c + 4 <= cols)
+                *(f32x4_any*)to = u[i];
+            else
+#pragma unroll
+                for (uint32_t j = 0; j < 3; ++j)
+                    if (c + j < cols) to[j] = u[i][j];
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            if (c + j >= cols) g[i][j] = 0;
+            sum += (double)g[i][j] * (double)g[i][j];
+        }
+    }
+    sum = block_sum<kTinyThreads>(sum, s_wave); // and the zeros are there
+    const float over = (float)((double)kUp / (sqrt(sum) + a.eps));
+#pragma unroll
+    for (uint32_t i = 0; i < kMost; ++i) {
+        const uint32_t at = i * kTinyThreads + threadIdx.x, row = at / in_row, c = at % in_row * 4;
+        if (at >= all) continue;
+        uint2 hi, lo;
+        split2(g[i] * over, hi, lo);
+        if (wide) {
+            *(uint2*)(s_x + row * kTinyX + c) = hi;
+            *(uint2*)(s_x + kXPlane + row * kTinyX + c) = lo;
+        } else {
+            const u16x4 h = __builtin_bit_cast(u16x4, hi), l = __builtin_bit_cast(u16x4, lo);
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                if (c + j >= cols) continue;
+                s_x[(c + j) * kTinyX + row] = h[j];
+                s_x[kXPlane + (c + j) * kTinyX + row] = l[j];
+            }
+        }
+    }
+    __syncthreads();
+
+    // A 32 x 32 tile of P P^T for each of the first four waves.
+    auto square = [&](const uint16_t* p, uint32_t ld, uint32_t plane, uint32_t k, const uint16_t* c, uint16_t* out) {
+        if (wave < 4) {
+            const uint32_t p0 = 32 * (wave & 1), q0 = 32 * (wave >> 1);
+            f32x16 acc = zeros();
+            for (uint32_t k0 = 0; k0 < k; k0 += 16) {
+                const f16x8 x[2] = {row_part(p, ld, p0, k0), row_part(p + plane, ld, p0, k0)};
+                const f16x8 y[2] = {row_part(p, ld, q0, k0), row_part(p + plane, ld, q0, k0)};
+                multiply2(acc, x, y);
+            }
+            const uint32_t q = q0 + (lane & 31);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t p1 = p0 + 8 * r + 4 * half, at = q * kTinyA + p1;
+                f32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = acc[4 * r + j] * kDown;
+                if (c) {
+                    Planes old;
+                    old.load(c + at, kAPlane);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = n.cc * v[j] + n.cb * old.at(j) + (p1 + j == q ? n.ca * kUp : 0.0f);
+                }
+                uint2 hi, lo;
+                split2(v, hi, lo);
+                *(uint2*)(out + at) = hi;
+                *(uint2*)(out + kAPlane + at) = lo;
+            }
+        }
+        __syncthreads();
+    };
+    constexpr int kTiles = kTinyShort / 32 * (kTinyLong / 32) / (kTinyThreads / 64);
+    const uint32_t tiles = kTinyShort / 32 * (l32 / 32);
+    const LastEnd end = {(float*)m.master, (void*)m.out, m.out_ld, cols, rows, a.keep, m.scale, a.out_f32};
+    for (uint32_t step = 0; step < n.steps; ++step) {
+        const bool last = step + 1 == n.steps;
+        square(s_x, kTinyX, kXPlane, l32, nullptr, s_a);
+        square(s_a, kTinyA, kAPlane, kTinyShort, s_a, s_b);
+        f32x16 acc[kTiles];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+            const uint32_t t = i * (kTinyThreads / 64) + wave, i0 = 32 * (t & 1), j0 = 32 * (t >> 1);
+            acc[i] = zeros();
+            if (t >= tiles) continue;
+#pragma unroll
+            for (uint32_t k0 = 0; k0 < kTinyShort; k0 += 16) {
+                const f16x8 b[2] = {row_part(s_b, kTinyA, i0, k0), row_part(s_b + kAPlane, kTinyA, i0, k0)};
+                const f16x8 x[2] = {column_part(s_x, kTinyX, j0, k0), column_part(s_x + kXPlane, kTinyX, j0, k0)};
+                if (last && !wide) // as it lies: the short side across
+                    multiply2(acc[i], b, x);
+                else
+                    multiply2(acc[i], x, b);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+            const uint32_t t = i * (kTinyThreads / 64) + wave, i0 = 32 * (t & 1), j0 = 32 * (t >> 1);
+            if (t >= tiles) continue;
+            if (last) {
+                f32x16 one[1][1] = {{acc[i]}};
+                Finish<LastEnd, 1, 1>::run(end, Early<LastEnd, 1>(end, 0), one, wide ? j0 : i0, wide ? i0 : j0, 0, nullptr);
+                continue;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                f32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = acc[i][4 * r + j] * kDown;
+                uint2 hi, lo;
+                split2(v, hi, lo);
+                uint16_t* to = s_x + (i0 + (lane & 31)) * kTinyX + j0 + 8 * r + 4 * half;
+                *(uint2*)to = hi;
+                *(uint2*)(to + kXPlane) = lo;
+            }
+        }
+        __syncthreads();
+    }
+}
+
 // ---- shapes ----
 
-enum Size { kSmall, kMiddle, kLarge };
-constexpr uint32_t kSide[] = {64, 128, 256};
+// Workgroup tiles, and what a step of 64 values of k takes one of them (us) where each compute unit has one, and where all
+// have two, at once or one behind the other; and what two rounds take more for their first loads and ends.
+//   256 x 256, 8 waves of 64 x 128: 1.33 PFLOP/s on the planes while all units are busy
+//   128 x 128, 4 waves of 64 x 64, two workgroups a unit: 1.0 PFLOP/s
+//   128 x 128, 8 waves of 64 x 32, one workgroup a unit: for so few tiles that no unit has two (A of 2048 x 8192: 126 us,
+//              with 4 waves 167)
+//   64 x 64,   4 waves of 32 x 32, for few tiles and short k; three buffers, as its loads come from other XCDs' writes (a
+//              matrix of 777 x 1003: 202 us, with two 239)
+enum Size { kSmall, kMiddle, kAlone, kLarge };
+constexpr uint32_t kSide[] = {64, 128, 128, 256};
+constexpr struct {
+    double alone, both, round;
+} kTime[] = {{0.5, 1.0, 8}, {1.6, 3.1, 8}, {1.25, 0, 12}, {4.9, 9.8, 20}};
 
 template <bool PA, bool QA>
 using Large = Shape<2, 2, PA, QA, 256, 256, 4, 2, 32, 2, true>;
 template <bool PA, bool QA>
 using Middle = Shape<2, 2, PA, QA, 128, 128, 2, 2, 32, 2, true>;
 template <bool PA, bool QA>
-using Small = Shape<2, 2, PA, QA, 64, 64, 2, 1, 32, 3, true>;
+using Alone = Shape<2, 2, PA, QA, 128, 128, 2, 4, 64, 2, true>;
+template <bool PA, bool QA>
+using Small = Shape<2, 2, PA, QA, 64, 64, 2, 2, 64, 3, true>;
 
 uint64_t blocks(uint64_t x, uint32_t side) { return (x + side - 1) / side; }
 
@@ -526,16 +746,33 @@ uint64_t number(A& a, uint32_t round, F tiles)
     return all;
 }
 
-// The size of tiles that is done first, of products that have `tiles(m, side)` with `steps(m)` of 64 values of k each.
+// The size of tiles that is done first, of products that have `tiles(m, side)` with `steps(m)` of 64 values of k each, the
+// longest first.
 template <class A, class T, class K>
 Size size_of(const A& a, T tiles, K steps)
 {
-    for (int s = kLarge; s > kSmall; --s) {
-        uint64_t all = 0;
-        for (uint32_t i = 0; i < a.count; ++i) all += tiles(a.m[i], kSide[s]);
-        if (all >= 256) return (Size)s;
+    Size best = kSmall;
+    double least = 1e30;
+    for (int z = kSmall; z <= kLarge; ++z) {
+        const auto& c = kTime[z];
+        uint64_t all = 0, work = 0;
+        for (uint32_t i = 0; i < a.count; ++i) {
+            const uint64_t n = tiles(a.m[i], kSide[z]);
+            all += n;
+            work += n * steps(a.m[i]);
+        }
+        if (z == kAlone && all > 256) continue;
+        const double most = (double)steps(a.m[0]), mean = (double)work / (double)all;
+        const uint64_t pairs = all / 512, left = all % 512;
+        double t = (double)pairs * (mean * c.both + c.round);
+        if (left > 256)
+            t += mean * c.both + c.round;
+        else if (left)
+            t += mean * c.alone + c.round / 2;
+        t = std::max(t, most * c.alone + c.round / 2);
+        if (t < least) least = t, best = (Size)z;
     }
-    return kSmall;
+    return best;
 }
 
 template <class K>
@@ -556,11 +793,14 @@ hipError_t apply(MuonArgs& a, hipStream_t stream)
     const auto steps = [](const MuonMatrix& m) { return blocks(std::min(m.rows, m.cols), 64); };
     std::stable_sort(a.m, a.m + a.count, [&](const MuonMatrix& x, const MuonMatrix& y) { return steps(x) > steps(y); });
     const Size size = size_of(a, tiles, steps);
-    const uint64_t all = number(a, kXcds, [&](const MuonMatrix& m) { return tiles(m, kSide[size]); });
+    a.shares = steps(a.m[0]) != steps(a.m[a.count - 1]);
+    const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const MuonMatrix& m) { return tiles(m, kSide[size]); });
     using LT = std::conditional_t<kNext, Large<true, false>, Large<false, true>>;
+    using AT = std::conditional_t<kNext, Alone<true, false>, Alone<false, true>>;
     using MT = std::conditional_t<kNext, Middle<true, false>, Middle<false, true>>;
     using ST = std::conditional_t<kNext, Small<true, false>, Small<false, true>>;
     return size == kLarge    ? launch_tiles(apply_kernel<Large<true, false>, LT, End>, &a, all, LT::kThreads, stream)
+           : size == kAlone  ? launch_tiles(apply_kernel<Alone<true, false>, AT, End>, &a, all, AT::kThreads, stream)
            : size == kMiddle ? launch_tiles(apply_kernel<Middle<true, false>, MT, End>, &a, all, MT::kThreads, stream)
                              : launch_tiles(apply_kernel<Small<true, false>, ST, End>, &a, all, ST::kThreads, stream);
 }
@@ -572,6 +812,16 @@ hipError_t launch_muon_first(MuonArgs& a, hipStream_t stream)
     const uint64_t tiles = number(a, 1, [](const MuonMatrix& m) { return (uint64_t)m.part_n; });
     return a.in_f32 ? launch_tiles(first_kernel<float>, &a, tiles, kThreads, stream)
                     : launch_tiles(first_kernel<uint16_t>, &a, tiles, kThreads, stream);
+}
+
+hipError_t launch_muon_tiny(const MuonArgs& a, const MuonPolynomial& n, hipStream_t stream)
+{
+    if (a.count == 0 || a.count > kMuonMats) return hipErrorInvalidValue;
+    if (a.in_f32)
+        tiny_kernel<float><<<a.count, kTinyThreads, 0, stream>>>(a, n);
+    else
+        tiny_kernel<uint16_t><<<a.count, kTinyThreads, 0, stream>>>(a, n);
+    return hipGetLastError();
 }
 
 hipError_t launch_muon_pack(MuonArgs& a, hipStream_t stream)
@@ -593,8 +843,10 @@ hipError_t launch_muon_tri(TriArgs& a, hipStream_t stream)
     const auto steps = [](const TriMatrix& m) { return (uint64_t)m.k / 64; };
     std::stable_sort(a.m, a.m + a.count, [&](const TriMatrix& x, const TriMatrix& y) { return x.k > y.k; });
     const Size size = size_of(a, tiles, steps);
-    const uint64_t all = number(a, kXcds, [&](const TriMatrix& m) { return tiles(m, kSide[size]); });
+    a.shares = steps(a.m[0]) != steps(a.m[a.count - 1]);
+    const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const TriMatrix& m) { return tiles(m, kSide[size]); });
     return size == kLarge    ? launch_tiles(tri_kernel<Large<false, false>>, &a, all, Large<false, false>::kThreads, stream)
+           : size == kAlone  ? launch_tiles(tri_kernel<Alone<false, false>>, &a, all, Alone<false, false>::kThreads, stream)
            : size == kMiddle ? launch_tiles(tri_kernel<Middle<false, false>>, &a, all, Middle<false, false>::kThreads, stream)
                              : launch_tiles(tri_kernel<Small<false, false>>, &a, all, Small<false, false>::kThreads, stream);
 }

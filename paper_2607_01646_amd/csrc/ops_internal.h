@@ -206,7 +206,7 @@ struct MuonArgs {
     float beta, one_beta, keep;
     double eps;
     const float* grad_scale;
-    bool nesterov, in_f32, out_f32;
+    bool nesterov, in_f32, out_f32, shares;
 };
 // Symmetric products out = ca I + cb c + cc p q, p q^T of rows of k values; c == 0: cc p q alone.
 struct TriMatrix {
@@ -217,7 +217,15 @@ struct TriArgs {
     TriMatrix m[kMuonMats];
     uint32_t count;
     float ca, cb, cc;
+    bool shares;
 };
+// Matrices of at most these sides: all of the step in one launch, which uses no workspace.
+constexpr uint32_t kTinyShort = 64, kTinyLong = 256;
+struct MuonPolynomial {
+    float ca, cb, cc;
+    uint32_t steps;
+};
+hipError_t launch_muon_tiny(const MuonArgs& a, const MuonPolynomial& n, hipStream_t stream);
 // Elements of the tiles of the launches that are not products.
 constexpr uint32_t kMuonRows = 16, kMuonCols = 256, kMuonTurn = 64;
 // Momentum, and the squares of the update.

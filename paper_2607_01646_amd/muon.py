@@ -84,7 +84,7 @@ def ckpt_orthogonalize(matrices, steps=5, coefficients=COEFFICIENTS, eps=1e-7, p
     singular values taken to about 1: each is divided by its 2-norm + eps and
     goes `steps` times through a x + b x^3 + c x^5 of its singular values.  A
     list of new tensors, or `out` (which may be the matrices themselves).
-    piece_bytes bounds the workspace (0 = 2 GiB, at least one matrix's)."""
+    piece_bytes bounds the workspace (0 = 4 GiB, at least one matrix's)."""
     matrices = _listed(matrices)
     ns = _ns(steps, coefficients, eps, piece_bytes)
     if out is not None:
