@@ -160,13 +160,13 @@ ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schul
         if (err != hipSuccess) return fail_free(CKPT_EHIP, "orthogonalisation: %s", hipGetErrorString(err));
     }
     const bool twos = in_twos(ns);
-    const uint64_t w = (uint64_t)(uintptr_t)workspace;
+    uint8_t* w = (uint8_t*)workspace;
     return grouped(jobs, ns.piece_bytes, &need, [&](size_t first, size_t last) {
         a.count = (uint32_t)(last - first);
         for (size_t k = first; k < last; ++k) {
             a.m[k - first] = jobs[k].m;
-            a.m[k - first].part = w + jobs[k].part;
-            a.m[k - first].x = w + jobs[k].x;
+            a.m[k - first].part = (double*)(w + jobs[k].part);
+            a.m[k - first].x = (uint16_t*)(w + jobs[k].x);
         }
         hipError_t err = launch_muon_first(a, s);
         if (err == hipSuccess) err = launch_muon_pack(a, s);
@@ -180,7 +180,8 @@ ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schul
             t.cc = poly ? (float)ns.c : 1.0f;
             for (size_t k = first; k < last; ++k) {
                 const Job& j = jobs[k];
-                t.m[k - first] = {w + j.*p, w + j.*q, poly ? w + j.*p : 0, w + j.*out, (uint32_t)j.s,
+                const auto at = [&](uint64_t Job::*o) { return (uint16_t*)(w + j.*o); };
+                t.m[k - first] = {at(p), at(q), poly ? at(p) : nullptr, at(out), (uint32_t)j.s,
                                   (uint32_t)up(p == &Job::x || p == &Job::y ? j.l : j.s, 64), 0, 0};
             }
             err = launch_muon_tri(t, s);
@@ -203,9 +204,9 @@ ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schul
             for (size_t k = first; k < last; ++k) {
                 MuonMatrix& m = a.m[k - first];
                 m = jobs[k].m;
-                m.x = w + jobs[k].*x;
-                m.y = w + jobs[k].*y;
-                m.f = w + jobs[k].*f;
+                m.x = (uint16_t*)(w + jobs[k].*x);
+                m.y = (uint16_t*)(w + jobs[k].*y);
+                m.f = (uint16_t*)(w + jobs[k].*f);
             }
             err = launch_muon_apply(a, step == ns.steps, s);
         }
@@ -325,9 +326,9 @@ extern "C" ckpt_status ckpt_orthogonalize(const ckpt_matrix* m, uint32_t n, uint
             span(m[i].out, m[i].out_stride, true);
             if (m[i].in != m[i].out || (rows > 1 && m[i].in_stride != m[i].out_stride)) span(m[i].in, m[i].in_stride, false);
             MuonMatrix& to = jobs[at++].m;
-            to.in = (uint64_t)(uintptr_t)m[i].in;
+            to.in = m[i].in;
             to.in_ld = m[i].in_stride;
-            to.out = (uint64_t)(uintptr_t)m[i].out;
+            to.out = m[i].out;
             to.out_ld = m[i].out_stride;
         }
         if (jobs.empty()) return CKPT_OK;
@@ -389,10 +390,10 @@ extern "C" ckpt_status ckpt_muon(const ckpt_muon_matrix* m, uint32_t n, const ck
                 spans.push_back({p, p + all * x.e, x.written});
             }
             MuonMatrix& to = jobs[at++].m;
-            to.in = (uint64_t)(uintptr_t)m[i].grad;
-            to.momentum = (uint64_t)(uintptr_t)m[i].momentum;
-            to.master = (uint64_t)(uintptr_t)m[i].master;
-            to.out = (uint64_t)(uintptr_t)m[i].param;
+            to.in = m[i].grad;
+            to.momentum = m[i].momentum;
+            to.master = m[i].master;
+            to.out = m[i].param;
             to.in_ld = to.out_ld = m[i].cols;
             to.scale = (float)(args->lr * m[i].scale);
         }

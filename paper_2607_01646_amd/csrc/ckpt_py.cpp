@@ -10,9 +10,13 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/version.h>
 
+#include <algorithm>
+#include <cmath>
 #include <vector>
 
 #include "../../include/ckpt.h"
+#include "../../include/ckpt_embed.h"
+#include "../../include/ckpt_muon.h"
 #include "../../include/ckpt_ops.h"
 
 namespace {
@@ -337,7 +341,292 @@ PyObject* linear_loss(PyObject*, PyObject* const* args, Py_ssize_t n_args)
     return Py_BuildValue("iNNNNN", (int)rc, wrap(loss), wrap(token_loss), wrap(lse), wrap(d_hidden), wrap(d_weight));
 }
 
+using MuonWorkFn = ckpt_status (*)(const ckpt_muon_matrix*, uint32_t, const ckpt_muon_args*, uint64_t*);
+using MuonFn = ckpt_status (*)(const ckpt_muon_matrix*, uint32_t, const ckpt_muon_args*, int32_t, void*, uint64_t, void*);
+
+// muon(workspace function's address, step function's address, params, masters,
+// momentums, grads, lr, momentum, nesterov, weight_decay, scale's rule (0 rms,
+// 1 spectral, 2 the number), scale, steps, a, b, c, eps, grad_scale,
+// piece_bytes, stream handle) -> status.  Allocates on torch's current stream.
+PyObject* muon(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    if (n_args != 20) {
+        PyErr_SetString(PyExc_TypeError, "muon takes 20 arguments");
+        return nullptr;
+    }
+    for (int k = 2; k < 6; ++k)
+        if (!PyList_CheckExact(args[k]) && !PyTuple_CheckExact(args[k])) Py_RETURN_NONE;
+    const unsigned long long work_fn = PyLong_AsUnsignedLongLong(args[0]), fn = PyLong_AsUnsignedLongLong(args[1]);
+    ckpt_muon_args a = {};
+    a.lr = PyFloat_AsDouble(args[6]);
+    a.momentum = PyFloat_AsDouble(args[7]);
+    const int nesterov = PyObject_IsTrue(args[8]);
+    a.weight_decay = PyFloat_AsDouble(args[9]);
+    const long rule = PyLong_AsLong(args[10]);
+    const double number = PyFloat_AsDouble(args[11]);
+    const unsigned long long steps = PyLong_AsUnsignedLongLong(args[12]);
+    a.ns.a = PyFloat_AsDouble(args[13]);
+    a.ns.b = PyFloat_AsDouble(args[14]);
+    a.ns.c = PyFloat_AsDouble(args[15]);
+    a.ns.eps = PyFloat_AsDouble(args[16]);
+    a.ns.piece_bytes = PyLong_AsUnsignedLongLong(args[18]);
+    const unsigned long long stream = PyLong_AsUnsignedLongLong(args[19]);
+    if (PyErr_Occurred() || nesterov < 0 || steps > 64) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    a.nesterov = nesterov != 0;
+    a.ns.steps = (uint32_t)steps;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(args[2]);
+    if (n == 0 || (uint64_t)n > UINT32_MAX) Py_RETURN_NONE;
+    int32_t device = 0;
+    std::vector<ckpt_muon_matrix> m;
+    at::Tensor work;
+    uint64_t bytes = 0;
+    ckpt_status rc;
+    try {
+        m.resize((size_t)n);
+        if (!read_scalar(args[17], &a.grad_scale)) Py_RETURN_NONE;
+        PyObject* const* items[4];
+        for (int k = 0; k < 4; ++k) {
+            if (PySequence_Fast_GET_SIZE(args[2 + k]) != n) Py_RETURN_NONE;
+            items[k] = PySequence_Fast_ITEMS(args[2 + k]);
+        }
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            const at::Tensor* t[4];
+            for (int k = 0; k < 4; ++k) {
+                t[k] = plain(items[k][i]);
+                if (!t[k] || !t[k]->is_contiguous()) Py_RETURN_NONE;
+                const uint32_t type = type_of(*t[k]);
+                if (k == 0 || k == 3) {
+                    uint32_t& want = k ? a.grad_dtype : a.param_dtype;
+                    if (i == 0) want = type;
+                    if (type == 0 || type != want) Py_RETURN_NONE;
+                } else if (type != CKPT_TYPE_F32) {
+                    Py_RETURN_NONE;
+                }
+                if (i == 0 && k == 0) device = t[0]->get_device();
+                if (t[k]->get_device() != device || t[k]->numel() != t[0]->numel() ||
+                    (t[k]->dim() != 1 && t[k]->sizes() != t[0]->sizes()))
+                    Py_RETURN_NONE;
+            }
+            if (t[0]->dim() < 2) Py_RETURN_NONE;
+            const uint64_t all = (uint64_t)t[0]->numel();
+            m[i].rows = (uint64_t)t[0]->size(0);
+            m[i].cols = m[i].rows ? all / m[i].rows : 0;
+            if (all) {
+                m[i].param = t[0]->data_ptr();
+                m[i].master = (float*)t[1]->data_ptr();
+                m[i].momentum = (float*)t[2]->data_ptr();
+                m[i].grad = t[3]->data_ptr();
+            }
+            const double r = (double)m[i].rows, c = (double)m[i].cols;
+            m[i].scale = rule == 0 ? 0.2 * std::sqrt(std::max(r, c)) : rule == 1 ? (c > 0 ? std::sqrt(std::max(1.0, r / c)) : 1.0) : number;
+            if (i + 1 == n) {
+                rc = ((MuonWorkFn)(uintptr_t)work_fn)(m.data(), (uint32_t)n, &a, &bytes);
+                if (rc == CKPT_OK && bytes) work = at::empty({(int64_t)bytes}, t[0]->options().dtype(at::kByte));
+            }
+        }
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    if (rc == CKPT_OK) {
+        Py_BEGIN_ALLOW_THREADS;
+        rc = ((MuonFn)(uintptr_t)fn)(m.data(), (uint32_t)n, &a, device, bytes ? work.data_ptr() : nullptr, bytes,
+                                     (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS;
+    }
+    return PyLong_FromLong(rc);
+}
+
+using OrthWorkFn = ckpt_status (*)(const ckpt_matrix*, uint32_t, const ckpt_newton_schulz*, uint64_t*);
+using OrthFn = ckpt_status (*)(const ckpt_matrix*, uint32_t, uint32_t, const ckpt_newton_schulz*, int32_t, void*, uint64_t, void*);
+
+// orthogonalize(workspace function's address, function's address, matrices,
+// steps, a, b, c, eps, piece_bytes, stream handle) -> (status, results).
+// Allocates on torch's current stream.
+PyObject* orthogonalize(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    if (n_args != 10) {
+        PyErr_SetString(PyExc_TypeError, "orthogonalize takes 10 arguments");
+        return nullptr;
+    }
+    if (!PyList_CheckExact(args[2]) && !PyTuple_CheckExact(args[2])) Py_RETURN_NONE;
+    const unsigned long long work_fn = PyLong_AsUnsignedLongLong(args[0]), fn = PyLong_AsUnsignedLongLong(args[1]);
+    ckpt_newton_schulz ns = {};
+    const unsigned long long steps = PyLong_AsUnsignedLongLong(args[3]);
+    ns.a = PyFloat_AsDouble(args[4]);
+    ns.b = PyFloat_AsDouble(args[5]);
+    ns.c = PyFloat_AsDouble(args[6]);
+    ns.eps = PyFloat_AsDouble(args[7]);
+    ns.piece_bytes = PyLong_AsUnsignedLongLong(args[8]);
+    const unsigned long long stream = PyLong_AsUnsignedLongLong(args[9]);
+    if (PyErr_Occurred() || steps > 64) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    ns.steps = (uint32_t)steps;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(args[2]);
+    PyObject* const* items = PySequence_Fast_ITEMS(args[2]);
+    if (n == 0 || (uint64_t)n > UINT32_MAX) Py_RETURN_NONE;
+    int32_t device = 0;
+    uint32_t type = 0;
+    std::vector<ckpt_matrix> m;
+    std::vector<at::Tensor> out;
+    at::Tensor work;
+    uint64_t bytes = 0;
+    ckpt_status rc;
+    try {
+        m.resize((size_t)n);
+        out.reserve((size_t)n);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            const at::Tensor* t = plain(items[i]);
+            if (!t || t->dim() != 2 || t->numel() == 0) Py_RETURN_NONE;
+            if (i == 0) {
+                type = type_of(*t);
+                device = t->get_device();
+            }
+            if (type == 0 || type_of(*t) != type || t->get_device() != device) Py_RETURN_NONE;
+            if (!read_rows(*t, &m[i].rows, &m[i].cols, &m[i].in_stride)) Py_RETURN_NONE;
+            out.push_back(at::empty(t->sizes(), t->options()));
+            m[i].in = t->data_ptr();
+            m[i].out = out.back().data_ptr();
+            m[i].out_stride = m[i].cols;
+        }
+        rc = ((OrthWorkFn)(uintptr_t)work_fn)(m.data(), (uint32_t)n, &ns, &bytes);
+        if (rc == CKPT_OK && bytes) work = at::empty({(int64_t)bytes}, out[0].options().dtype(at::kByte));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    if (rc == CKPT_OK) {
+        Py_BEGIN_ALLOW_THREADS;
+        rc = ((OrthFn)(uintptr_t)fn)(m.data(), (uint32_t)n, type, &ns, device, bytes ? work.data_ptr() : nullptr, bytes,
+                                     (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS;
+    }
+    PyObject* list = PyList_New(n);
+    if (!list) return nullptr;
+    for (Py_ssize_t i = 0; i < n; ++i) PyList_SET_ITEM(list, i, THPVariable_Wrap(out[(size_t)i]));
+    return Py_BuildValue("iN", (int)rc, list);
+}
+
+using EmbedFn = ckpt_status (*)(const ckpt_embed_args*, int32_t, void*);
+using EmbedWorkFn = ckpt_status (*)(const ckpt_embed_args*, uint64_t*);
+using EmbedGradFn = ckpt_status (*)(const ckpt_embed_args*, int32_t, void*, uint64_t, void*);
+
+const at::Tensor* read_ids(PyObject* o, const at::Tensor& with)
+{
+    const at::Tensor* t = plain(o);
+    return t && t->scalar_type() == at::kLong && t->is_contiguous() && t->device() == with.device() ? t : nullptr;
+}
+
+// embedding(function's address, table, ids, scale, ignore_index, stream
+// handle) -> (status, rows).  Allocates on torch's current stream.
+PyObject* embedding(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    if (n_args != 6) {
+        PyErr_SetString(PyExc_TypeError, "embedding takes 6 arguments");
+        return nullptr;
+    }
+    const unsigned long long fn = PyLong_AsUnsignedLongLong(args[0]), stream = PyLong_AsUnsignedLongLong(args[5]);
+    ckpt_embed_args a = {};
+    a.scale = PyFloat_AsDouble(args[3]);
+    a.ignore_index = PyLong_AsLongLong(args[4]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    at::Tensor rows;
+    int32_t device = 0;
+    try {
+        const at::Tensor* table = plain(args[1]);
+        if (!table || table->dim() != 2 || !(a.dtype = a.table_dtype = type_of(*table))) Py_RETURN_NONE;
+        const at::Tensor* ids = read_ids(args[2], *table);
+        if (!ids || !read_rows(*table, &a.vocab, &a.dim, &a.table_stride)) Py_RETURN_NONE;
+        device = table->get_device();
+        a.tokens = (uint64_t)ids->numel();
+        std::vector<int64_t> shape(ids->sizes().begin(), ids->sizes().end());
+        shape.push_back((int64_t)a.dim);
+        rows = at::empty(shape, table->options());
+        a.rows_stride = a.dim;
+        a.table = table->data_ptr();
+        a.ids = a.tokens ? (const int64_t*)ids->data_ptr() : nullptr;
+        a.rows = a.tokens ? rows.data_ptr() : nullptr;
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    ckpt_status rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = ((EmbedFn)(uintptr_t)fn)(&a, device, (void*)(uintptr_t)stream);
+    Py_END_ALLOW_THREADS;
+    return Py_BuildValue("iN", (int)rc, THPVariable_Wrap(rows));
+}
+
+// embedding_grad(workspace function's address, function's address, d_rows,
+// ids, vocab, scale, ignore_index, add_to or None, stream handle) -> (status,
+// table).  Allocates on torch's current stream.
+PyObject* embedding_grad(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    if (n_args != 9) {
+        PyErr_SetString(PyExc_TypeError, "embedding_grad takes 9 arguments");
+        return nullptr;
+    }
+    const unsigned long long work_fn = PyLong_AsUnsignedLongLong(args[0]), fn = PyLong_AsUnsignedLongLong(args[1]);
+    const unsigned long long stream = PyLong_AsUnsignedLongLong(args[8]);
+    ckpt_embed_args a = {};
+    a.vocab = PyLong_AsUnsignedLongLong(args[4]);
+    a.scale = PyFloat_AsDouble(args[5]);
+    a.ignore_index = PyLong_AsLongLong(args[6]);
+    if (PyErr_Occurred() || a.vocab == 0 || a.vocab > (1u << 22)) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    at::Tensor table, work;
+    int32_t device = 0;
+    uint64_t bytes = 0;
+    ckpt_status rc;
+    try {
+        const at::Tensor* d = plain(args[2]);
+        if (!d || d->dim() < 1 || !(a.dtype = type_of(*d))) Py_RETURN_NONE;
+        const at::Tensor* ids = read_ids(args[3], *d);
+        if (!ids || ids->sizes() != d->sizes().slice(0, d->dim() - 1) ||
+            !read_rows(*d, &a.tokens, &a.dim, &a.rows_stride))
+            Py_RETURN_NONE;
+        device = d->get_device();
+        if (args[7] == Py_None) {
+            table = at::empty({(int64_t)a.vocab, (int64_t)a.dim}, d->options());
+            a.table_stride = a.dim;
+        } else {
+            const at::Tensor* t = plain(args[7]);
+            uint64_t rows = 0, cols = 0;
+            if (!t || t->dim() != 2 || t->device() != d->device() || !read_rows(*t, &rows, &cols, &a.table_stride) ||
+                rows != a.vocab || cols != a.dim)
+                Py_RETURN_NONE;
+            table = *t;
+            a.add = 1;
+        }
+        if (!(a.table_dtype = type_of(table))) Py_RETURN_NONE;
+        a.table = table.data_ptr();
+        a.ids = a.tokens ? (const int64_t*)ids->data_ptr() : nullptr;
+        a.rows = a.tokens ? d->data_ptr() : nullptr;
+        rc = ((EmbedWorkFn)(uintptr_t)work_fn)(&a, &bytes);
+        if (rc == CKPT_OK) work = at::empty({(int64_t)bytes}, d->options().dtype(at::kByte));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    if (rc == CKPT_OK) {
+        Py_BEGIN_ALLOW_THREADS;
+        rc = ((EmbedGradFn)(uintptr_t)fn)(&a, device, work.data_ptr(), bytes, (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS;
+    }
+    return Py_BuildValue("iN", (int)rc, THPVariable_Wrap(table));
+}
+
 PyMethodDef methods[] = {{"adamw", (PyCFunction)(void (*)(void))adamw, METH_FASTCALL, nullptr},
+                         {"embedding", (PyCFunction)(void (*)(void))embedding, METH_FASTCALL, nullptr},
+                         {"embedding_grad", (PyCFunction)(void (*)(void))embedding_grad, METH_FASTCALL, nullptr},
+                         {"muon", (PyCFunction)(void (*)(void))muon, METH_FASTCALL, nullptr},
+                         {"orthogonalize", (PyCFunction)(void (*)(void))orthogonalize, METH_FASTCALL, nullptr},
                          {"grad_norm", (PyCFunction)(void (*)(void))grad_norm, METH_FASTCALL, nullptr},
                          {"linear_loss", (PyCFunction)(void (*)(void))linear_loss, METH_FASTCALL, nullptr},
                          {"pack_noalloc", (PyCFunction)(void (*)(void))pack_noalloc, METH_FASTCALL, nullptr},

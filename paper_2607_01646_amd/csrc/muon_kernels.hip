@@ -38,16 +38,47 @@ __device__ inline f32x4 load4(const uint16_t* p)
 __device__ inline float load1(const float* p) { return *p; }
 __device__ inline float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 
-// Values c .. c + 3 of a row of `cols`, zeros past its end.
-template <class T>
-__device__ inline f32x4 load_row(const T* row, uint32_t c, uint32_t cols)
+// Values c[i] .. c[i] + 3 of rows of `cols`, zeros past their ends.  The loads are in no branch of their own, which each
+// would wait for what it loads: those that would go past the end begin before it.
+template <int N, class T>
+__device__ inline void load_rows(const T* const (&row)[N], const uint32_t (&c)[N], uint32_t cols, f32x4 (&v)[N])
 {
-    if (c + 4 <= cols) return load4(row + c);
-    f32x4 r = {0, 0, 0, 0};
+    if (cols < 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) v[i][j] = load1(row[i] + min(c[i] + j, cols - 1));
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) v[i][j] = c[i] + j < cols ? v[i][j] : 0.0f;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = load4(row[i] + min(c[i], cols - 4));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t by = c[i] - min(c[i], cols - 4);
+        if (by & 1) v[i] = {v[i][1], v[i][2], v[i][3], 0};
+        if (by & 2) v[i] = {v[i][2], v[i][3], 0, 0};
+        if (by >= 4) v[i] = {0, 0, 0, 0};
+    }
+}
+
+__device__ inline void store4(float* p, f32x4 x) { *(f32x4_any*)p = x; }
+__device__ inline void store4(uint16_t* p, f32x4 x)
+{
+    *(u16x4_any*)p = u16x4{bf16_of(x[0]), bf16_of(x[1]), bf16_of(x[2]), bf16_of(x[3])};
+}
+__device__ inline void store1(float* p, float x) { *p = x; }
+__device__ inline void store1(uint16_t* p, float x) { *p = bf16_of(x); }
+template <class T>
+__device__ inline void store_row(T* row, uint32_t c, uint32_t cols, f32x4 x)
+{
+    if (c + 4 <= cols) return store4(row + c, x);
 #pragma unroll
     for (uint32_t j = 0; j < 3; ++j)
-        if (c + j < cols) r[j] = load1(row + c + j);
-    return r;
+        if (c + j < cols) store1(row + c + j, x[j]);
 }
 
 // x as hi + lo, each to nearest.
@@ -109,15 +140,20 @@ __global__ __launch_bounds__(kThreads) void first_kernel(const MuonArgs a)
     const uint32_t r0 = t / nc * kMuonRows + (threadIdx.x >> 6) * 4, c = t % nc * kMuonCols + (threadIdx.x & 63) * 4;
     const uint64_t ld = a.m[f].in_ld;
     const G* in = (const G*)a.m[f].in;
-    float* momentum = (float*)a.m[f].momentum;
+    float* momentum = a.m[f].momentum;
     const float cs = a.grad_scale ? *a.grad_scale : 1.0f;
     f32x4 g[4], m[4];
+    const G* from[4];
+    const float* old[4];
+    const uint32_t cs4[4] = {c, c, c, c};
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
         const uint64_t row = min(r0 + i, rows - 1);
-        g[i] = load_row(in + row * ld, c, cols);
-        if (momentum) m[i] = load_row(momentum + row * cols, c, cols);
+        from[i] = in + row * ld;
+        old[i] = momentum + row * cols;
     }
+    if (momentum) load_rows(old, cs4, cols, m);
+    load_rows(from, cs4, cols, g);
     double sum = 0;
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
@@ -129,20 +165,14 @@ __global__ __launch_bounds__(kThreads) void first_kernel(const MuonArgs a)
                 m[i][j] = a.beta * m[i][j] + a.one_beta * cg;
                 g[i][j] = update(a, m[i][j], cg);
             }
-            float* to = momentum + (uint64_t)(r0 + i) * cols + c;
-            if (c + 4 <= cols)
-                *(f32x4_any*)to = m[i];
-            else
-#pragma unroll
-                for (uint32_t j = 0; j < 3; ++j)
-                    if (c + j < cols) to[j] = m[i][j];
+            store_row(momentum + (uint64_t)(r0 + i) * cols, c, cols, m[i]);
         }
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j)
             if (c + j < cols) sum += (double)g[i][j] * (double)g[i][j]; // (zero gradients past the end need not be zero updates)
     }
     sum = block_sum(sum, s_wave);
-    if (threadIdx.x == 0) ((double*)a.m[f].part)[t] = sum;
+    if (threadIdx.x == 0) a.m[f].part[t] = sum;
 }
 
 template <class G>
@@ -155,28 +185,36 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const MuonArgs a)
     const uint32_t s = min(rows, cols), ldx = up64(max(rows, cols));
     const uint64_t plane = (uint64_t)s * ldx, ld = a.m[f].in_ld;
     const G* in = (const G*)a.m[f].in;
-    const float* momentum = (const float*)a.m[f].momentum;
+    const float* momentum = a.m[f].momentum;
     const float cs = a.grad_scale ? *a.grad_scale : 1.0f;
-    uint16_t* x = (uint16_t*)a.m[f].x;
+    uint16_t* x = a.m[f].x;
     double sum = 0;
-    for (uint32_t k = threadIdx.x; k < a.m[f].part_n; k += kThreads) sum += ((const double*)a.m[f].part)[k];
+    for (uint32_t k = threadIdx.x; k < a.m[f].part_n; k += kThreads) sum += a.m[f].part[k];
     sum = block_sum(sum, s_wave);
     const float over = (float)((double)kUp / (sqrt(sum) + a.eps));
-    // Four values of U over its norm.
-    auto values = [&](uint32_t row, uint32_t c) {
-        const bool any = row < rows && c < cols;
-        const uint64_t r = any ? row : 0;
-        f32x4 v = {0, 0, 0, 0};
-        if (!any) return v;
-        if (!momentum || a.nesterov) v = load_row(in + r * ld, c, cols);
-        if (momentum) {
-            const f32x4 m = load_row(momentum + r * cols, c, cols);
+    // Runs of four values of U over its norm, of the rows r0, r0 + by, ..; zeros outside the matrix.
+    auto values = [&](uint32_t r0, uint32_t by, uint32_t c, f32x4 (&v)[4]) {
+        const G* from[4];
+        const float* old[4];
+        const uint32_t cs4[4] = {c, c, c, c};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = update(a, m[j], cs * v[j]);
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint64_t row = min(r0 + i * by, rows - 1);
+            from[i] = in + row * ld;
+            old[i] = momentum + row * cols;
         }
+        f32x4 m[4];
+        if (momentum) load_rows(old, cs4, cols, m);
+        if (!momentum || a.nesterov) load_rows(from, cs4, cols, v);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = c + j < cols ? v[j] * over : 0.0f;
-        return v;
+        for (uint32_t i = 0; i < 4; ++i) {
+            if (momentum) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][j] = update(a, m[i][j], cs * v[i][j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] = r0 + i * by < rows && c + j < cols ? v[i][j] * over : 0.0f;
+        }
     };
     auto store = [&](uint64_t at, f32x4 v) {
         uint2 hi, lo;
@@ -189,8 +227,7 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const MuonArgs a)
         const uint32_t r0 = t / nc * kMuonRows + (threadIdx.x >> 6) * 4, c = t % nc * kMuonCols + (threadIdx.x & 63) * 4;
         if (c >= ldx) return;
         f32x4 v[4];
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) v[i] = values(r0 + i, c);
+        values(r0, 1, c, v);
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
             if (r0 + i < rows) store((uint64_t)(r0 + i) * ldx + c, v[i]);
@@ -201,8 +238,7 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const MuonArgs a)
     const uint32_t r0 = t / nc * kMuonTurn, c0 = t % nc * kMuonTurn;
     const uint32_t at = (threadIdx.x & 15) * 4, line = threadIdx.x >> 4;
     f32x4 v[4];
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) v[i] = values(r0 + line + 16 * i, c0 + at);
+    values(r0 + line, 16, c0 + at, v);
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i)
 #pragma unroll
@@ -408,16 +444,15 @@ struct Finish<LastEnd, TP, TQ> {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             v[r] = old[r] * e.keep - v[r] * e.lr;
-                            *(f32x4_any*)(w + 8 * r) = v[r];
+                            store4(w + 8 * r, v[r]);
                         }
                     }
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (e.f32)
-                            *(f32x4_any*)((float*)e.out + to + 8 * r) = v[r];
+                            store4((float*)e.out + to + 8 * r, v[r]);
                         else
-                            *(u16x4_any*)((uint16_t*)e.out + to + 8 * r) =
-                                u16x4{bf16_of(v[r][0]), bf16_of(v[r][1]), bf16_of(v[r][2]), bf16_of(v[r][3])};
+                            store4((uint16_t*)e.out + to + 8 * r, v[r]);
                     continue;
                 }
 #pragma unroll
@@ -475,10 +510,10 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads >= 512 ? 2 : 1) void tri_k
     while (i * (i + 1) / 2 > t) --i;
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
     const uint32_t j = t - i * (i + 1) / 2;
-    const Operand P = {(const uint16_t*)m.p, (uint64_t)m.s * m.k, m.k, m.s, m.k};
-    const Operand Q = {(const uint16_t*)m.q, (uint64_t)m.s * m.k, m.k, m.s, m.k};
+    const Operand P = {m.p, (uint64_t)m.s * m.k, m.k, m.s, m.k};
+    const Operand Q = {m.q, (uint64_t)m.s * m.k, m.k, m.s, m.k};
     const uint32_t ld = up64(m.s);
-    const TriEnd end = {(uint16_t*)m.out, (const uint16_t*)m.c, (uint64_t)m.s * ld, m.s, ld, a.ca, a.cb, a.cc};
+    const TriEnd end = {m.out, m.c, (uint64_t)m.s * ld, m.s, ld, a.ca, a.cb, a.cc};
     product<S>(P, Q, {m.s, m.s, m.k, 1, false}, end, make_uint2(__builtin_amdgcn_readfirstlane(j), __builtin_amdgcn_readfirstlane(i)),
                t, 0, s0, s1, s2, s3);
 }
@@ -498,13 +533,13 @@ __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply
     if (!tile_in(a.shares, at - m.first, ns * nl, t)) return;
     const uint32_t band = t / (kBand * np), in = t % (kBand * np), width = min(kBand, nq - band * kBand);
     const uint2 tile = make_uint2(in / width, band * kBand + in % width);
-    const Operand X = {(const uint16_t*)m.x, (uint64_t)s * ldx, ldx, s, ldx};
-    const Operand B = {(const uint16_t*)m.f, (uint64_t)s * lda, lda, s, lda};
+    const Operand X = {m.x, (uint64_t)s * ldx, ldx, s, ldx};
+    const Operand B = {m.f, (uint64_t)s * lda, lda, s, lda};
     if constexpr (std::is_same_v<End, NextEnd>) {
-        const NextEnd end = {(uint16_t*)m.y, (uint64_t)s * ldx, s, ldx};
+        const NextEnd end = {m.y, (uint64_t)s * ldx, s, ldx};
         product<W>(X, B, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3);
     } else {
-        const LastEnd end = {(float*)m.master, (void*)m.out, m.out_ld, p, q, a.keep, m.scale, a.out_f32};
+        const LastEnd end = {m.master, m.out, m.out_ld, p, q, a.keep, m.scale, a.out_f32};
         if (wide)
             product<W>(X, B, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3);
         else
@@ -520,13 +555,14 @@ __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply
 // apart than they are long, which spreads the 16 rows that a quarter of a wave reads over the banks.
 constexpr int kTinyThreads = 512, kTinyX = kTinyLong + 8, kTinyA = kTinyShort + 8;
 
-// The lane's 8 values of rows [r0, r0 + 32), k [k0, k0 + 16).
+// Products of 16 x 16 x 32: there are tiles enough for each wave to have several sums on their way.
+// The lane's 8 values of rows [r0, r0 + 16), k [k0, k0 + 32): row lane % 16, k 8 (lane / 16) + 0..7.
 __device__ inline f16x8 row_part(const uint16_t* m, uint32_t ld, uint32_t r0, uint32_t k0)
 {
     const uint32_t lane = threadIdx.x & 63;
-    return *(const f16x8*)(m + (r0 + (lane & 31)) * ld + k0 + 8 * (lane >> 5));
+    return *(const f16x8*)(m + (r0 + (lane & 15)) * ld + k0 + 8 * (lane >> 4));
 }
-// The same of columns [c0, c0 + 32), k down the rows: 16 lanes name 4 rows of 16 values and each receives a column of them.
+// The same of columns [c0, c0 + 16), k down the rows: 16 lanes name 4 rows of 16 values and each receives a column of them.
 __device__ inline f16x8 column_part(const uint16_t* m, uint32_t ld, uint32_t c0, uint32_t k0)
 {
     typedef __attribute__((address_space(3))) i16x4* Ptr;
@@ -534,23 +570,17 @@ __device__ inline f16x8 column_part(const uint16_t* m, uint32_t ld, uint32_t c0,
     i16x4 h[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        const uint32_t k = k0 + 8 * (lane >> 5) + 4 * u + ((lane >> 2) & 3);
-        h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(m + k * ld + c0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)));
+        const uint32_t k = k0 + 8 * (lane >> 4) + 4 * u + ((lane >> 2) & 3);
+        h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(m + k * ld + c0 + 4 * (lane & 3)));
     }
     return __builtin_bit_cast(f16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
 }
-__device__ inline void multiply2(f32x16& acc, const f16x8 (&a)[2], const f16x8 (&b)[2])
+// out[q][p]: q = lane % 16, p = 4 (lane / 16) + 0..3.
+__device__ inline void multiply2(f32x4& acc, const f16x8 (&p)[2], const f16x8 (&q)[2])
 {
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[1], acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1], b[0], acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[0], acc, 0, 0, 0);
-}
-__device__ inline f32x16 zeros()
-{
-    f32x16 z;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = 0;
-    return z;
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], q[1], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[1], q[0], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], q[0], acc, 0, 0, 0);
 }
 
 template <class G>
@@ -561,28 +591,37 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
     __shared__ double s_wave[kTinyThreads / 64];
     const MuonMatrix& m = a.m[blockIdx.x];
     const uint32_t rows = m.rows, cols = m.cols, l32 = (max(rows, cols) + 31) & ~31u;
-    const uint32_t lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool wide = rows <= cols;
 
     // The update, in registers until its norm is known.
     constexpr uint32_t kMost = kTinyShort * kTinyLong / 4 / kTinyThreads;
     const uint32_t in_row = (cols + 3) / 4, all = rows * in_row;
     const G* in = (const G*)m.in;
-    float* momentum = (float*)m.momentum;
+    float* momentum = m.momentum;
     const float cs = a.grad_scale ? *a.grad_scale : 1.0f;
     f32x4 g[kMost], u[kMost];
+    uint32_t row[kMost], col[kMost];
+    {
+        const G* from[kMost];
+        const float* old[kMost];
 #pragma unroll
-    for (uint32_t i = 0; i < kMost; ++i) {
-        const uint32_t at = min(i * kTinyThreads + threadIdx.x, all - 1), row = at / in_row, c = at % in_row * 4;
-        g[i] = load_row(in + row * m.in_ld, c, cols);
-        if (momentum) u[i] = load_row(momentum + row * cols, c, cols);
+        for (uint32_t i = 0; i < kMost; ++i) {
+            const uint32_t at = min(i * kTinyThreads + threadIdx.x, all - 1);
+            row[i] = at / in_row;
+            col[i] = at % in_row * 4;
+            from[i] = in + row[i] * m.in_ld;
+            old[i] = momentum + row[i] * cols;
+        }
+        if (momentum) load_rows(old, col, cols, u);
+        load_rows(from, col, cols, g);
     }
     for (uint32_t k = threadIdx.x; k < 2 * kXPlane / 8; k += kTinyThreads) ((uint4*)s_x)[k] = make_uint4(0, 0, 0, 0);
     double sum = 0;
 #pragma unroll
     for (uint32_t i = 0; i < kMost; ++i) {
-        const uint32_t at = i * kTinyThreads + threadIdx.x, row = at / in_row, c = at % in_row * 4;
-        if (at >= all) continue;
+        if (i * kTinyThreads + threadIdx.x >= all) continue;
+        const uint32_t c = col[i];
         if (momentum) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -590,13 +629,7 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
                 u[i][j] = a.beta * u[i][j] + a.one_beta * cg;
                 g[i][j] = update(a, u[i][j], cg);
             }
-            float* to = momentum + row * cols + c;
-            if (c + 4 <= cols)
-                *(f32x4_any*)to = u[i];
-            else
-#pragma unroll
-                for (uint32_t j = 0; j < 3; ++j)
-                    if (c + j < cols) to[j] = u[i][j];
+            store_row(momentum + row[i] * cols, c, cols, u[i]);
         }
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
@@ -608,102 +641,125 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
     const float over = (float)((double)kUp / (sqrt(sum) + a.eps));
 #pragma unroll
     for (uint32_t i = 0; i < kMost; ++i) {
-        const uint32_t at = i * kTinyThreads + threadIdx.x, row = at / in_row, c = at % in_row * 4;
-        if (at >= all) continue;
+        if (i * kTinyThreads + threadIdx.x >= all) continue;
+        const uint32_t c = col[i];
         uint2 hi, lo;
         split2(g[i] * over, hi, lo);
         if (wide) {
-            *(uint2*)(s_x + row * kTinyX + c) = hi;
-            *(uint2*)(s_x + kXPlane + row * kTinyX + c) = lo;
+            *(uint2*)(s_x + row[i] * kTinyX + c) = hi;
+            *(uint2*)(s_x + kXPlane + row[i] * kTinyX + c) = lo;
         } else {
             const u16x4 h = __builtin_bit_cast(u16x4, hi), l = __builtin_bit_cast(u16x4, lo);
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) {
                 if (c + j >= cols) continue;
-                s_x[(c + j) * kTinyX + row] = h[j];
-                s_x[kXPlane + (c + j) * kTinyX + row] = l[j];
+                s_x[(c + j) * kTinyX + row[i]] = h[j];
+                s_x[kXPlane + (c + j) * kTinyX + row[i]] = l[j];
             }
         }
     }
     __syncthreads();
 
-    // A 32 x 32 tile of P P^T for each of the first four waves.
+    // P P^T: two tiles a wave, of the same q.
     auto square = [&](const uint16_t* p, uint32_t ld, uint32_t plane, uint32_t k, const uint16_t* c, uint16_t* out) {
-        if (wave < 4) {
-            const uint32_t p0 = 32 * (wave & 1), q0 = 32 * (wave >> 1);
-            f32x16 acc = zeros();
-            for (uint32_t k0 = 0; k0 < k; k0 += 16) {
-                const f16x8 x[2] = {row_part(p, ld, p0, k0), row_part(p + plane, ld, p0, k0)};
-                const f16x8 y[2] = {row_part(p, ld, q0, k0), row_part(p + plane, ld, q0, k0)};
-                multiply2(acc, x, y);
+        const uint32_t q0 = 16 * (wave >> 1), p0 = 32 * (wave & 1), q = q0 + (lane & 15), p1 = p0 + 4 * (lane >> 4);
+        f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+        for (uint32_t k0 = 0; k0 < k; k0 += 32) {
+            const f16x8 y[2] = {row_part(p, ld, q0, k0), row_part(p + plane, ld, q0, k0)};
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const f16x8 x[2] = {row_part(p, ld, p0 + 16 * t, k0), row_part(p + plane, ld, p0 + 16 * t, k0)};
+                multiply2(acc[t], x, y);
             }
-            const uint32_t q = q0 + (lane & 31);
+        }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const uint32_t p1 = p0 + 8 * r + 4 * half, at = q * kTinyA + p1;
-                f32x4 v;
+        for (int t = 0; t < 2; ++t) {
+            const uint32_t at = q * kTinyA + p1 + 16 * t;
+            f32x4 v = acc[t] * kDown;
+            if (c) {
+                Planes old;
+                old.load(c + at, kAPlane);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = acc[4 * r + j] * kDown;
-                if (c) {
-                    Planes old;
-                    old.load(c + at, kAPlane);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = n.cc * v[j] + n.cb * old.at(j) + (p1 + j == q ? n.ca * kUp : 0.0f);
-                }
-                uint2 hi, lo;
-                split2(v, hi, lo);
-                *(uint2*)(out + at) = hi;
-                *(uint2*)(out + kAPlane + at) = lo;
+                for (int j = 0; j < 4; ++j) v[j] = n.cc * v[j] + n.cb * old.at(j) + (p1 + 16 * t + j == q ? n.ca * kUp : 0.0f);
             }
+            uint2 hi, lo;
+            split2(v, hi, lo);
+            *(uint2*)(out + at) = hi;
+            *(uint2*)(out + kAPlane + at) = lo;
         }
         __syncthreads();
     };
-    constexpr int kTiles = kTinyShort / 32 * (kTinyLong / 32) / (kTinyThreads / 64);
-    const uint32_t tiles = kTinyShort / 32 * (l32 / 32);
-    const LastEnd end = {(float*)m.master, (void*)m.out, m.out_ld, cols, rows, a.keep, m.scale, a.out_f32};
-    for (uint32_t step = 0; step < n.steps; ++step) {
-        const bool last = step + 1 == n.steps;
+    // B X: a wave has 32 columns of X (those past the matrix are zeros), which it reads once: two strips of 16, 4 tiles each.
+    constexpr int kTiles = 8;
+    static_assert(kTinyShort == 64 && kTinyLong == 32 * (kTinyThreads / 64), "");
+    f32x4 acc[kTiles];
+    auto i0 = [](int t) { return 16u * (t & 3); };
+    auto j0 = [&](int t) { return 32 * wave + 16 * (t >> 2); };
+    auto apply = [&](auto turned) { // turned: [q][p] is [long][short]
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) acc[t] = {0, 0, 0, 0};
+#pragma unroll
+        for (uint32_t k0 = 0; k0 < kTinyShort; k0 += 32) {
+            f16x8 x[2][2], b[4][2];
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) x[t][z] = column_part(s_x + z * kXPlane, kTinyX, j0(4 * t), k0);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) b[t][z] = row_part(s_b + z * kAPlane, kTinyA, i0(t), k0);
+            }
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                if constexpr (turned)
+                    multiply2(acc[t], b[t & 3], x[t >> 2]);
+                else
+                    multiply2(acc[t], x[t >> 2], b[t & 3]);
+            }
+        }
+    };
+    for (uint32_t step = 0;; ++step) {
         square(s_x, kTinyX, kXPlane, l32, nullptr, s_a);
         square(s_a, kTinyA, kAPlane, kTinyShort, s_a, s_b);
-        f32x16 acc[kTiles];
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            const uint32_t t = i * (kTinyThreads / 64) + wave, i0 = 32 * (t & 1), j0 = 32 * (t >> 1);
-            acc[i] = zeros();
-            if (t >= tiles) continue;
-#pragma unroll
-            for (uint32_t k0 = 0; k0 < kTinyShort; k0 += 16) {
-                const f16x8 b[2] = {row_part(s_b, kTinyA, i0, k0), row_part(s_b + kAPlane, kTinyA, i0, k0)};
-                const f16x8 x[2] = {column_part(s_x, kTinyX, j0, k0), column_part(s_x + kXPlane, kTinyX, j0, k0)};
-                if (last && !wide) // as it lies: the short side across
-                    multiply2(acc[i], b, x);
-                else
-                    multiply2(acc[i], x, b);
-            }
-        }
+        if (step + 1 == n.steps) break;
+        apply(std::false_type());
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            const uint32_t t = i * (kTinyThreads / 64) + wave, i0 = 32 * (t & 1), j0 = 32 * (t >> 1);
-            if (t >= tiles) continue;
-            if (last) {
-                f32x16 one[1][1] = {{acc[i]}};
-                Finish<LastEnd, 1, 1>::run(end, Early<LastEnd, 1>(end, 0), one, wide ? j0 : i0, wide ? i0 : j0, 0, nullptr);
-                continue;
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                f32x4 v;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = acc[i][4 * r + j] * kDown;
-                uint2 hi, lo;
-                split2(v, hi, lo);
-                uint16_t* to = s_x + (i0 + (lane & 31)) * kTinyX + j0 + 8 * r + 4 * half;
-                *(uint2*)to = hi;
-                *(uint2*)(to + kXPlane) = lo;
-            }
+        for (int t = 0; t < kTiles; ++t) {
+            uint2 hi, lo;
+            split2(acc[t] * kDown, hi, lo);
+            uint16_t* to = s_x + (i0(t) + (lane & 15)) * kTinyX + j0(t) + 4 * (lane >> 4);
+            *(uint2*)to = hi;
+            *(uint2*)(to + kXPlane) = lo;
         }
         __syncthreads();
+    }
+    // The last as the matrix lies, in runs of 4 values of its rows.
+    uint32_t r[kTiles], c[kTiles];
+    const float* w[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        r[t] = (wide ? i0(t) : j0(t)) + (lane & 15);
+        c[t] = (wide ? j0(t) : i0(t)) + 4 * (lane >> 4);
+        w[t] = m.master + min(r[t], rows - 1) * cols;
+    }
+    f32x4 old[kTiles];
+    if (m.master) load_rows(w, c, cols, old);
+    if (wide)
+        apply(std::false_type());
+    else
+        apply(std::true_type());
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        if (r[t] >= rows || c[t] >= cols) continue;
+        f32x4 v = acc[t] * (kDown * kDown);
+        if (m.master) {
+            v = old[t] * a.keep - v * m.scale;
+            store_row(m.master + r[t] * cols, c[t], cols, v);
+        }
+        if (a.out_f32)
+            store_row((float*)m.out + r[t] * m.out_ld, c[t], cols, v);
+        else
+            store_row((uint16_t*)m.out + r[t] * m.out_ld, c[t], cols, v);
     }
 }
 

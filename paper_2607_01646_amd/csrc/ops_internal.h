@@ -192,11 +192,13 @@ hipError_t launch_norm_finish(const double* part, double max_norm, float* out, h
 // A matrix of s x l values, s the shorter side, is held as two planes of fp16 (22 bits) that are 2^12 times its values, in
 // rows of up(l, 64) with zeros behind them; its Gram matrix and polynomials of that are s x s in rows of up(s, 64).
 constexpr uint32_t kMuonMats = 32; // per launch: kernel arguments stay below 4 KiB
-struct MuonMatrix {
-    uint64_t x, y, f; // launch_muon_apply: y (or the result) = f x
-    uint64_t in, momentum, master, out; // momentum == 0: `in` is orthogonalised, and out is the result's; else out is the parameter's
+struct MuonMatrix { // pointers, not addresses: the kernels' accesses are global ones then
+    uint16_t *x, *y, *f; // launch_muon_apply: y (or the result) = f x
+    const void* in;
+    float *momentum, *master; // nullptr: `in` is orthogonalised, and out is the result's; else out is the parameter's
+    void* out;
     uint64_t in_ld, out_ld;
-    uint64_t part; // double [part_n]: sums of squares, a tile's each
+    double* part; // [part_n]: sums of squares, a tile's each
     uint32_t part_n, rows, cols, first;
     float scale; // lr times the matrix's scale
 };
@@ -208,9 +210,10 @@ struct MuonArgs {
     const float* grad_scale;
     bool nesterov, in_f32, out_f32, shares;
 };
-// Symmetric products out = ca I + cb c + cc p q, p q^T of rows of k values; c == 0: cc p q alone.
+// Symmetric products out = ca I + cb c + cc p q, p q^T of rows of k values; no c: cc p q alone.
 struct TriMatrix {
-    uint64_t p, q, c, out;
+    const uint16_t *p, *q, *c;
+    uint16_t* out;
     uint32_t s, k, first, unused;
 };
 struct TriArgs {

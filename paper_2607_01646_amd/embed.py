@@ -10,8 +10,8 @@ import ctypes as C
 
 import torch
 
+from .ckpt import CKPT_OK, _native_module, lib
 from .ops import _TYPES, _check, _handle, _on, _rows, _type
-from .ckpt import lib
 
 __all__ = ["ckpt_embed_args", "ckpt_embedding", "ckpt_embedding_grad"]
 
@@ -24,6 +24,17 @@ class ckpt_embed_args(C.Structure):
 
 
 _lib = None
+_native = None
+
+
+def _module():
+    """(the native module or None, addresses of the entry points)."""
+    global _native
+    if _native is None:
+        L = _ops()
+        _native = (_native_module(), [C.cast(getattr(L, n), C.c_void_p).value for n in
+                                      ("ckpt_embedding", "ckpt_embedding_grad_workspace", "ckpt_embedding_grad")])
+    return _native
 
 
 def _ops():
@@ -57,6 +68,15 @@ def ckpt_embedding(table, ids, scale=1.0, ignore_index=-100, stream=None):
     rows of any spacing) at ids [...] (int64), rounded once.  A token whose id
     is ignore_index has a row of zeros; one with another id outside [0, vocab)
     a row of NaN."""
+    native, at = _native or _module()
+    if native is not None and isinstance(table, torch.Tensor) and table.is_cuda:
+        with _on(stream, table):
+            got = native.embedding(at[0], table, ids, scale, ignore_index, _handle(stream, table))
+        if got is not None:
+            if got[0] != CKPT_OK:
+                _check(got[0])
+            return got[1]
+    # Arguments that the native module leaves to this code, and those refused; every call where there is none.
     a = ckpt_embed_args()
     a.dtype = a.table_dtype = _type(table, "table")
     if table.dim() != 2:
@@ -78,6 +98,16 @@ def ckpt_embedding_grad(d_rows, ids, vocab, scale=1.0, ignore_index=-100, dtype=
     fp32) it is added to what is there, in place, and add_to is returned; rows
     that no token has stay as they are.  Tokens with ignore_index or an id
     outside [0, vocab) are not read."""
+    native, at = _native or _module()
+    if native is not None and isinstance(d_rows, torch.Tensor) and d_rows.is_cuda and dtype is None:
+        with _on(stream, d_rows):
+            got = native.embedding_grad(at[1], at[2], d_rows, ids, vocab, scale, ignore_index, add_to,
+                                        _handle(stream, d_rows))
+        if got is not None:
+            if got[0] != CKPT_OK:
+                _check(got[0])
+            return got[1]
+    # Arguments that the native module leaves to this code, and those refused; every call where there is none.
     a = ckpt_embed_args()
     a.dtype = _type(d_rows, "d_rows")
     a.ids = _ids(ids, d_rows.device)

@@ -11,8 +11,8 @@ import math
 
 import torch
 
-from .ops import _check, _handle, _listed, _module, _on, _plain, _rows, _type
-from .ckpt import CKPT_OK, lib
+from .ckpt import CKPT_OK, _native_module, lib
+from .ops import CKPT_TYPE_F32, _check, _handle, _listed, _on, _plain, _rows, _type
 
 __all__ = ["ckpt_matrix", "ckpt_muon", "ckpt_muon_args", "ckpt_muon_matrix", "ckpt_newton_schulz", "ckpt_orthogonalize"]
 
@@ -41,6 +41,20 @@ class ckpt_muon_args(C.Structure):
 
 
 _lib = None
+_native = None
+_RULES = {"rms": 0, "spectral": 1}
+_NAMES = ("param", "master", "momentum", "grad")
+
+
+def _module():
+    """(the native module or None, addresses of the entry points)."""
+    global _native
+    if _native is None:
+        L = _ops()
+        _native = (_native_module(), [C.cast(getattr(L, n), C.c_void_p).value for n in
+                                      ("ckpt_orthogonalize_workspace", "ckpt_orthogonalize", "ckpt_muon_workspace",
+                                       "ckpt_muon")])
+    return _native
 
 
 def _ops():
@@ -64,7 +78,7 @@ def _ops():
 
 def _ns(steps, coefficients, eps, piece_bytes):
     a, b, c = coefficients
-    if not 1 <= steps <= 64:
+    if not 0 <= steps <= 64:
         raise ValueError("%r steps: 1 to 64" % (steps,))
     return ckpt_newton_schulz(steps, 0, a, b, c, eps, piece_bytes)
 
@@ -86,6 +100,16 @@ def ckpt_orthogonalize(matrices, steps=5, coefficients=COEFFICIENTS, eps=1e-7, p
     list of new tensors, or `out` (which may be the matrices themselves).
     piece_bytes bounds the workspace (0 = 4 GiB, at least one matrix's)."""
     matrices = _listed(matrices)
+    native, at = _native or _module()
+    if native is not None and out is None and matrices and isinstance(matrices[0], torch.Tensor) and matrices[0].is_cuda:
+        a, b, c = coefficients
+        with _on(stream, matrices[0]):
+            got = native.orthogonalize(at[0], at[1], matrices, steps, a, b, c, eps, piece_bytes, _handle(stream, matrices[0]))
+        if got is not None:
+            if got[0] != CKPT_OK:
+                _check(got[0])
+            return got[1]
+    # Arguments that the native module leaves to this code, and those refused; every call where there is none.
     ns = _ns(steps, coefficients, eps, piece_bytes)
     if out is not None:
         out = _listed(out)
@@ -129,6 +153,19 @@ def ckpt_muon(params, masters, momentums, grads, lr, momentum=0.95, nesterov=Tru
     sqrt(max(1, rows / cols)); or a number.  One list may be a bucket, behind
     Checkpointer.wait_captured of the same range on the same stream."""
     params, masters, momentums, grads = map(_listed, (params, masters, momentums, grads))
+    native, at = _native or _module()
+    if native is not None and params and isinstance(params[0], torch.Tensor) and params[0].is_cuda and \
+            (scale in _RULES if isinstance(scale, str) else isinstance(scale, float)):
+        a, b, c = coefficients
+        with _on(stream, params[0]):
+            rc = native.muon(at[2], at[3], params, masters, momentums, grads, lr, momentum, nesterov, weight_decay,
+                             _RULES.get(scale, 2), 0.0 if isinstance(scale, str) else scale, steps, a, b, c, eps,
+                             grad_scale, piece_bytes, _handle(stream, params[0]))
+        if rc is not None:
+            if rc != CKPT_OK:
+                _check(rc)
+            return
+    # Arguments that the native module leaves to this code, and those refused; every call where there is none.
     lists = (params, masters, momentums, grads)
     n = len(params)
     if any(len(x) != n for x in lists):
@@ -137,7 +174,7 @@ def ckpt_muon(params, masters, momentums, grads, lr, momentum=0.95, nesterov=Tru
     if n == 0:
         return
     pt, gt = _type(params[0], "param 0"), _type(grads[0], "grad 0")
-    kinds = (pt, _F32, _F32, gt)
+    kinds = (pt, CKPT_TYPE_F32, CKPT_TYPE_F32, gt)
     device = params[0].device
     arr = (ckpt_muon_matrix * n)()
     for i, row in enumerate(zip(*lists)):
@@ -160,6 +197,3 @@ def ckpt_muon(params, masters, momentums, grads, lr, momentum=0.95, nesterov=Tru
         work = torch.empty(need.value, dtype=torch.uint8, device=device)
         _check(L.ckpt_muon(arr, n, C.byref(args), device.index, work.data_ptr(), need.value, _handle(stream, params[0])))
 
-
-_F32 = 2
-_NAMES = ("param", "master", "momentum", "grad")
