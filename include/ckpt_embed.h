@@ -43,7 +43,7 @@ ckpt_status ckpt_embedding(const ckpt_embed_args* a, int32_t device, void* strea
  * id outside [0, vocab) give nothing and are not read.  With `add` rows that no
  * token has are left as they are.  `workspace`: 256-byte aligned device
  * memory of at least the bytes that _workspace says, the call's own until its
- * work on `stream` has run.  Errors as above. */
+ * work on `stream` has run (NULL where that is 0).  Errors as above. */
 ckpt_status ckpt_embedding_grad_workspace(const ckpt_embed_args* a, uint64_t* bytes);
 ckpt_status ckpt_embedding_grad(const ckpt_embed_args* a, int32_t device, void* workspace, uint64_t workspace_bytes,
                                 void* stream);

@@ -29,14 +29,18 @@ ckpt_status check_embed(const ckpt_embed_args* a, bool grad)
 
 // Where everything lies in the workspace.
 struct GradPlan {
-    uint32_t range, chunk;
-    uint64_t start, order, word, part, part_ld, bytes;
+    bool few = false;
+    uint32_t range = 0, chunk = 0;
+    uint64_t start = 0, order = 0, word = 0, part = 0, part_ld = 0, bytes = 0;
 };
 
 GradPlan plan_grad(const ckpt_embed_args* a)
 {
     GradPlan l;
     const uint64_t n = a->tokens, columns = 1024 / (a->dtype == CKPT_TYPE_F32 ? 4 : 2), runs = (a->dim + columns - 1) / columns;
+    // (A launch's lanes are counted in 32 bits.)
+    l.few = n > 0 && n <= kFewRows && (a->vocab + 15) / 16 * runs <= 1u << 23;
+    if (l.few) return l;
     // Sorting workgroups: each reads all ids, so no more than the GPU has units, unless LDS holds no more words.
     l.range = (uint32_t)std::min<uint64_t>(std::max<uint64_t>((a->vocab + 255) / 256, 32), kSortRange);
     // Sorted tokens that a wave sums: 64 ids at a time, as long as that leaves each SIMD four waves; and no more than 1024
@@ -122,7 +126,7 @@ extern "C" ckpt_status ckpt_embedding_grad(const ckpt_embed_args* a, int32_t dev
     clear_free_error();
     if (ckpt_status st = check_embed(a, true)) return st;
     const GradPlan l = plan_grad(a);
-    if (!workspace || (uintptr_t)workspace % 256) return fail_free(CKPT_EINVAL, "workspace: null or not 256-byte aligned");
+    if (l.bytes && (!workspace || (uintptr_t)workspace % 256)) return fail_free(CKPT_EINVAL, "workspace: null or not 256-byte aligned");
     if (workspace_bytes < l.bytes)
         return fail_free(CKPT_EINVAL, "workspace of %llu bytes needs %llu", (unsigned long long)workspace_bytes,
                          (unsigned long long)l.bytes);
@@ -130,7 +134,8 @@ extern "C" ckpt_status ckpt_embedding_grad(const ckpt_embed_args* a, int32_t dev
     if (ckpt_status st = enter_device(device, dg)) return st;
     Known known;
     if (ckpt_status st = check_pointers(a, device, known)) return st;
-    if (ckpt_status st = check_given({workspace, 1, l.bytes, l.bytes, 1, "workspace"}, device, known)) return st;
+    if (l.bytes)
+        if (ckpt_status st = check_given({workspace, 1, l.bytes, l.bytes, 1, "workspace"}, device, known)) return st;
     uint8_t* w = (uint8_t*)workspace;
     EmbedArgs k = embed_args(a);
     k.range = l.range;
@@ -140,8 +145,8 @@ extern "C" ckpt_status ckpt_embedding_grad(const ckpt_embed_args* a, int32_t dev
     k.word = (uint32_t*)(w + l.word);
     k.part = (float*)(w + l.part);
     k.part_ld = l.part_ld;
-    hipError_t err = launch_sort(k, (hipStream_t)stream);
-    if (err == hipSuccess) err = launch_table_sums(k, (hipStream_t)stream);
+    hipError_t err = l.few ? launch_few_sums(k, (hipStream_t)stream) : launch_sort(k, (hipStream_t)stream);
+    if (err == hipSuccess && !l.few) err = launch_table_sums(k, (hipStream_t)stream);
     if (err != hipSuccess) return fail_free(CKPT_EHIP, "table's gradient: %s", hipGetErrorString(err));
     return CKPT_OK;
 }

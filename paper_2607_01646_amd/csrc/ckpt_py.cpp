@@ -610,13 +610,13 @@ PyObject* embedding_grad(PyObject*, PyObject* const* args, Py_ssize_t n_args)
         a.ids = a.tokens ? (const int64_t*)ids->data_ptr() : nullptr;
         a.rows = a.tokens ? d->data_ptr() : nullptr;
         rc = ((EmbedWorkFn)(uintptr_t)work_fn)(&a, &bytes);
-        if (rc == CKPT_OK) work = at::empty({(int64_t)bytes}, d->options().dtype(at::kByte));
+        if (rc == CKPT_OK && bytes) work = at::empty({(int64_t)bytes}, d->options().dtype(at::kByte));
     } catch (...) {
         Py_RETURN_NONE;
     }
     if (rc == CKPT_OK) {
         Py_BEGIN_ALLOW_THREADS;
-        rc = ((EmbedGradFn)(uintptr_t)fn)(&a, device, work.data_ptr(), bytes, (void*)(uintptr_t)stream);
+        rc = ((EmbedGradFn)(uintptr_t)fn)(&a, device, bytes ? work.data_ptr() : nullptr, bytes, (void*)(uintptr_t)stream);
         Py_END_ALLOW_THREADS;
     }
     return Py_BuildValue("iN", (int)rc, THPVariable_Wrap(table));

@@ -28,30 +28,44 @@ __device__ inline uint16_t bf16_of(float x) { return __builtin_bit_cast(uint16_t
 __device__ inline float float_of(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ inline float float_of(float x) { return x; }
 
-// A lane's 16 bytes of a row: 8 bf16 or 4 fp32, from column c on; any alignment of the elements.
+// A lane's 16 bytes of a row: 8 bf16 or 4 fp32, at any alignment of the elements.  The loads of a wave's rows are in no
+// branch: a lane whose columns go past the end has the row's last ones (those of a row of fewer: some of them twice), from
+// first() on, and settle() puts its sums in their places.
 template <class T>
 struct Piece {
     static constexpr uint32_t kValues = 16 / sizeof(T);
     u32x4 raw;
+    static __device__ inline uint32_t first(uint32_t c, uint32_t dim) { return dim < kValues ? 0 : min(c, dim - kValues); }
     __device__ inline float at(int j) const
     {
         if constexpr (sizeof(T) == 4) return __uint_as_float(raw[j]);
         return __uint_as_float(j & 1 ? raw[j / 2] & 0xFFFF0000u : raw[j / 2] << 16);
     }
-    __device__ inline void load(const T* row, uint32_t c, uint32_t dim)
+    __device__ inline void load(const T* row, uint32_t from, bool narrow, uint32_t dim)
     {
-        if (c + kValues <= dim) {
-            raw = *(const u32x4_any*)(row + c);
+        if (!narrow) {
+            raw = *(const u32x4_any*)(row + from);
             return;
         }
         raw = {0, 0, 0, 0};
 #pragma unroll
-        for (uint32_t j = 0; j < kValues - 1; ++j) {
-            if (c + j >= dim) continue;
+        for (uint32_t j = 0; j < kValues; ++j) {
+            const T x = row[min(j, dim - 1)];
             if constexpr (sizeof(T) == 4)
-                raw[j] = __float_as_uint(row[c + j]);
+                raw[j] = __float_as_uint(x);
             else
-                raw[j / 2] |= (uint32_t)row[c + j] << (j & 1 ? 16 : 0);
+                raw[j / 2] |= (uint32_t)x << (j & 1 ? 16 : 0);
+        }
+    }
+    // Values that begin at column first(c) to such that begin at c.
+    static __device__ inline void settle(float (&x)[kValues], uint32_t c, uint32_t dim)
+    {
+        const uint32_t by = c - first(c, dim);
+#pragma unroll
+        for (uint32_t b = 1; b < kValues; b *= 2) {
+            const bool move = by & b;
+#pragma unroll
+            for (uint32_t j = 0; j < kValues; ++j) x[j] = move ? (j + b < kValues ? x[j + b] : 0.0f) : x[j];
         }
     }
 };
@@ -109,31 +123,33 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const EmbedArgs a, uin
     T* to = (T*)a.rows + (uint64_t)t * a.rows_ld;
     const uint32_t c0 = run * UNROLL * kRun + lane * kValues;
     const float instead = id == a.ignore_index ? 0.0f : __builtin_nanf("");
+    const bool narrow = a.dim < kValues;
     Piece<T> p[UNROLL];
-    if (there) {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u)
-            if (c0 + u * kRun < a.dim) p[u].load(from, c0 + u * kRun, a.dim);
-    }
+    for (int u = 0; u < UNROLL; ++u) p[u].load(from, Piece<T>::first(c0 + u * kRun, a.dim), narrow, a.dim);
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
         if (c0 + u * kRun >= a.dim) continue;
         float x[kValues];
 #pragma unroll
         for (int j = 0; j < (int)kValues; ++j) x[j] = there ? p[u].at(j) * a.scale : instead;
+        if (c0 + u * kRun + kValues > a.dim) Piece<T>::settle(x, c0 + u * kRun, a.dim);
         store(to, c0 + u * kRun, a.dim, x);
     }
 }
 
 // ---- the tokens by word ----
 //
-// A workgroup has `range` words.  It goes over all ids twice (they stay in the L2): the first time each wave counts its
-// own sixteenth of the tokens for each of the words, and those below all of them, which is where the workgroup's tokens
-// begin; the second time each wave puts its tokens in their places.  A wave's places of a word follow those of the waves
-// before it, a lane's those of the lanes before it: the order is the tokens' own.
+// A workgroup has `range` words and goes over all ids (they stay in the L2), each wave over its own sixteenth: it counts its
+// tokens for each of the words, and those below all of them, which is where the workgroup's tokens begin, and lists the
+// ones that are the workgroup's in LDS.  Then each wave puts its tokens in their places.  A wave's places of a word follow
+// those of the waves before it, a lane's those of the lanes before it: the order is the tokens' own.  A wave whose tokens
+// its list does not hold goes over the ids again.  Bound by the instructions of the first pass.
+constexpr uint32_t kList = 256;
 __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const EmbedArgs a)
 {
     extern __shared__ uint32_t s_place[]; // [kSortWaves][range]
+    __shared__ uint32_t s_list[kSortWaves][kList];
     __shared__ uint32_t s_below[kSortWaves], s_sum[kSortWaves];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t first = blockIdx.x * a.range, words = min(a.range, a.vocab - first);
@@ -142,36 +158,46 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const EmbedArgs a
     uint32_t* mine = s_place + wave * a.range;
     const uint32_t each = (uint32_t)((((uint64_t)a.tokens + kSortWaves - 1) / kSortWaves + 63) / 64 * 64);
     const uint64_t begin = (uint64_t)wave * each, end = min(begin + each, (uint64_t)a.tokens);
-    constexpr int kAhead = 4;
-    // The words of a wave's next tokens: kNoWord for those that do not count.
+    constexpr int kAhead = 8;
+    // The words of a wave's next tokens: kNoWord for those that do not count.  An ignored id that is a word's number is one
+    // in 2^32 bits; no other has its upper half 0 and its lower below vocab.
+    const uint32_t ignored = a.ignore_index >= 0 && a.ignore_index < (int64_t)a.vocab ? (uint32_t)a.ignore_index : kNoWord;
     auto load = [&](uint64_t t0, uint32_t (&w)[kAhead]) {
-        int64_t id[kAhead];
+        uint2 id[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const uint64_t t = t0 + 64 * u + lane;
-            id[u] = t < end ? a.ids[t] : -1;
-        }
+        for (int u = 0; u < kAhead; ++u) id[u] = ((const uint2*)a.ids)[min(t0 + 64 * u + lane, end - 1)];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            w[u] = id[u] >= 0 && id[u] < (int64_t)a.vocab && id[u] != a.ignore_index ? (uint32_t)id[u] : kNoWord;
+            w[u] = id[u].y == 0 && id[u].x < a.vocab && id[u].x != ignored && t0 + 64 * u + lane < end ? id[u].x : kNoWord;
     };
-    uint32_t below = 0;
+    uint32_t below = 0, listed = 0;
     for (uint64_t t = begin; t < end; t += 64 * kAhead) {
         uint32_t w[kAhead];
         load(t, w);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             below += __builtin_popcountll(__ballot(w[u] < first));
-            if (w[u] - first < words) atomicAdd(mine + (w[u] - first), 1u);
+            const bool in = w[u] - first < words;
+            const uint64_t which = __ballot(in);
+            if (which == 0) continue;
+            const uint32_t place = listed + __builtin_popcountll(which & ((1ull << lane) - 1));
+            if (in) {
+                atomicAdd(mine + (w[u] - first), 1u);
+                if (place < kList) s_list[wave][place] = (uint32_t)(t + 64 * u + lane);
+            }
+            listed += __builtin_popcountll(which);
         }
     }
     if (lane == 0) s_below[wave] = below;
     __syncthreads();
     // Word r's tokens of all waves, and of all words before it.
     const uint32_t r = threadIdx.x;
-    uint32_t count = 0;
-    if (r < words)
-        for (uint32_t w = 0; w < kSortWaves; ++w) count += s_place[w * a.range + r];
+    uint32_t of[kSortWaves], count = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kSortWaves; ++w) {
+        of[w] = s_place[w * a.range + min(r, words - 1)];
+        count += r < words ? of[w] : 0;
+    }
     uint32_t upto = count;
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t x = __shfl_up(upto, o);
@@ -180,63 +206,74 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const EmbedArgs a
     if (lane == 63) s_sum[wave] = upto;
     __syncthreads();
     uint32_t at = upto - count;
+#pragma unroll
     for (uint32_t w = 0; w < kSortWaves; ++w) at += s_below[w] + (w < wave ? s_sum[w] : 0);
     if (r < words) {
         a.start[first + r] = at;
         if (first + r + 1 == a.vocab) a.start[a.vocab] = at + count;
+#pragma unroll
         for (uint32_t w = 0; w < kSortWaves; ++w) {
-            uint32_t& place = s_place[w * a.range + r];
-            const uint32_t here = place;
-            place = at;
-            at += here;
+            s_place[w * a.range + r] = at;
+            at += of[w];
         }
     }
     __syncthreads();
     const uint32_t bits = 32 - __builtin_clz(words);
+    // The places of up to 64 tokens of this wave, in their lanes' order.
+    auto put = [&](bool in, uint32_t token, uint32_t word) {
+        uint64_t same = __ballot(in);
+        const uint32_t d = in ? word - first : 0;
+        for (uint32_t b = 0; b < bits; ++b) { // the lanes with this lane's word
+            const uint64_t has = __ballot(d >> b & 1);
+            same &= d >> b & 1 ? has : ~has;
+        }
+        if (in) {
+            const uint32_t place = mine[d] + __builtin_popcountll(same & ((1ull << lane) - 1));
+            a.order[place] = token;
+            a.word[place] = word;
+        }
+        // Every lane has read its word's place before the last of them moves it on.
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (in && (same >> lane) == 1) mine[d] += __builtin_popcountll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    if (listed <= kList) {
+        for (uint32_t k = 0; k < listed; k += 64) {
+            const uint32_t token = s_list[wave][min(k + lane, listed - 1)];
+            put(k + lane < listed, token, ((const uint2*)a.ids)[token].x);
+        }
+        return;
+    }
     for (uint64_t t = begin; t < end; t += 64 * kAhead) {
         uint32_t w[kAhead];
         load(t, w);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const bool in = w[u] - first < words;
-            uint64_t same = __ballot(in);
-            if (same == 0) continue;
-            const uint32_t d = in ? w[u] - first : 0;
-            for (uint32_t b = 0; b < bits; ++b) { // the lanes with this lane's word
-                const uint64_t has = __ballot(d >> b & 1);
-                same &= d >> b & 1 ? has : ~has;
-            }
-            if (in) {
-                const uint32_t place = mine[d] + __builtin_popcountll(same & ((1ull << lane) - 1));
-                a.order[place] = (uint32_t)(t + 64 * u + lane);
-                a.word[place] = w[u];
-            }
-            // Every lane has read its word's place before the last of them moves it on.
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            if (in && (same >> lane) == 1) mine[d] += __builtin_popcountll(same);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
+        for (int u = 0; u < kAhead; ++u)
+            if (__ballot(w[u] - first < words)) put(w[u] - first < words, (uint32_t)(t + 64 * u + lane), w[u]);
     }
 }
 
 // ---- the sums ----
 
-// A word's sum into its row of the table.
+// N values of a row of the table that a sum is added to, from column `from` on.
 template <class O, int N>
-__device__ inline void write_row(const EmbedArgs& a, uint32_t word, uint32_t c, float (&x)[N])
-{
-    O* row = (O*)a.table + (uint64_t)word * a.table_ld;
+struct Old {
+    O x[N];
+    __device__ inline void load(const O* row, uint32_t from, bool narrow, uint32_t dim)
+    {
+        typedef O any __attribute__((ext_vector_type(N), aligned(sizeof(O))));
+        if (!narrow) {
+            const any v = *(const any*)(row + from);
 #pragma unroll
-    for (int j = 0; j < N; ++j) x[j] *= a.scale;
-    if (a.add) {
+            for (int j = 0; j < N; ++j) x[j] = v[j];
+        } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (c + j < a.dim) x[j] += float_of(row[c + j]);
+            for (uint32_t j = 0; j < N; ++j) x[j] = row[min(j, dim - 1)];
+        }
     }
-    store(row, c, a.dim, x);
-}
+};
 
 // Workgroups up to `chunk_blocks`: each wave a chunk of sorted tokens and a run of columns.  The others: rows that no token
 // has, 16 a workgroup.
@@ -258,76 +295,147 @@ __global__ __launch_bounds__(kThreads) void sums_kernel(const EmbedArgs a, uint3
     }
     const uint64_t job = blockIdx.x * 4ull + wave;
     const uint32_t chunk = __builtin_amdgcn_readfirstlane((uint32_t)(job / runs)), run = __builtin_amdgcn_readfirstlane((uint32_t)(job % runs));
-    const uint32_t all = a.start[a.vocab]; // tokens that count
+    if (chunk >= chunks) return;
     const uint64_t lo = (uint64_t)chunk * a.chunk;
-    if (chunk >= chunks || lo >= all) return;
-    const uint32_t hi = (uint32_t)min(lo + a.chunk, (uint64_t)all);
-    const uint32_t c = (run * 64 + lane) * kValues;
+    const uint32_t all = a.start[a.vocab]; // tokens that count
+    const uint32_t c = (run * 64 + lane) * kValues, from = Piece<T>::first(c, a.dim);
+    const bool narrow = a.dim < (uint32_t)kValues;
     float sum[kValues];
 #pragma unroll
     for (int j = 0; j < kValues; ++j) sum[j] = 0;
-    uint32_t now = kNoWord, begin = 0; // the word that is summed, and its first token here
-    auto flush = [&](uint32_t end) {
-        if (c < a.dim) {
-            const bool head = begin == lo && a.start[now] < lo, tail = end == hi && a.start[now + 1] > hi;
-            if (!head && !tail)
-                write_row<O>(a, now, c, sum);
-            else
-                store(a.part + ((head ? 0 : chunks) + (uint64_t)chunk) * a.part_ld, c, (uint32_t)a.part_ld, sum); // part_ld covers whole pieces
-        }
-#pragma unroll
-        for (int j = 0; j < kValues; ++j) sum[j] = 0;
-    };
-    for (uint32_t base = (uint32_t)lo; base < hi; base += 64) {
-        const uint32_t n = min(64u, hi - base), at = base + min(lane, n - 1);
-        const uint32_t tokens = a.order[at], words = a.word[at];
+    for (uint64_t base = lo; base < lo + a.chunk; base += 64) {
+        // 64 tokens at a time: their words, and where those begin and end (what lies past the last token is not used).
+        const uint64_t at = min(base + lane, (uint64_t)a.tokens - 1);
+        const uint32_t tokens = a.order[at], words = min(a.word[at], a.vocab - 1);
+        const uint32_t begins = a.start[words], ends = a.start[words + 1];
+        const uint32_t hi = (uint32_t)min(lo + a.chunk, (uint64_t)all);
+        if (base >= hi) return;
+        const uint32_t n = min(64u, hi - (uint32_t)base);
         for (uint32_t i = 0; i < n; i += kAhead) {
             Piece<T> p[kAhead];
+            Old<O, kValues> old[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const uint32_t t = __builtin_amdgcn_readlane(tokens, min(i + u, n - 1));
-                if (c < a.dim && i + u < n) p[u].load((const T*)a.rows + (uint64_t)t * a.rows_ld, c, a.dim);
+                const uint32_t k = min(i + u, n - 1), end = __builtin_amdgcn_readlane(ends, k);
+                p[u].load((const T*)a.rows + (uint64_t)__builtin_amdgcn_readlane(tokens, k) * a.rows_ld, from, narrow, a.dim);
+                if (a.add && end == base + k + 1) // its last token: what the word's sum is added to
+                    old[u].load((const O*)a.table + (uint64_t)__builtin_amdgcn_readlane(words, k) * a.table_ld, from, narrow, a.dim);
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (i + u >= n) break;
-                const uint32_t w = __builtin_amdgcn_readlane(words, i + u);
-                if (w != now) {
-                    if (now != kNoWord) flush(base + i + u);
-                    now = w;
-                    begin = base + i + u;
-                }
-                if (c < a.dim) {
+                const uint32_t here = (uint32_t)base + i + u;
+                const uint32_t end = __builtin_amdgcn_readlane(ends, i + u);
 #pragma unroll
-                    for (int j = 0; j < kValues; ++j) sum[j] += p[u].at(j);
+                for (int j = 0; j < kValues; ++j) sum[j] += p[u].at(j);
+                if (here + 1 != end && here + 1 != hi) continue;
+                // The word's last token, or the chunk's: its row, or a sum that is joined with others.
+                const bool head = __builtin_amdgcn_readlane(begins, i + u) < lo, tail = end > hi;
+                if (head || tail) {
+                    if (c + kValues > a.dim) Piece<T>::settle(sum, c, a.dim);
+                    if (c < a.dim) // part_ld covers whole pieces
+                        store(a.part + ((head ? 0 : chunks) + (uint64_t)chunk) * a.part_ld, c, (uint32_t)a.part_ld, sum);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kValues; ++j) sum[j] = sum[j] * a.scale + (a.add ? float_of(old[u].x[j]) : 0.0f);
+                    if (c + kValues > a.dim) Piece<T>::settle(sum, c, a.dim);
+                    if (c < a.dim) store((O*)a.table + (uint64_t)__builtin_amdgcn_readlane(words, i + u) * a.table_ld, c, a.dim, sum);
                 }
+#pragma unroll
+                for (int j = 0; j < kValues; ++j) sum[j] = 0;
             }
         }
     }
-    flush(hi);
 }
 
-// Words that begin in a chunk and go on behind it.
-template <class O>
-__global__ __launch_bounds__(kThreads) void join_sums_kernel(const EmbedArgs a, uint32_t chunks, uint32_t runs)
+// A word's sum into its row of the table.
+template <class O, int N>
+__device__ inline void write_row(const EmbedArgs& a, uint32_t word, uint32_t c, float (&x)[N])
 {
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint64_t job = blockIdx.x * 4ull + wave;
-    const uint32_t chunk = __builtin_amdgcn_readfirstlane((uint32_t)(job / runs)), run = __builtin_amdgcn_readfirstlane((uint32_t)(job % runs));
-    const uint32_t all = a.start[a.vocab];
+    O* row = (O*)a.table + (uint64_t)word * a.table_ld;
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] *= a.scale;
+    if (a.add) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (c + j < a.dim) x[j] += float_of(row[c + j]);
+    }
+    store(row, c, a.dim, x);
+}
+
+// Words that begin in a chunk and go on behind it: a workgroup a chunk.
+template <class O>
+__global__ __launch_bounds__(kThreads) void join_sums_kernel(const EmbedArgs a, uint32_t chunks)
+{
+    const uint32_t chunk = blockIdx.x, all = a.start[a.vocab];
     const uint64_t lo = (uint64_t)chunk * a.chunk, hi = lo + a.chunk;
-    if (chunk >= chunks || hi >= all) return;
+    if (hi >= all) return;
     const uint32_t word = a.word[hi - 1];
     const uint32_t begin = a.start[word], end = a.start[word + 1];
-    const uint32_t c = (run * 64 + lane) * 4;
-    if (begin < lo || end <= hi || c >= a.dim) return;
+    if (begin < lo || end <= hi) return;
     const uint32_t last = (end - 1) / a.chunk;
     typedef float f32x4 __attribute__((ext_vector_type(4)));
-    f32x4 sum = *(const f32x4*)(a.part + ((uint64_t)chunks + chunk) * a.part_ld + c);
+    for (uint32_t c = (blockIdx.y * kThreads + threadIdx.x) * 4; c < a.dim; c += gridDim.y * kThreads * 4) {
+        f32x4 sum = *(const f32x4*)(a.part + ((uint64_t)chunks + chunk) * a.part_ld + c);
 #pragma unroll 8
-    for (uint32_t k = chunk + 1; k <= last; ++k) sum += *(const f32x4*)(a.part + k * a.part_ld + c);
-    float x[4] = {sum[0], sum[1], sum[2], sum[3]};
-    write_row<O>(a, word, c, x);
+        for (uint32_t k = chunk + 1; k <= last; ++k) sum += *(const f32x4*)(a.part + k * a.part_ld + c);
+        float x[4] = {sum[0], sum[1], sum[2], sum[3]};
+        write_row<O>(a, word, c, x);
+    }
+}
+
+// ---- few tokens ----
+//
+// Up to 128: every wave has all ids in its registers, finds the tokens of 4 words by ballots and writes those rows' run of
+// columns.  One launch and no workspace: sorting so few takes longer than their sums (64 tokens of 64: XXX us, sorted XXX).
+template <class T, class O>
+__global__ __launch_bounds__(kThreads) void few_kernel(const EmbedArgs a)
+{
+    constexpr int kValues = Piece<T>::kValues, kIds = kFewRows / 64, kAhead = 4;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t v0 = (blockIdx.x * 4 + wave) * 4;
+    const uint32_t c = (blockIdx.y * 64 + lane) * kValues, from = Piece<T>::first(c, a.dim);
+    const bool narrow = a.dim < (uint32_t)kValues;
+    int64_t id[kIds];
+#pragma unroll
+    for (int k = 0; k < kIds; ++k) id[k] = a.ids[min(64 * k + lane, a.tokens - 1)];
+    uint32_t word[kIds];
+#pragma unroll
+    for (int k = 0; k < kIds; ++k)
+        word[k] = 64 * k + lane < a.tokens && id[k] >= 0 && id[k] < (int64_t)a.vocab && id[k] != a.ignore_index ? (uint32_t)id[k] : kNoWord;
+    for (uint32_t v = v0; v < min(v0 + 4, a.vocab); ++v) {
+        float sum[kValues];
+#pragma unroll
+        for (int j = 0; j < kValues; ++j) sum[j] = 0;
+        bool any = false;
+#pragma unroll
+        for (int k = 0; k < kIds; ++k) {
+            uint64_t left = __ballot(word[k] == v);
+            any |= left != 0;
+            while (left) {
+                Piece<T> p[kAhead];
+                bool there[kAhead];
+                uint32_t t = 64 * k;
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    there[u] = left != 0;
+                    t = there[u] ? 64 * k + __builtin_ctzll(left | 1ull << 63) : t;
+                    left &= left - 1;
+                    p[u].load((const T*)a.rows + (uint64_t)t * a.rows_ld, from, narrow, a.dim);
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                    for (int j = 0; j < kValues; ++j) sum[j] += there[u] ? p[u].at(j) : 0.0f;
+            }
+        }
+        if (c >= a.dim || (a.add && !any)) continue;
+        if (c + kValues > a.dim) Piece<T>::settle(sum, c, a.dim);
+        if (any)
+            write_row<O>(a, v, c, sum);
+        else
+            store((O*)a.table + (uint64_t)v * a.table_ld, c, a.dim, sum);
+    }
 }
 
 uint64_t cut(uint64_t x, uint64_t by) { return (x + by - 1) / by; }
@@ -355,9 +463,18 @@ hipError_t sums_of(const EmbedArgs& a, hipStream_t stream)
     if ((chunk_blocks + zero_blocks) * kThreads > 0xffffffffu) return hipErrorInvalidValue;
     if (chunk_blocks + zero_blocks)
         sums_kernel<T, O><<<(uint32_t)(chunk_blocks + zero_blocks), kThreads, 0, stream>>>(a, (uint32_t)chunks, (uint32_t)runs, (uint32_t)chunk_blocks);
-    const uint64_t join_runs = cut(a.dim, 256), join_blocks = cut((chunks ? chunks - 1 : 0) * join_runs, 4);
-    if (join_blocks * kThreads > 0xffffffffu) return hipErrorInvalidValue;
-    if (join_blocks) join_sums_kernel<O><<<(uint32_t)join_blocks, kThreads, 0, stream>>>(a, (uint32_t)chunks, (uint32_t)join_runs);
+    // A chunk's columns by as many workgroups as leave each SIMD some waves where words may be long.
+    if (chunks > 1)
+        join_sums_kernel<O><<<dim3((uint32_t)chunks - 1, (uint32_t)std::min<uint64_t>(cut(a.dim, 4 * kThreads), 4)), kThreads, 0, stream>>>(a, (uint32_t)chunks);
+    return hipGetLastError();
+}
+
+template <class T, class O>
+hipError_t few_of(const EmbedArgs& a, hipStream_t stream)
+{
+    const uint64_t blocks = cut(a.vocab, 16), runs = cut(a.dim, 64 * Piece<T>::kValues);
+    if (blocks * runs * kThreads > 0xffffffffu || runs > 65535) return hipErrorInvalidValue;
+    few_kernel<T, O><<<dim3((uint32_t)blocks, (uint32_t)runs), kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -375,6 +492,14 @@ hipError_t launch_sort(const EmbedArgs& a, hipStream_t stream)
     const uint32_t blocks = (uint32_t)cut(a.vocab, a.range);
     sort_kernel<<<blocks, kSortWaves * 64, kSortWaves * a.range * 4, stream>>>(a);
     return hipGetLastError();
+}
+
+hipError_t launch_few_sums(const EmbedArgs& a, hipStream_t stream)
+{
+    if (a.tokens == 0 || a.tokens > kFewRows) return hipErrorInvalidValue;
+    if (a.rows_f32)
+        return a.table_f32 ? few_of<float, float>(a, stream) : few_of<float, uint16_t>(a, stream);
+    return a.table_f32 ? few_of<uint16_t, float>(a, stream) : few_of<uint16_t, uint16_t>(a, stream);
 }
 
 hipError_t launch_table_sums(const EmbedArgs& a, hipStream_t stream)

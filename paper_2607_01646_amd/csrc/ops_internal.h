@@ -262,6 +262,9 @@ struct EmbedArgs {
 constexpr uint32_t kSortWaves = 16, kSortRange = 1000;
 hipError_t launch_lookup(const EmbedArgs& a, hipStream_t stream);
 hipError_t launch_sort(const EmbedArgs& a, hipStream_t stream);
+// Up to kFewRows tokens (at least one): the gradient in one launch, without sorting and workspace.
+constexpr uint32_t kFewRows = 128;
+hipError_t launch_few_sums(const EmbedArgs& a, hipStream_t stream);
 hipError_t launch_table_sums(const EmbedArgs& a, hipStream_t stream);
 
 } // namespace ckpt
