@@ -31,7 +31,7 @@ ckpt_status check_embed(const ckpt_embed_args* a, bool grad)
 struct GradPlan {
     bool few = false;
     uint32_t range = 0, chunk = 0;
-    uint64_t start = 0, order = 0, word = 0, part = 0, part_ld = 0, bytes = 0;
+    uint64_t start = 0, order = 0, word = 0, part = 0, part_ld = 0, join = 0, bytes = 0;
 };
 
 GradPlan plan_grad(const ckpt_embed_args* a)
@@ -59,6 +59,7 @@ GradPlan plan_grad(const ckpt_embed_args* a)
     l.order = take(4 * n);
     l.word = take(4 * n);
     l.part = take(8 * l.part_ld * ((n + chunk - 1) / chunk));
+    l.join = take(8 * ((n + chunk - 1) / chunk));
     l.bytes = at;
     return l;
 }
@@ -145,6 +146,7 @@ extern "C" ckpt_status ckpt_embedding_grad(const ckpt_embed_args* a, int32_t dev
     k.word = (uint32_t*)(w + l.word);
     k.part = (float*)(w + l.part);
     k.part_ld = l.part_ld;
+    k.join = (uint2*)(w + l.join);
     hipError_t err = l.few ? launch_few_sums(k, (hipStream_t)stream) : launch_sort(k, (hipStream_t)stream);
     if (err == hipSuccess && !l.few) err = launch_table_sums(k, (hipStream_t)stream);
     if (err != hipSuccess) return fail_free(CKPT_EHIP, "table's gradient: %s", hipGetErrorString(err));

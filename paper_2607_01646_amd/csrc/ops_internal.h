@@ -257,6 +257,7 @@ struct EmbedArgs {
     uint32_t *order, *word; // [tokens]: the tokens by word, and their words
     float* part;            // [2][chunks][part_ld]: sums of words that a chunk shares with the one before it, and with the one behind it
     uint64_t part_ld;
+    uint2* join; // [chunks]: the word that begins in the chunk and goes on behind it (or none), and its last chunk
 };
 // Counters of a sorting workgroup's waves fit in LDS.
 constexpr uint32_t kSortWaves = 16, kSortRange = 1000;
