@@ -28,6 +28,7 @@ typedef struct {
     uint64_t rows_stride;
     void* table; /* [vocab, dim]: the lookup reads it; the gradient writes it, or adds to it */
     uint64_t table_stride;
+                  /* rows and table: not in one another, from the first to the last element of each */
     uint32_t add; /* the gradient: 0 = every row is written, 1 = added to what is there */
     uint32_t reserved; /* 0 */
 } ckpt_embed_args;

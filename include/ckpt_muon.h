@@ -40,7 +40,7 @@ typedef struct {
 typedef struct {
     const void* in; /* [rows, cols], rows in_stride elements apart */
     uint64_t in_stride;
-    void* out; /* may be `in` itself; outputs do not overlap otherwise */
+    void* out; /* may be `in` itself (with its stride) */
     uint64_t out_stride;
     uint64_t rows, cols; /* up to 2^22 each; 0 is allowed */
 } ckpt_matrix;
@@ -48,7 +48,8 @@ typedef struct {
 /* Orthogonalises n matrices of one type (CKPT_TYPE_*).  `workspace`: 256-byte
  * aligned device memory of at least the bytes that _workspace says, the call's
  * own until its work on `stream` has run (NULL where that is 0).
- * Errors: EINVAL (sizes, numbers, pointers, outputs that overlap), EHIP. */
+ * Results do not overlap each other or other matrices; contiguous ones are
+ * checked.  Errors: EINVAL (sizes, numbers, pointers, overlaps), EHIP. */
 ckpt_status ckpt_orthogonalize_workspace(const ckpt_matrix* m, uint32_t n, const ckpt_newton_schulz* ns,
                                          uint64_t* bytes);
 ckpt_status ckpt_orthogonalize(const ckpt_matrix* m, uint32_t n, uint32_t dtype, const ckpt_newton_schulz* ns,

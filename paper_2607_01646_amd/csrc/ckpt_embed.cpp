@@ -72,6 +72,12 @@ ckpt_status check_pointers(const ckpt_embed_args* a, int device, Known& known)
                            {a->table, a->vocab, a->dim, a->table_stride, te, "table"}};
     for (const Given& g : given)
         if (ckpt_status st = check_given(g, device, known)) return st;
+    // One is written while the other is read.
+    uint64_t rows = 0, table = 0;
+    extent(a->tokens, a->dim, a->rows_stride, e, &rows);
+    extent(a->vocab, a->dim, a->table_stride, te, &table);
+    const uint64_t r = (uint64_t)(uintptr_t)a->rows, t = (uint64_t)(uintptr_t)a->table;
+    if (rows && r < t + table && t < r + rows) return fail_free(CKPT_EINVAL, "rows and table overlap");
     return CKPT_OK;
 }
 

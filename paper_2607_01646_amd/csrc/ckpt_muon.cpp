@@ -258,12 +258,12 @@ ckpt_status muon_jobs(const ckpt_muon_matrix* m, uint32_t n, const ckpt_muon_arg
                          args->grad_dtype);
     if (args->nesterov > 1 || args->reserved) return fail_free(CKPT_EINVAL, "nesterov is 0 or 1, reserved 0");
     if (!(args->momentum >= 0 && args->momentum < 1)) return fail_free(CKPT_EINVAL, "momentum %g is not in [0, 1)", args->momentum);
-    if (!std::isfinite(args->lr) || !std::isfinite(args->weight_decay))
+    if (!std::isfinite(args->lr) || !std::isfinite(args->weight_decay) || !std::isfinite((float)(1 - args->lr * args->weight_decay)))
         return fail_free(CKPT_EINVAL, "lr %g, weight_decay %g", args->lr, args->weight_decay);
     if (ckpt_status st = check_ns(args->ns)) return st;
     for (uint32_t i = 0; i < n; ++i) {
         if (ckpt_status st = sizes(m[i].rows, m[i].cols, i)) return st;
-        if (!std::isfinite(m[i].scale)) return fail_free(CKPT_EINVAL, "matrix %u: scale %g", i, m[i].scale);
+        if (!std::isfinite((float)(args->lr * m[i].scale))) return fail_free(CKPT_EINVAL, "matrix %u: scale %g", i, m[i].scale);
         if (m[i].rows && m[i].cols) add_job(jobs, m[i].rows, m[i].cols);
     }
     return CKPT_OK;

@@ -128,9 +128,9 @@ __device__ inline float update(const MuonArgs& a, float m, float cg)
 
 // ---- the update and its norm ----
 //
-// Bound by HBM: gradient and momentum are read, the momentum written.  The squares' sums are in 64 bits, a tile's each,
-// and added up in their order by every workgroup that needs the norm (at most 2^13 of them for a matrix of 2^25 elements,
-// 64 KiB from the L2; a launch of its own would take longer).
+// Bound by HBM: gradient and momentum are read, the momentum written.  The squares' sums are in 64 bits, a tile's each.
+// Few are added up by every workgroup that needs the norm; more than kMuonParts by one, in a launch of its own (11008 x
+// 4096: each of 11008 workgroups would read 88 KiB).  A matrix's own number of tiles decides that.
 template <class G>
 __global__ __launch_bounds__(kThreads) void first_kernel(const MuonArgs a)
 {
@@ -175,6 +175,17 @@ __global__ __launch_bounds__(kThreads) void first_kernel(const MuonArgs a)
     if (threadIdx.x == 0) a.m[f].part[t] = sum;
 }
 
+__global__ __launch_bounds__(1024) void norm_kernel(const MuonArgs a)
+{
+    __shared__ double s_wave[16];
+    const MuonMatrix& m = a.m[blockIdx.x];
+    if (m.part_n <= kMuonParts) return;
+    double sum = 0;
+    for (uint32_t k = threadIdx.x; k < m.part_n; k += 1024) sum += m.part[k];
+    sum = block_sum<1024>(sum, s_wave);
+    if (threadIdx.x == 0) m.part[0] = sum; // every part was read before the workgroup met
+}
+
 template <class G>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const MuonArgs a)
 {
@@ -189,7 +200,8 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const MuonArgs a)
     const float cs = a.grad_scale ? *a.grad_scale : 1.0f;
     uint16_t* x = a.m[f].x;
     double sum = 0;
-    for (uint32_t k = threadIdx.x; k < a.m[f].part_n; k += kThreads) sum += a.m[f].part[k];
+    const uint32_t parts = a.m[f].part_n <= kMuonParts ? a.m[f].part_n : 1;
+    for (uint32_t k = threadIdx.x; k < parts; k += kThreads) sum += a.m[f].part[k];
     sum = block_sum(sum, s_wave);
     const float over = (float)((double)kUp / (sqrt(sum) + a.eps));
     // Runs of four values of U over its norm, of the rows r0, r0 + by, ..; zeros outside the matrix.
@@ -882,6 +894,12 @@ hipError_t launch_muon_tiny(const MuonArgs& a, const MuonPolynomial& n, hipStrea
 
 hipError_t launch_muon_pack(MuonArgs& a, hipStream_t stream)
 {
+    bool many = false;
+    for (uint32_t i = 0; i < a.count; ++i) many |= a.m[i].part_n > kMuonParts;
+    if (many) {
+        norm_kernel<<<a.count, 1024, 0, stream>>>(a);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
     const uint64_t tiles = number(a, 1, [](const MuonMatrix& m) {
         return m.rows <= m.cols ? blocks(m.rows, kMuonRows) * blocks(((uint64_t)m.cols + 63) / 64 * 64, kMuonCols)
                                 : blocks(m.rows, kMuonTurn) * blocks(m.cols, kMuonTurn);

@@ -230,7 +230,7 @@ struct MuonPolynomial {
 };
 hipError_t launch_muon_tiny(const MuonArgs& a, const MuonPolynomial& n, hipStream_t stream);
 // Elements of the tiles of the launches that are not products.
-constexpr uint32_t kMuonRows = 16, kMuonCols = 256, kMuonTurn = 64;
+constexpr uint32_t kMuonRows = 16, kMuonCols = 256, kMuonTurn = 64, kMuonParts = 1024;
 // Momentum, and the squares of the update.
 hipError_t launch_muon_first(MuonArgs& a, hipStream_t stream);
 // The update over its norm into x.

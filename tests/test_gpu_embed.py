@@ -87,13 +87,15 @@ def test_strides_and_values_that_are_no_numbers():
 
 def reference(d, ids, vocab, scale, old=None):
     """Sums in 64 bits, and bounds: a word's sum of k rows in fp32, k + 4 roundings of partial sums."""
+    d, ids = d.cpu(), ids.cpu()  # (adding to one row on the GPU takes seconds)
     there = (ids >= 0) & (ids < vocab) & (ids != IGNORE)
-    want = torch.zeros(vocab, d.shape[1], dtype=torch.float64, device="cuda")
-    size, count = want.clone(), torch.zeros(vocab, dtype=torch.float64, device="cuda")
+    want = torch.zeros(vocab, d.shape[1], dtype=torch.float64)
+    size = want.clone()
     rows = d[there].double()
     want.index_add_(0, ids[there], rows)
     size.index_add_(0, ids[there], rows.abs())
-    count.index_add_(0, ids[there], torch.ones_like(rows[:, 0]) if rows.numel() else torch.zeros(0, dtype=torch.float64, device="cuda"))
+    count = torch.bincount(ids[there], minlength=vocab).double().cuda()
+    want, size = want.cuda(), size.cuda()
     want, bound = scale * want, abs(scale) * (count + 4)[:, None] * U32 * size
     if old is not None:
         want = want + old.double()
@@ -104,8 +106,8 @@ def reference(d, ids, vocab, scale, old=None):
 @pytest.mark.parametrize("rows, table", [(BF, BF), (F32, F32), (BF, F32), (F32, BF)])
 @pytest.mark.parametrize("kind", ["even", "text", "one"])
 @pytest.mark.parametrize("n, dim, vocab", [(1, 1, 1), (1, 4096, 300), (3, 7, 5), (63, 64, 33), (64, 64, 256), (65, 513, 100),
-                                           (129, 5000, 7), (1000, 1000, 77), (3000, 65, 1001), (5000, 320, 40000), (20000, 9, 3),
-                                           (70000, 130, 2500)])
+                                           (128, 1030, 40), (129, 5000, 7), (1000, 1000, 77), (3000, 65, 1001),
+                                           (5000, 320, 40000), (20000, 9, 3), (70000, 130, 2500)])
 def test_gradient(n, dim, vocab, kind, rows, table):
     d = torch.randn(n, dim, generator=gen(n), device="cuda").to(rows)
     ids = masked(words(n, vocab, kind))
@@ -244,6 +246,45 @@ def test_the_gradient_is_the_lookups():
             assert (value(more) - value(less)) / 2 == float(grad[v, c])
 
 
+def test_without_the_native_module(monkeypatch):
+    """The binding's own code does what the native one does."""
+    from paper_2607_01646_amd import embed
+    ids = masked(words(500, 90, "text")).view(5, 100)
+    table = torch.randn(90, 70, device="cuda").to(BF)
+    rows = P.ckpt_embedding(table, ids, scale=3.0)
+    grad = P.ckpt_embedding_grad(rows, ids, 90, scale=3.0)
+    more = P.ckpt_embedding_grad(rows, ids, 90, add_to=grad.clone())
+    monkeypatch.setattr(embed, "_native", (None, embed._module()[1]))
+    assert torch.equal(P.ckpt_embedding(table, ids, scale=3.0), rows)
+    assert torch.equal(P.ckpt_embedding_grad(rows, ids, 90, scale=3.0), grad)
+    assert torch.equal(P.ckpt_embedding_grad(rows, ids, 90, add_to=grad.clone()), more)
+
+
+def test_no_more_workspace_than_said_and_none_for_few():
+    """The rows behind the last token, and what lies around the workspace, stay as they are."""
+    import ctypes as C
+    from paper_2607_01646_amd import embed
+    for n in (100, 5000):
+        d = torch.randn(n + 10, 200, device="cuda")
+        ids = words(n, 300, "text")
+        a = embed.ckpt_embed_args(dtype=P.CKPT_TYPE_F32, table_dtype=P.CKPT_TYPE_F32, tokens=n, dim=200, vocab=300,
+                                  ids=ids.data_ptr(), ignore_index=IGNORE, scale=1.0, rows=d.data_ptr(), rows_stride=200)
+        table = torch.full((302, 200), 7.0, device="cuda")
+        a.table, a.table_stride = table[1].data_ptr(), 200
+        need = C.c_uint64()
+        assert embed._ops().ckpt_embedding_grad_workspace(C.byref(a), C.byref(need)) == P.CKPT_OK
+        assert (need.value == 0) == (n == 100)
+        work = torch.full((need.value + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+        assert embed._ops().ckpt_embedding_grad(C.byref(a), 0, work[256:].data_ptr() if need.value else None, need.value,
+                                                torch.cuda.current_stream().cuda_stream) == P.CKPT_OK
+        torch.cuda.synchronize()
+        assert (work[:256] == 0x5A).all() and (work[-256:] == 0x5A).all()
+        assert (table[0] == 7).all() and (table[-1] == 7).all()
+        assert torch.equal(table[1:-1], P.ckpt_embedding_grad(d[:n], ids, 300))
+        if need.value:
+            assert embed._ops().ckpt_embedding_grad(C.byref(a), 0, work[256:].data_ptr(), need.value - 1, None) == P.CKPT_EINVAL
+
+
 def test_refusals():
     table = torch.randn(10, 8, device="cuda")
     ids = torch.tensor([1, 2], device="cuda")
@@ -272,6 +313,9 @@ def test_refusals():
     for bad in (table[:9], table[:, :7], table.half(), table.cpu()):
         with pytest.raises(ValueError):
             P.ckpt_embedding_grad(d, ids, 10, add_to=bad)
+    both = torch.randn(14, 8, device="cuda")
+    with pytest.raises(P.CkptError):
+        P.ckpt_embedding_grad(both[9:11], ids, 10, add_to=both[:10])
     with pytest.raises(ValueError):
         P.ckpt_embedding_grad(d, ids, 10, dtype=torch.float16)
     with pytest.raises(ValueError):

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from muon_util import check_orthogonal, step
+from muon_util import check_orthogonal, orthogonal, step
 from ops_util import U32, within
 
 pytestmark = pytest.mark.gpu
@@ -80,6 +80,50 @@ def test_a_matrix_does_not_depend_on_the_others():
         for a, b in zip(P.ckpt_orthogonalize(x, piece_bytes=piece), alone):
             assert torch.equal(a, b), (piece, tuple(a.shape))
     assert P.ckpt_orthogonalize([]) == []
+
+
+@pytest.mark.parametrize("count", [2, 3, 4, 6, 16, 24])
+def test_every_size_of_tiles(count):
+    """So many matrices of the same sides that each size of tiles is the quickest for some launch: a matrix's result is that
+    of its own call, which is checked."""
+    x = [matrix((1000, 1100) if k % 2 else (1100, 1000), BF if count == 4 else F32, seed=k) for k in range(count)]
+    out = P.ckpt_orthogonalize(x)
+    for a, b in zip(out, x):
+        assert torch.equal(a, P.ckpt_orthogonalize([b])[0])
+    for k in range(2):
+        check_orthogonal(out[k], x[k])
+
+
+def test_more_parts_of_a_norm_than_a_workgroup_adds_up():
+    """Above 1024 tiles of 16 x 256: a launch for the norm, beside matrices that need none."""
+    x = [matrix((40, 110)), matrix((70, 70000)), matrix((70000, 65)), matrix((300, 300))]
+    out = P.ckpt_orthogonalize(x)
+    for a, b in zip(out, x):
+        assert torch.equal(a, P.ckpt_orthogonalize([b])[0])
+        check_orthogonal(a, b, str(tuple(b.shape)))
+
+
+def test_without_the_native_module(monkeypatch):
+    """The binding's own code does what the native one does."""
+    from paper_2607_01646_amd import muon
+    lists, _ = state([(33, 65), (96, 3, 5), (200, 70)], BF, BF)
+    twin = [[t.clone() for t in x] for x in lists]
+    x = [matrix((90, 70)), matrix((70, 300))]
+    want = P.ckpt_orthogonalize(x)
+    P.ckpt_muon(*lists, lr=1e-2, scale=0.7, weight_decay=0.1)
+    monkeypatch.setattr(muon, "_native", (None, muon._module()[1]))
+    P.ckpt_muon(*twin, lr=1e-2, scale=0.7, weight_decay=0.1)
+    assert all(torch.equal(a, b) for c, d in zip(lists, twin) for a, b in zip(c, d))
+    assert all(torch.equal(a, b) for a, b in zip(P.ckpt_orthogonalize(x), want))
+
+
+def test_the_step_follows_differences_of_its_definition():
+    """Along a direction: X of U + h D against X of U, which the definition's polynomial gives in 64 bits."""
+    u, d = matrix((96, 160)), matrix((96, 160), seed=1)
+    more, less = P.ckpt_orthogonalize([u + 0.5 * d, u - 0.5 * d])
+    want = orthogonal(u + 0.5 * d) - orthogonal(u - 0.5 * d)
+    # each to its own bound, and these are 1e3 times smaller than the difference
+    assert float(((more - less).double() - want).norm()) < 1e-4 * float(want.norm())
 
 
 def test_strided_rows_and_results_in_place():
@@ -217,6 +261,7 @@ def test_refusals():
                dict(weight_decay=math.inf), dict(scale=math.inf), dict(coefficients=(3.0, 3.0, 3.0)),
                dict(coefficients=(math.nan, 0.0, 0.0))):
         refuse(P.CkptError, p, w, m, g, **kw)
+    refuse(P.CkptError, p, w, m, g, lr=1e30, scale=1e30)
     refuse(P.CkptError, [p[0], p[0]], [w[0], w[0]], [m[0], m[0]], [g[0], g[0]])  # one matrix twice
     refuse(P.CkptError, p, w, w, g)
     with pytest.raises(ValueError):
