@@ -4,7 +4,6 @@
 // the host, and nothing outlives a call.
 #include <algorithm>
 #include <cmath>
-#include <iterator>
 #include <new>
 #include <vector>
 
@@ -15,6 +14,7 @@
 namespace ckpt {
 namespace {
 
+constexpr uint64_t kSingly = 384; // up to this short side: step by step, which is fewer launches and twice as exact
 constexpr uint64_t kDefaultPiece = 4ull << 30; // the matrices of a layer of 4096 x 11008, in one group
 
 ckpt_status check_ns(const ckpt_newton_schulz& ns)
@@ -44,7 +44,7 @@ ckpt_status check_ns(const ckpt_newton_schulz& ns)
 // s^2 l, and of those of the short side 11 instead of 5, in units of s^3.  It is as exact as step by step (a Gram matrix of
 // X itself sets every other step right; with three from one, what is rounded off beside the large singular values grows in
 // the small ones' place until it is all there is).  The product of both factors has to fit the operands' scale.
-bool in_twos(const ckpt_newton_schulz& ns)
+bool fits_twos(const ckpt_newton_schulz& ns)
 {
     constexpr int kGrid = 512;
     for (int k = 0; k <= kGrid; ++k) {
@@ -70,7 +70,8 @@ bool lay_out(Job& j, uint64_t rows, uint64_t cols, uint64_t& at)
 {
     j.s = std::min(rows, cols);
     j.l = std::max(rows, cols);
-    const uint64_t x = up(4 * j.s * up(j.l, 64), 256), a = up(4 * j.s * up(j.s, 64), 256); // at most 2^46 each
+    const bool vector = j.s == 1; // no products
+    const uint64_t x = vector ? 0 : up(4 * j.s * up(j.l, 64), 256), a = vector ? 0 : up(4 * j.s * up(j.s, 64), 256); // at most 2^46 each
     const uint64_t tiles = ((rows + kMuonRows - 1) / kMuonRows) * ((cols + kMuonCols - 1) / kMuonCols);
     j.x = at;
     j.y = j.x + x;
@@ -85,16 +86,22 @@ bool lay_out(Job& j, uint64_t rows, uint64_t cols, uint64_t& at)
     return tiles <= (1u << 23);
 }
 
-// Takes the matrices out that need no workspace: by their own sides, so that a matrix's result does not depend on others.
-std::vector<Job> take_tiny(std::vector<Job>& jobs)
+// The matrices of a call by the way they go, which their own sides decide: a matrix's result does not depend on others.
+struct Jobs {
+    std::vector<Job> vectors; // one row or column
+    std::vector<Job> tiny;    // one launch, no workspace
+    std::vector<Job> others;
+};
+Jobs sorted(const std::vector<Job>& jobs)
 {
-    std::vector<Job> tiny;
-    const auto small = [](const Job& j) {
-        return std::min(j.m.rows, j.m.cols) <= kTinyShort && std::max(j.m.rows, j.m.cols) <= kTinyLong;
-    };
-    std::copy_if(jobs.begin(), jobs.end(), std::back_inserter(tiny), small);
-    jobs.erase(std::remove_if(jobs.begin(), jobs.end(), small), jobs.end());
-    return tiny;
+    Jobs to;
+    for (const Job& j : jobs) {
+        const uint32_t s = std::min(j.m.rows, j.m.cols), l = std::max(j.m.rows, j.m.cols);
+        (s == 1 ? to.vectors : s <= kTinyShort && l <= kTinyLong ? to.tiny : to.others).push_back(j);
+    }
+    std::stable_partition(to.others.begin(), to.others.end(),
+                          [](const Job& j) { return std::min(j.m.rows, j.m.cols) > kSingly; });
+    return to;
 }
 
 // Cuts the matrices into groups: calls `run(first, last)` for each, and finds the bytes that the largest takes.
@@ -112,7 +119,7 @@ ckpt_status grouped(std::vector<Job>& jobs, uint64_t piece_bytes, uint64_t* most
             if (!lay_out(j, j.m.rows, j.m.cols, next))
                 return fail_free(CKPT_EINVAL, "matrix of %u x %u: too many elements", j.m.rows, j.m.cols);
             tiles += std::max<uint64_t>(j.m.part_n, (j.s + 63) / 64 * ((j.l + 63) / 64)); // of any launch, at most
-            if (k > i && (next > budget || tiles > (1u << 23))) break;
+            if (k > i && (next > budget || tiles > (1u << 23) || (j.s > kSingly) != (jobs[i].s > kSingly))) break;
             if (tiles > (1u << 23)) return fail_free(CKPT_EINVAL, "matrix of %u x %u: too many elements", j.m.rows, j.m.cols);
             jobs[k] = j;
             at = next;
@@ -125,6 +132,16 @@ ckpt_status grouped(std::vector<Job>& jobs, uint64_t piece_bytes, uint64_t* most
 }
 
 ckpt_status nothing(size_t, size_t) { return CKPT_OK; }
+
+// The bytes that all of a call needs: its groups run one behind the other.
+ckpt_status needed(Jobs& jobs, uint64_t piece_bytes, uint64_t* bytes)
+{
+    uint64_t vectors = 0;
+    if (ckpt_status st = grouped(jobs.vectors, piece_bytes, &vectors, nothing)) return st;
+    if (ckpt_status st = grouped(jobs.others, piece_bytes, bytes, nothing)) return st;
+    *bytes = std::max(*bytes, vectors);
+    return CKPT_OK;
+}
 
 ckpt_status sizes(uint64_t rows, uint64_t cols, uint32_t i)
 {
@@ -143,25 +160,39 @@ void add_job(std::vector<Job>& jobs, uint64_t rows, uint64_t cols)
 }
 
 // The launches of all groups.  `a`: what they share.
-ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schulz& ns, void* workspace,
+ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_schulz& ns, void* workspace,
                     uint64_t workspace_bytes, hipStream_t s)
 {
     uint64_t need = 0;
-    const std::vector<Job> tiny = take_tiny(jobs);
-    if (ckpt_status st = grouped(jobs, ns.piece_bytes, &need, nothing)) return st;
+    Jobs sides = sorted(all);
+    std::vector<Job>& jobs = sides.others;
+    if (ckpt_status st = needed(sides, ns.piece_bytes, &need)) return st;
     if (need > workspace_bytes)
         return fail_free(CKPT_EINVAL, "workspace of %llu bytes needs %llu", (unsigned long long)workspace_bytes,
                          (unsigned long long)need);
     a.eps = ns.eps;
-    for (size_t i = 0; i < tiny.size(); i += kMuonMats) {
-        a.count = (uint32_t)std::min<size_t>(kMuonMats, tiny.size() - i);
-        for (uint32_t k = 0; k < a.count; ++k) a.m[k] = tiny[i + k].m;
-        const hipError_t err = launch_muon_tiny(a, {(float)ns.a, (float)ns.b, (float)ns.c, ns.steps}, s);
-        if (err != hipSuccess) return fail_free(CKPT_EHIP, "orthogonalisation: %s", hipGetErrorString(err));
-    }
-    const bool twos = in_twos(ns);
     uint8_t* w = (uint8_t*)workspace;
+    const MuonPolynomial polynomial = {(float)ns.a, (float)ns.b, (float)ns.c, ns.steps};
+    const auto done = [](hipError_t err) {
+        return err == hipSuccess ? CKPT_OK : fail_free(CKPT_EHIP, "orthogonalisation: %s", hipGetErrorString(err));
+    };
+    for (size_t i = 0; i < sides.tiny.size(); i += kMuonMats) {
+        a.count = (uint32_t)std::min<size_t>(kMuonMats, sides.tiny.size() - i);
+        for (uint32_t k = 0; k < a.count; ++k) a.m[k] = sides.tiny[i + k].m;
+        if (ckpt_status st = done(launch_muon_tiny(a, polynomial, s))) return st;
+    }
+    const ckpt_status vectors = grouped(sides.vectors, ns.piece_bytes, &need, [&](size_t first, size_t last) {
+        a.count = (uint32_t)(last - first);
+        for (size_t k = first; k < last; ++k) {
+            a.m[k - first] = sides.vectors[k].m;
+            a.m[k - first].part = (double*)(w + sides.vectors[k].part);
+        }
+        return done(launch_muon_vectors(a, polynomial, s));
+    });
+    if (vectors) return vectors;
+    const bool fits = fits_twos(ns);
     return grouped(jobs, ns.piece_bytes, &need, [&](size_t first, size_t last) {
+        const bool twos = fits && jobs[first].s > kSingly;
         a.count = (uint32_t)(last - first);
         for (size_t k = first; k < last; ++k) {
             a.m[k - first] = jobs[k].m;
@@ -170,6 +201,7 @@ ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schul
         }
         hipError_t err = launch_muon_first(a, s);
         if (err == hipSuccess) err = launch_muon_pack(a, s);
+        const auto k_of = [](uint64_t Job::*p, const Job& j) { return (uint32_t)up(p == &Job::x || p == &Job::y ? j.l : j.s, 64); };
         // out = cb c + cc p q of all matrices, and with `poly` ca I in it.
         const auto tri = [&](uint64_t Job::*p, uint64_t Job::*q, uint64_t Job::*out, bool poly) {
             if (err != hipSuccess) return;
@@ -182,7 +214,7 @@ ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schul
                 const Job& j = jobs[k];
                 const auto at = [&](uint64_t Job::*o) { return (uint16_t*)(w + j.*o); };
                 t.m[k - first] = {at(p), at(q), poly ? at(p) : nullptr, at(out), (uint32_t)j.s,
-                                  (uint32_t)up(p == &Job::x || p == &Job::y ? j.l : j.s, 64), 0, 0};
+                                  k_of(p, j), 0, muon_chunk(k_of(p, j), p == &Job::x || p == &Job::y)};
             }
             err = launch_muon_tri(t, s);
         };
@@ -210,7 +242,7 @@ ckpt_status run_all(std::vector<Job>& jobs, MuonArgs& a, const ckpt_newton_schul
             }
             err = launch_muon_apply(a, step == ns.steps, s);
         }
-        return err == hipSuccess ? CKPT_OK : fail_free(CKPT_EHIP, "orthogonalisation: %s", hipGetErrorString(err));
+        return done(err);
     });
 }
 
@@ -293,8 +325,8 @@ extern "C" ckpt_status ckpt_orthogonalize_workspace(const ckpt_matrix* m, uint32
         std::vector<Job> jobs;
         if (!bytes) return fail_free(CKPT_EINVAL, "null argument");
         if (ckpt_status st = orthogonalize_jobs(m, n, ns, jobs)) return st;
-        take_tiny(jobs);
-        return grouped(jobs, ns->piece_bytes, bytes, nothing);
+        Jobs sides = sorted(jobs);
+        return needed(sides, ns->piece_bytes, bytes);
     });
 }
 
@@ -347,8 +379,8 @@ extern "C" ckpt_status ckpt_muon_workspace(const ckpt_muon_matrix* m, uint32_t n
         std::vector<Job> jobs;
         if (!bytes) return fail_free(CKPT_EINVAL, "null argument");
         if (ckpt_status st = muon_jobs(m, n, args, jobs)) return st;
-        take_tiny(jobs);
-        return grouped(jobs, args->ns.piece_bytes, bytes, nothing);
+        Jobs sides = sorted(jobs);
+        return needed(sides, args->ns.piece_bytes, bytes);
     });
 }
 

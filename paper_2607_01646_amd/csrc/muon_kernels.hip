@@ -186,6 +186,43 @@ __global__ __launch_bounds__(1024) void norm_kernel(const MuonArgs a)
     if (threadIdx.x == 0) m.part[0] = sum; // every part was read before the workgroup met
 }
 
+// Matrices of one row or one column: X stays a multiple of the update, and A is a number.  All of it behind first_kernel, in
+// the same tiles.
+template <class G>
+__global__ __launch_bounds__(kThreads) void vector_kernel(const MuonArgs a, const MuonPolynomial n)
+{
+    __shared__ double s_wave[kThreads / 64];
+    const uint32_t f = matrix_of(a, blockIdx.x), t = blockIdx.x - a.m[f].first;
+    const MuonMatrix& m = a.m[f];
+    const uint32_t rows = m.rows, cols = m.cols, nc = (cols + kMuonCols - 1) / kMuonCols;
+    double sum = 0;
+    const uint32_t parts = m.part_n <= kMuonParts ? m.part_n : 1;
+    for (uint32_t k = threadIdx.x; k < parts; k += kThreads) sum += m.part[k];
+    const double norm = sqrt(block_sum(sum, s_wave));
+    double x = norm / (norm + a.eps), factor = 1 / (norm + a.eps);
+    for (uint32_t step = 0; step < n.steps; ++step) {
+        const double s = x * x, by = n.ca + s * (n.cb + s * n.cc);
+        x *= by;
+        factor *= by;
+    }
+    const float cs = a.grad_scale ? *a.grad_scale : 1.0f;
+    const uint32_t r0 = t / nc * kMuonRows, c0 = t % nc * kMuonCols;
+    const uint32_t r = rows == 1 ? 0 : r0 + threadIdx.x, c = rows == 1 ? c0 + threadIdx.x : 0;
+    if (r >= rows || c >= cols || (rows != 1 && threadIdx.x >= kMuonRows)) return;
+    float u = load1((const G*)m.in + r * m.in_ld + c);
+    const uint64_t at = (uint64_t)r * cols + c;
+    if (m.momentum) u = update(a, m.momentum[at], cs * u);
+    float y = (float)((double)u * factor);
+    if (m.master) {
+        y = m.master[at] * a.keep - y * m.scale;
+        m.master[at] = y;
+    }
+    if (a.out_f32)
+        ((float*)m.out)[r * m.out_ld + c] = y;
+    else
+        ((uint16_t*)m.out)[r * m.out_ld + c] = bf16_of(y);
+}
+
 template <class G>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const MuonArgs a)
 {
@@ -509,25 +546,27 @@ template <class S>
 __global__ __launch_bounds__(S::kThreads, S::kThreads >= 512 ? 2 : 1) void tri_kernel(const TriArgs a)
 {
     CKPT_BUFFERS(S, S);
-    static_assert(S::BP == S::BQ && S::kThreads / 64 * kTurnWave <= S::kBuffer, "");
+    static_assert(S::BQ % S::BP == 0 && S::kThreads / 64 * kTurnWave <= S::kBuffer, "");
     const uint32_t lane = threadIdx.x & 63;
     const uint32_t at = nth_tile(a.shares, gridDim.x);
     const uint64_t before = __ballot(lane < a.count && a.m[lane < kMuonMats ? lane : 0].first <= at);
     const TriMatrix m = a.m[__builtin_amdgcn_readfirstlane(63 - __builtin_clzll(before))];
-    const uint32_t n = (m.s + S::BP - 1) / S::BP;
+    // Row i of the triangle, of BQ values of q, has kWide tiles more than the one before it.
+    constexpr uint32_t kWide = S::BQ / S::BP;
+    const uint32_t n = (m.s + S::BQ - 1) / S::BQ;
     uint32_t t;
-    if (!tile_in(a.shares, at - m.first, n * (n + 1) / 2, t)) return;
-    // Row i of the triangle begins at tile i (i + 1) / 2.
-    uint32_t i = (uint32_t)((__builtin_sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-    while (i * (i + 1) / 2 > t) --i;
-    while ((i + 1) * (i + 2) / 2 <= t) ++i;
-    const uint32_t j = t - i * (i + 1) / 2;
+    if (!tile_in(a.shares, at - m.first, kWide * (n * (n + 1) / 2), t)) return;
+    uint32_t i = (uint32_t)((__builtin_sqrtf(8.0f * (t / kWide) + 1.0f) - 1.0f) * 0.5f);
+    while (kWide * (i * (i + 1) / 2) > t) --i;
+    while (kWide * ((i + 1) * (i + 2) / 2) <= t) ++i;
+    const uint32_t j = t - kWide * (i * (i + 1) / 2);
+    if (j * S::BP >= m.s) return; // past the matrix: its last row of tiles may be less than half full
     const Operand P = {m.p, (uint64_t)m.s * m.k, m.k, m.s, m.k};
     const Operand Q = {m.q, (uint64_t)m.s * m.k, m.k, m.s, m.k};
     const uint32_t ld = up64(m.s);
     const TriEnd end = {m.out, m.c, (uint64_t)m.s * ld, m.s, ld, a.ca, a.cb, a.cc};
     product<S>(P, Q, {m.s, m.s, m.k, 1, false}, end, make_uint2(__builtin_amdgcn_readfirstlane(j), __builtin_amdgcn_readfirstlane(i)),
-               t, 0, s0, s1, s2, s3);
+               t, 0, s0, s1, s2, s3, m.chunk);
 }
 
 // [q][p] is [short][long]; for the last X of a tall matrix [long][short], as it lies.  W: the shape of the one, T: of the other.
@@ -538,24 +577,25 @@ __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply
     const uint32_t at = nth_tile(a.shares, gridDim.x);
     const MuonMatrix& m = a.m[matrix_of(a, at)];
     const uint32_t s = min(m.rows, m.cols), l = max(m.rows, m.cols), ldx = up64(l), lda = up64(s);
-    const uint32_t ns = (s + W::BP - 1) / W::BP, nl = (l + W::BP - 1) / W::BP;
     const bool wide = std::is_same_v<End, NextEnd> || m.rows <= m.cols;
-    const uint32_t p = wide ? l : s, q = wide ? s : l, np = wide ? nl : ns, nq = wide ? ns : nl;
+    static_assert(W::BP == T::BP && W::BQ == T::BQ, "");
+    const uint32_t p = wide ? l : s, q = wide ? s : l, np = (p + W::BP - 1) / W::BP, nq = (q + W::BQ - 1) / W::BQ;
     uint32_t t;
-    if (!tile_in(a.shares, at - m.first, ns * nl, t)) return;
+    if (!tile_in(a.shares, at - m.first, np * nq, t)) return;
+    const uint32_t chunk = muon_chunk(lda, false);
     const uint32_t band = t / (kBand * np), in = t % (kBand * np), width = min(kBand, nq - band * kBand);
     const uint2 tile = make_uint2(in / width, band * kBand + in % width);
     const Operand X = {m.x, (uint64_t)s * ldx, ldx, s, ldx};
     const Operand B = {m.f, (uint64_t)s * lda, lda, s, lda};
     if constexpr (std::is_same_v<End, NextEnd>) {
         const NextEnd end = {m.y, (uint64_t)s * ldx, s, ldx};
-        product<W>(X, B, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3);
+        product<W>(X, B, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3, chunk);
     } else {
         const LastEnd end = {m.master, m.out, m.out_ld, p, q, a.keep, m.scale, a.out_f32};
         if (wide)
-            product<W>(X, B, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3);
+            product<W>(X, B, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3, chunk);
         else
-            product<T>(B, X, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3);
+            product<T>(B, X, {p, q, lda, 1, false}, end, tile, t, 0, s0, s1, s2, s3, chunk);
     }
 }
 
@@ -777,28 +817,28 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
 
 // ---- shapes ----
 
-// Workgroup tiles, and what a step of 64 values of k takes one of them (us) where each compute unit has one, and where all
-// have two, at once or one behind the other; and what two rounds take more for their first loads and ends.
-//   256 x 256, 8 waves of 64 x 128: 1.33 PFLOP/s on the planes while all units are busy
-//   128 x 128, 4 waves of 64 x 64, two workgroups a unit: 1.0 PFLOP/s
-//   128 x 128, 8 waves of 64 x 32, one workgroup a unit: for so few tiles that no unit has two (A of 2048 x 8192: 126 us,
-//              with 4 waves 167)
+// Workgroup tiles, and what a step of 64 values of k takes one of them (us) where each compute unit has one; for its first
+// loads and its end each takes some us more.  One workgroup a unit.
+//   256 x 256, 8 waves of 64 x 128: 1.33 PFLOP/s on the planes while all units are busy; no registers for sums in parts
+//   128 x 256, 8 waves of 64 x 64: 1.17
+//   128 x 128, 8 waves of 64 x 32: 1.0; the quickest where there are no more tiles than units (A of 2048 x 8192: 126 us;
+//              by 4 waves, two workgroups a unit, 173)
 //   64 x 64,   4 waves of 32 x 32, for few tiles and short k; three buffers, as its loads come from other XCDs' writes (a
 //              matrix of 777 x 1003: 202 us, with two 239)
-enum Size { kSmall, kMiddle, kAlone, kLarge };
-constexpr uint32_t kSide[] = {64, 128, 128, 256};
+enum Size { kSmall, kMiddle, kWide, kLarge };
 constexpr struct {
-    double alone, both, round;
-} kTime[] = {{0.5, 1.0, 8}, {1.6, 3.1, 8}, {1.25, 0, 12}, {4.9, 9.8, 20}};
+    uint32_t p, q;
+    double few, many, end; // us a step with up to 128 tiles, and with 256 and more; us a tile
+} kTile[] = {{64, 64, 0.48, 0.56, 4}, {128, 128, 1.05, 1.75, 6}, {128, 256, 1.9, 2.75, 8}, {256, 256, 3.4, 4.9, 10}};
 
 template <bool PA, bool QA>
 using Large = Shape<2, 2, PA, QA, 256, 256, 4, 2, 32, 2, true>;
 template <bool PA, bool QA>
-using Middle = Shape<2, 2, PA, QA, 128, 128, 2, 2, 32, 2, true>;
+using Wide = Shape<2, 2, PA, QA, 128, 256, 2, 4, 32, 3, true, true>;
 template <bool PA, bool QA>
-using Alone = Shape<2, 2, PA, QA, 128, 128, 2, 4, 64, 2, true>;
+using Middle = Shape<2, 2, PA, QA, 128, 128, 2, 4, 64, 2, true, true>;
 template <bool PA, bool QA>
-using Small = Shape<2, 2, PA, QA, 64, 64, 2, 2, 64, 3, true>;
+using Small = Shape<2, 2, PA, QA, 64, 64, 2, 2, 64, 3, true, true>;
 
 uint64_t blocks(uint64_t x, uint32_t side) { return (x + side - 1) / side; }
 
@@ -814,30 +854,28 @@ uint64_t number(A& a, uint32_t round, F tiles)
     return all;
 }
 
-// The size of tiles that is done first, of products that have `tiles(m, side)` with `steps(m)` of 64 values of k each, the
-// longest first.
+// The size of tiles that is done first, of products that have `tiles(m, size)` with `steps(m)` of 64 values of k each, the
+// longest first; `parts`: some have sums in parts.
 template <class A, class T, class K>
-Size size_of(const A& a, T tiles, K steps)
+Size size_of(const A& a, bool parts, T tiles, K steps)
 {
     Size best = kSmall;
     double least = 1e30;
     for (int z = kSmall; z <= kLarge; ++z) {
-        const auto& c = kTime[z];
+        if (z == kLarge && parts) continue;
+        const auto& c = kTile[z];
         uint64_t all = 0, work = 0;
         for (uint32_t i = 0; i < a.count; ++i) {
-            const uint64_t n = tiles(a.m[i], kSide[z]);
+            const uint64_t n = tiles(a.m[i], (Size)z);
             all += n;
             work += n * steps(a.m[i]);
         }
-        if (z == kAlone && all > 256) continue;
         const double most = (double)steps(a.m[0]), mean = (double)work / (double)all;
-        const uint64_t pairs = all / 512, left = all % 512;
-        double t = (double)pairs * (mean * c.both + c.round);
-        if (left > 256)
-            t += mean * c.both + c.round;
-        else if (left)
-            t += mean * c.alone + c.round / 2;
-        t = std::max(t, most * c.alone + c.round / 2);
+        const uint64_t rounds = all / 256, left = all % 256;
+        const auto step = [&](uint64_t n) { return n <= 128 ? c.few : c.few + (c.many - c.few) * (double)(std::min<uint64_t>(n, 256) - 128) / 128; };
+        double t = (double)rounds * (mean * c.many + c.end);
+        if (left) t += mean * step(rounds ? left : all) + c.end;
+        t = std::max(t, most * step(all) + c.end);
         if (t < least) least = t, best = (Size)z;
     }
     return best;
@@ -855,20 +893,24 @@ template <class End>
 hipError_t apply(MuonArgs& a, hipStream_t stream)
 {
     constexpr bool kNext = std::is_same_v<End, NextEnd>;
-    const auto tiles = [](const MuonMatrix& m, uint32_t side) {
-        return blocks(std::min(m.rows, m.cols), side) * blocks(std::max(m.rows, m.cols), side);
+    const auto tiles = [](const MuonMatrix& m, Size z) {
+        const bool wide = kNext || m.rows <= m.cols;
+        const uint32_t s = std::min(m.rows, m.cols), l = std::max(m.rows, m.cols);
+        return blocks(wide ? l : s, kTile[z].p) * blocks(wide ? s : l, kTile[z].q);
     };
     const auto steps = [](const MuonMatrix& m) { return blocks(std::min(m.rows, m.cols), 64); };
     std::stable_sort(a.m, a.m + a.count, [&](const MuonMatrix& x, const MuonMatrix& y) { return steps(x) > steps(y); });
-    const Size size = size_of(a, tiles, steps);
+    bool parts = false;
+    for (uint32_t i = 0; i < a.count; ++i) parts |= muon_chunk((uint32_t)steps(a.m[i]) * 64, false) != 0;
+    const Size size = size_of(a, parts, tiles, steps);
     a.shares = steps(a.m[0]) != steps(a.m[a.count - 1]);
-    const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const MuonMatrix& m) { return tiles(m, kSide[size]); });
+    const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const MuonMatrix& m) { return tiles(m, size); });
     using LT = std::conditional_t<kNext, Large<true, false>, Large<false, true>>;
-    using AT = std::conditional_t<kNext, Alone<true, false>, Alone<false, true>>;
+    using WT = std::conditional_t<kNext, Wide<true, false>, Wide<false, true>>;
     using MT = std::conditional_t<kNext, Middle<true, false>, Middle<false, true>>;
     using ST = std::conditional_t<kNext, Small<true, false>, Small<false, true>>;
     return size == kLarge    ? launch_tiles(apply_kernel<Large<true, false>, LT, End>, &a, all, LT::kThreads, stream)
-           : size == kAlone  ? launch_tiles(apply_kernel<Alone<true, false>, AT, End>, &a, all, AT::kThreads, stream)
+           : size == kWide   ? launch_tiles(apply_kernel<Wide<true, false>, WT, End>, &a, all, WT::kThreads, stream)
            : size == kMiddle ? launch_tiles(apply_kernel<Middle<true, false>, MT, End>, &a, all, MT::kThreads, stream)
                              : launch_tiles(apply_kernel<Small<true, false>, ST, End>, &a, all, ST::kThreads, stream);
 }
@@ -892,14 +934,30 @@ hipError_t launch_muon_tiny(const MuonArgs& a, const MuonPolynomial& n, hipStrea
     return hipGetLastError();
 }
 
-hipError_t launch_muon_pack(MuonArgs& a, hipStream_t stream)
+static hipError_t launch_norms(const MuonArgs& a, hipStream_t stream)
 {
     bool many = false;
     for (uint32_t i = 0; i < a.count; ++i) many |= a.m[i].part_n > kMuonParts;
-    if (many) {
-        norm_kernel<<<a.count, 1024, 0, stream>>>(a);
-        if (const hipError_t e = hipGetLastError()) return e;
-    }
+    if (!many) return hipSuccess;
+    norm_kernel<<<a.count, 1024, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_muon_vectors(MuonArgs& a, const MuonPolynomial& n, hipStream_t stream)
+{
+    if (const hipError_t e = launch_muon_first(a, stream)) return e;
+    if (const hipError_t e = launch_norms(a, stream)) return e;
+    const uint64_t tiles = number(a, 1, [](const MuonMatrix& m) { return (uint64_t)m.part_n; });
+    if (a.in_f32)
+        vector_kernel<float><<<(uint32_t)tiles, kThreads, 0, stream>>>(a, n);
+    else
+        vector_kernel<uint16_t><<<(uint32_t)tiles, kThreads, 0, stream>>>(a, n);
+    return hipGetLastError();
+}
+
+hipError_t launch_muon_pack(MuonArgs& a, hipStream_t stream)
+{
+    if (const hipError_t e = launch_norms(a, stream)) return e;
     const uint64_t tiles = number(a, 1, [](const MuonMatrix& m) {
         return m.rows <= m.cols ? blocks(m.rows, kMuonRows) * blocks(((uint64_t)m.cols + 63) / 64 * 64, kMuonCols)
                                 : blocks(m.rows, kMuonTurn) * blocks(m.cols, kMuonTurn);
@@ -910,17 +968,19 @@ hipError_t launch_muon_pack(MuonArgs& a, hipStream_t stream)
 
 hipError_t launch_muon_tri(TriArgs& a, hipStream_t stream)
 {
-    const auto tiles = [](const TriMatrix& m, uint32_t side) {
-        const uint64_t n = blocks(m.s, side);
-        return n * (n + 1) / 2;
+    const auto tiles = [](const TriMatrix& m, Size z) {
+        const uint64_t n = blocks(m.s, kTile[z].q);
+        return n * (n + 1) / 2 * (kTile[z].q / kTile[z].p);
     };
     const auto steps = [](const TriMatrix& m) { return (uint64_t)m.k / 64; };
     std::stable_sort(a.m, a.m + a.count, [&](const TriMatrix& x, const TriMatrix& y) { return x.k > y.k; });
-    const Size size = size_of(a, tiles, steps);
+    bool parts = false;
+    for (uint32_t i = 0; i < a.count; ++i) parts |= a.m[i].chunk != 0;
+    const Size size = size_of(a, parts, tiles, steps);
     a.shares = steps(a.m[0]) != steps(a.m[a.count - 1]);
-    const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const TriMatrix& m) { return tiles(m, kSide[size]); });
+    const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const TriMatrix& m) { return tiles(m, size); });
     return size == kLarge    ? launch_tiles(tri_kernel<Large<false, false>>, &a, all, Large<false, false>::kThreads, stream)
-           : size == kAlone  ? launch_tiles(tri_kernel<Alone<false, false>>, &a, all, Alone<false, false>::kThreads, stream)
+           : size == kWide   ? launch_tiles(tri_kernel<Wide<false, false>>, &a, all, Wide<false, false>::kThreads, stream)
            : size == kMiddle ? launch_tiles(tri_kernel<Middle<false, false>>, &a, all, Middle<false, false>::kThreads, stream)
                              : launch_tiles(tri_kernel<Small<false, false>>, &a, all, Small<false, false>::kThreads, stream);
 }

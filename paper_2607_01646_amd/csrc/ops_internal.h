@@ -210,11 +210,21 @@ struct MuonArgs {
     const float* grad_scale;
     bool nesterov, in_f32, out_f32, shares;
 };
+// Values of k whose products are added up together before they are added to the sum (0: all): of X X^T, which the norms of
+// rows are, and where there are few, whose rounding fp32 would not hide.  A matrix's own sides decide.
+inline
+#ifdef __HIPCC__
+    __host__ __device__
+#endif
+    uint32_t muon_chunk(uint32_t k, bool gram)
+{
+    return k <= 384 ? 128 : !gram ? 0 : k <= 1024 ? 256 : 512;
+}
 // Symmetric products out = ca I + cb c + cc p q, p q^T of rows of k values; no c: cc p q alone.
 struct TriMatrix {
     const uint16_t *p, *q, *c;
     uint16_t* out;
-    uint32_t s, k, first, unused;
+    uint32_t s, k, first, chunk; // chunk: muon_chunk
 };
 struct TriArgs {
     TriMatrix m[kMuonMats];
@@ -228,6 +238,8 @@ struct MuonPolynomial {
     float ca, cb, cc;
     uint32_t steps;
 };
+// Matrices of one row or column: `part` is all that they need of the workspace.
+hipError_t launch_muon_vectors(MuonArgs& a, const MuonPolynomial& n, hipStream_t stream);
 hipError_t launch_muon_tiny(const MuonArgs& a, const MuonPolynomial& n, hipStream_t stream);
 // Elements of the tiles of the launches that are not products.
 constexpr uint32_t kMuonRows = 16, kMuonCols = 256, kMuonTurn = 64, kMuonParts = 1024;

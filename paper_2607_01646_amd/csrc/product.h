@@ -163,10 +163,14 @@ __device__ inline uint2 tile_of(uint32_t block, uint32_t np, uint32_t nq)
 //
 // 2 and 2 (HALF): planes of fp16, hi = x and lo = x - hi rounded to nearest, 22 bits together; hi hi, hi lo and lo hi are
 // made, and lo lo, 2^-22 of the value, is left out.
-template <int ZP_, int ZQ_, bool PA_, bool QA_, int BP_, int BQ_, int NWP_, int NWQ_, int BK_, int BUFS_, bool HALF_ = false>
+//
+// PARTS: the sums of every `chunk` values of k are added up in registers of their own.  A sum that grows is rounded by more
+// and more (of squares, 8192 values of k: 9.5e-7 of it in one go), with two planes 3 times for every 16 values.
+template <int ZP_, int ZQ_, bool PA_, bool QA_, int BP_, int BQ_, int NWP_, int NWQ_, int BK_, int BUFS_, bool HALF_ = false,
+          bool PARTS_ = false>
 struct Shape {
     static constexpr int ZP = ZP_, ZQ = ZQ_, BP = BP_, BQ = BQ_, NWP = NWP_, NWQ = NWQ_, BK = BK_, BUFS = BUFS_;
-    static constexpr bool PA = PA_, QA = QA_, HALF = HALF_;
+    static constexpr bool PA = PA_, QA = QA_, HALF = HALF_, PARTS = PARTS_;
     // Products of planes whose indexes sum to more than this are left out.
     static constexpr int kMostSum = ZP == 3 && ZQ == 3 ? 2 : HALF && ZP == 2 && ZQ == 2 ? 1 : ZP + ZQ - 2;
     static constexpr int kThreads = NWP * NWQ * 64;
@@ -185,7 +189,8 @@ struct Shape {
 // Tile `tile` (of p and q) by the `block`-th of the tiles' workgroups, for run `slice` of k.
 template <class S, class End>
 __device__ inline void product(const Operand& P, const Operand& Q, const ProductShape& shape, const End& end,
-                               uint2 tile, uint32_t block, uint32_t slice, uint16_t* s0, uint16_t* s1, uint16_t* s2, uint16_t* s3)
+                               uint2 tile, uint32_t block, uint32_t slice, uint16_t* s0, uint16_t* s1, uint16_t* s2, uint16_t* s3,
+                               uint32_t chunk = 0)
 {
     constexpr int ZP = S::ZP, ZQ = S::ZQ, BK = S::BK, BUFS = S::BUFS, kThreads = S::kThreads;
     constexpr int TP = S::BP / S::NWP / 32, TQ = S::BQ / S::NWQ / 32;
@@ -307,15 +312,57 @@ __device__ inline void product(const Operand& P, const Operand& Q, const Product
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((BUFS - 1) * kLoads) : "memory");
     read(even, s0, 0);
     uint32_t step = first;
-    for (; step + BUFS <= last; step += BUFS) {
-        one_step(s0, s1, step);
-        one_step(s1, BUFS > 2 ? s2 : s0, step + 1);
-        if constexpr (BUFS > 2) one_step(s2, BUFS > 3 ? s3 : s0, step + 2);
-        if constexpr (BUFS > 3) one_step(s3, s0, step + 3);
+    // PARTS: `chunk` is a multiple of 64, or 0 for one sum of all.
+    f32x16 sum[S::PARTS ? TP : 1][S::PARTS ? TQ : 1];
+    uint32_t part_end = chunk ? first + chunk / BK : 0xffffffffu;
+    if constexpr (S::PARTS) {
+#pragma unroll
+        for (int a = 0; a < TP; ++a)
+#pragma unroll
+            for (int b = 0; b < TQ; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[a][b][i] = 0;
     }
+    auto begin = [&](uint32_t at) { // a step
+        if constexpr (S::PARTS) {
+            if (at != part_end) return;
+            part_end += chunk / BK;
+#pragma unroll
+            for (int a = 0; a < TP; ++a)
+#pragma unroll
+                for (int b = 0; b < TQ; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[a][b][i] += acc[a][b][i], acc[a][b][i] = 0;
+        }
+    };
+    for (; step + BUFS <= last; step += BUFS) {
+        begin(step);
+        one_step(s0, s1, step);
+        begin(step + 1);
+        one_step(s1, BUFS > 2 ? s2 : s0, step + 1);
+        if constexpr (BUFS > 2) {
+            begin(step + 2);
+            one_step(s2, BUFS > 3 ? s3 : s0, step + 2);
+        }
+        if constexpr (BUFS > 3) {
+            begin(step + 3);
+            one_step(s3, s0, step + 3);
+        }
+    }
+    begin(step);
     if (step < last) one_step(s0, s1, step);
+    begin(step + 1);
     if (BUFS > 2 && step + 1 < last) one_step(s1, s2, step + 1);
+    begin(step + 2);
     if (BUFS > 3 && step + 2 < last) one_step(s2, s3, step + 2);
+    if constexpr (S::PARTS) {
+#pragma unroll
+        for (int a = 0; a < TP; ++a)
+#pragma unroll
+            for (int b = 0; b < TQ; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[a][b][i] += sum[a][b][i];
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // no load is left that would write the LDS of another workgroup
     Finish<End, TP, TQ>::run(end, early, acc, p0 + wp, q0 + wq, slice, s0);
 }

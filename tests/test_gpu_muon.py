@@ -14,7 +14,7 @@ if torch.cuda.is_available():
     import paper_2607_01646_amd as P
 
 BF, F32 = torch.bfloat16, torch.float32
-SHAPES = [(1, 1), (1, 7), (7, 1), (2, 3), (31, 33), (63, 65), (64, 64), (65, 64), (64, 256), (130, 70), (127, 513),
+SHAPES = [(1, 1), (1, 7), (7, 1), (1, 5000), (3000, 1), (2, 3), (31, 33), (63, 65), (64, 64), (65, 64), (64, 256), (130, 70), (127, 513),
           (300, 1000), (1000, 300), (512, 512), (257, 2049)]
 
 

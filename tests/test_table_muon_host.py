@@ -136,6 +136,8 @@ def up(x, a):
 def bytes_of(r, c):
     s, l = min(r, c), max(r, c)
     tiles = -(-r // 16) * -(-c // 256)
+    if s == 1:
+        return up(8 * tiles, 256)
     return 2 * up(4 * s * up(l, 64), 256) + 3 * up(4 * s * up(s, 64), 256) + up(8 * tiles, 256)
 
 
@@ -146,7 +148,8 @@ def test_the_workspace_is_bounded_by_the_piece(piece):
     rc, n = need_orth(shapes, piece_bytes=piece)
     largest = max(bytes_of(*s) for s in shapes)
     assert rc == P.CKPT_OK and largest <= n <= max(piece or 4 << 30, largest)
-    assert need_orth([(64, 256), (1, 1), (200, 64), (5, 0)]) == (P.CKPT_OK, 0)
+    assert need_orth([(64, 256), (2, 2), (200, 64), (5, 0)]) == (P.CKPT_OK, 0)
+    assert need_orth([(1, 5), (70000, 1), (64, 64)]) == (P.CKPT_OK, up(bytes_of(1, 5), 256) + bytes_of(70000, 1))
     assert need_orth([]) == (P.CKPT_OK, 0)
     assert need_orth([(300, 200)]) == (P.CKPT_OK, bytes_of(300, 200))
 
@@ -227,8 +230,8 @@ def test_products_wait_for_no_load_that_is_to_stay_in_flight():
     """In the loops of the large products nothing but the barrier at which the waves meet waits for the loads made since the
     last one."""
     text = kernels("muon_kernels.hip")
-    bodies = re.findall(r"^(_ZN4ckpt\w*(?:tri|apply)_kernelI\w*Li256ELi256E\w*):\s(.*?)s_endpgm", text, re.S | re.M)
-    assert len(bodies) == 3
+    bodies = re.findall(r"^(_ZN4ckpt\w*(?:tri|apply)_kernelI\w*Li(?:256|128)ELi256E\w*):\s(.*?)s_endpgm", text, re.S | re.M)
+    assert len(bodies) == 6
     for name, body in bodies:
         lines = [x.strip() for x in body.split("\n") if x.strip() and not x.strip().startswith(";")]
         labels = {x.split(":")[0]: i for i, x in enumerate(lines) if x.startswith(".L")}
@@ -249,4 +252,4 @@ def test_products_wait_for_no_load_that_is_to_stay_in_flight():
                     assert flying == 0 or after.startswith("s_barrier"), (name, x, after)
                 elif x.startswith("s_barrier"):
                     flying = 0
-            assert waits
+            assert waits or "Li32ELi3E" in name  # three buffers: the meeting leaves a step's loads in flight, too
