@@ -43,10 +43,10 @@ GradPlan plan_grad(const ckpt_embed_args* a)
     if (l.few) return l;
     // Sorting workgroups: each reads all ids, so no more than the GPU has units, unless LDS holds no more words.
     l.range = (uint32_t)std::min<uint64_t>(std::max<uint64_t>((a->vocab + 255) / 256, 32), kSortRange);
-    // Sorted tokens that a wave sums: 64 ids at a time, as long as that leaves each SIMD four waves; and no more than 1024
+    // Sorted tokens that a wave sums: 64 ids at a time, as long as that leaves each SIMD two waves (8192 tokens of 4096: 61 us with the table, with four waves 70); and no more than 1024
     // chunks, which bounds what is joined for a word that most tokens have.
     uint64_t chunk = std::max<uint64_t>(64, up((n + 1023) / 1024, 64));
-    while (chunk > 8 && (n + chunk - 1) / chunk * runs < 4096) chunk /= 2;
+    while (chunk > 8 && (n + chunk - 1) / chunk * runs < 2048) chunk /= 2;
     l.chunk = (uint32_t)chunk;
     l.part_ld = up(a->dim, 8);
     uint64_t at = 0;

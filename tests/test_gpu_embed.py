@@ -207,6 +207,22 @@ def test_many_elements():
     assert float(got.sum(dtype=torch.float64)) == dim * (4 + 3 * 65998)
 
 
+def test_many_tokens():
+    """More than a launch of the lookup takes, of few words."""
+    n = (1 << 26) + 77
+    ids = torch.arange(n, device="cuda") % 5
+    table = torch.tensor([[1.0, -2.0], [2.0, 3.0], [4.0, 0.5], [8.0, 0.0], [16.0, 1.0]], device="cuda").to(BF)
+    rows = P.ckpt_embedding(table, ids)
+    for at in (0, 1, (1 << 25) - 1, 1 << 25, (1 << 26) - 1, 1 << 26, n - 1):
+        assert torch.equal(rows[at], table[at % 5])
+    assert float(rows[:, 0].sum(dtype=torch.float64)) == float(table.double()[:, 0][ids[:5]].sum()) * (n // 5) + float(
+        table.double()[:n % 5, 0].sum())
+    got = P.ckpt_embedding_grad(rows, ids, 5, scale=2.0 ** -20, dtype=F32)
+    count = torch.bincount(ids, minlength=5).double()
+    want = table.double() * count[:, None] * 2.0 ** -20
+    within(got, want, 1024 * U32 * want.abs(), "table")  # whole numbers up to 2^24 a chunk, and at most 1024 of those
+
+
 def test_another_stream_and_a_graph():
     ids = masked(words(777, 200, "text"))
     table = torch.randn(200, 130, device="cuda").to(BF)
