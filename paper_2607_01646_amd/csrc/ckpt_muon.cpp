@@ -17,22 +17,40 @@ namespace {
 constexpr uint64_t kSingly = 384; // up to this short side: step by step, which is fewer launches and twice as exact
 constexpr uint64_t kDefaultPiece = 4ull << 30; // the matrices of a layer of 4096 x 11008, in one group
 
+// The largest that a singular value becomes, that a step multiplies one by, and that two steps do (NaN and infinity: as
+// infinity).  They begin in [0, 1]; the operands' scale has room for 16.
+struct Iterates {
+    double value = 0, factor = 0, both = 0;
+    explicit Iterates(const ckpt_newton_schulz& ns)
+    {
+        constexpr int kGrid = 128;
+        double x[kGrid], before[kGrid] = {};
+        for (int k = 0; k < kGrid; ++k) x[k] = (k + 1.0) / kGrid;
+        factor = std::fabs(ns.a); // of values near 0
+        both = ns.steps > 1 ? ns.a * ns.a : 0;
+        bool fine = std::isfinite(ns.a) && std::isfinite(ns.b) && std::isfinite(ns.c);
+        for (uint32_t i = 0; i < ns.steps && fine; ++i) {
+            for (int k = 0; k < kGrid; ++k) { // side by side: this is part of every call
+                const double s = x[k] * x[k], by = ns.a + s * (ns.b + s * ns.c);
+                x[k] *= by;
+                value = std::max(value, std::fabs(x[k]));
+                factor = std::max(factor, std::fabs(by));
+                both = std::max(both, std::fabs(by * before[k]));
+                before[k] = by;
+            }
+            fine = value <= 1e3;
+        }
+        if (!fine) value = factor = both = INFINITY;
+    }
+};
+
 ckpt_status check_ns(const ckpt_newton_schulz& ns)
 {
     if (ns.steps < 1 || ns.steps > 64) return fail_free(CKPT_EINVAL, "%u steps: 1 to 64", ns.steps);
     if (ns.reserved) return fail_free(CKPT_EINVAL, "reserved is not 0");
     if (!(ns.eps >= 1e-30 && ns.eps <= 1)) return fail_free(CKPT_EINVAL, "eps %g is not in [1e-30, 1]", ns.eps);
-    // Singular values begin in [0, 1].  The operands' scale has room for 16, and the polynomial's coefficient of a value for 15.
-    constexpr int kGrid = 512;
-    bool fine = std::isfinite(ns.a) && std::isfinite(ns.b) && std::isfinite(ns.c);
-    for (int k = 0; fine && k <= kGrid; ++k) {
-        double x = (double)k / kGrid;
-        for (uint32_t i = 0; fine && i < ns.steps; ++i) {
-            const double s = x * x, factor = ns.a + s * (ns.b + s * ns.c);
-            x *= factor;
-            fine = std::fabs(x) <= 2 && std::fabs(factor) <= 8;
-        }
-    }
+    const Iterates it(ns);
+    const bool fine = it.value <= 2 && it.factor <= 8;
     if (!fine)
         return fail_free(CKPT_EINVAL, "the polynomial %g x + %g x^3 + %g x^5 leaves [-2, 2], or multiplies a value by more than 8",
                          ns.a, ns.b, ns.c);
@@ -44,19 +62,7 @@ ckpt_status check_ns(const ckpt_newton_schulz& ns)
 // s^2 l, and of those of the short side 11 instead of 5, in units of s^3.  It is as exact as step by step (a Gram matrix of
 // X itself sets every other step right; with three from one, what is rounded off beside the large singular values grows in
 // the small ones' place until it is all there is).  The product of both factors has to fit the operands' scale.
-bool fits_twos(const ckpt_newton_schulz& ns)
-{
-    constexpr int kGrid = 512;
-    for (int k = 0; k <= kGrid; ++k) {
-        double x = (double)k / kGrid, before = 0;
-        for (uint32_t i = 0; i < ns.steps; ++i) {
-            const double s = x * x, factor = ns.a + s * (ns.b + s * ns.c);
-            if (std::fabs(before * factor) > 14) return false;
-            x *= before = factor;
-        }
-    }
-    return true;
-}
+bool fits_twos(const ckpt_newton_schulz& ns) { return Iterates(ns).both <= 14; }
 
 // A matrix of the call, whichever entry point it is of.
 struct Job {

@@ -608,7 +608,7 @@ __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply
 //
 // Up to 64 x 256: a workgroup makes all of a matrix's step, X, A and B in LDS, in the time that the launches' latencies
 // would take many times over (4 matrices of 64 x 64 to 256: 33 us, 112 by the kernels above).  The same sums of the same
-// operands, but step by step.  X is padded with zeros to 64 rows and a multiple of 32 columns; rows lie 16 bytes further
+// operands, but step by step.  X is padded with zeros to 64 rows and 256 columns; rows lie 16 bytes further
 // apart than they are long, which spreads the 16 rows that a quarter of a wave reads over the banks.
 constexpr int kTinyThreads = 512, kTinyX = kTinyLong + 8, kTinyA = kTinyShort + 8;
 
@@ -647,7 +647,7 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
     __shared__ __attribute__((aligned(16))) uint16_t s_x[2 * kXPlane], s_a[2 * kAPlane], s_b[2 * kAPlane];
     __shared__ double s_wave[kTinyThreads / 64];
     const MuonMatrix& m = a.m[blockIdx.x];
-    const uint32_t rows = m.rows, cols = m.cols, l32 = (max(rows, cols) + 31) & ~31u;
+    const uint32_t rows = m.rows, cols = m.cols, l64 = up64(max(rows, cols));
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool wide = rows <= cols;
 
@@ -721,12 +721,20 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
     auto square = [&](const uint16_t* p, uint32_t ld, uint32_t plane, uint32_t k, const uint16_t* c, uint16_t* out) {
         const uint32_t q0 = 16 * (wave >> 1), p0 = 32 * (wave & 1), q = q0 + (lane & 15), p1 = p0 + 4 * (lane >> 4);
         f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-        for (uint32_t k0 = 0; k0 < k; k0 += 32) {
-            const f16x8 y[2] = {row_part(p, ld, q0, k0), row_part(p + plane, ld, q0, k0)};
+        for (uint32_t k0 = 0; k0 < k; k0 += 64) {
+            f16x8 y[2][2], x[2][2][2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const f16x8 x[2] = {row_part(p, ld, p0 + 16 * t, k0), row_part(p + plane, ld, p0 + 16 * t, k0)};
-                multiply2(acc[t], x, y);
+            for (uint32_t h = 0; h < 2; ++h)
+#pragma unroll
+                for (uint32_t z = 0; z < 2; ++z) {
+                    y[h][z] = row_part(p + z * plane, ld, q0, k0 + 32 * h);
+                    x[h][0][z] = row_part(p + z * plane, ld, p0, k0 + 32 * h);
+                    x[h][1][z] = row_part(p + z * plane, ld, p0 + 16, k0 + 32 * h);
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                multiply2(acc[0], x[h][0], y[h]);
+                multiply2(acc[1], x[h][1], y[h]);
             }
         }
 #pragma unroll
@@ -774,14 +782,16 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
             }
         }
     };
+    const bool mine = 32 * wave < l64; // the wave's columns are not all zeros
     for (uint32_t step = 0;; ++step) {
-        square(s_x, kTinyX, kXPlane, l32, nullptr, s_a);
+        square(s_x, kTinyX, kXPlane, l64, nullptr, s_a);
         square(s_a, kTinyA, kAPlane, kTinyShort, s_a, s_b);
         if (step + 1 == n.steps) break;
-        apply(std::false_type());
+        if (mine) apply(std::false_type());
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
+            if (!mine) break;
             uint2 hi, lo;
             split2(acc[t] * kDown, hi, lo);
             uint16_t* to = s_x + (i0(t) + (lane & 15)) * kTinyX + j0(t) + 4 * (lane >> 4);
@@ -790,6 +800,7 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
         }
         __syncthreads();
     }
+    if (!mine) return;
     // The last as the matrix lies, in runs of 4 values of its rows.
     uint32_t r[kTiles], c[kTiles];
     const float* w[kTiles];
