@@ -3,9 +3,9 @@
  * update, and of the orthogonalisation alone.
  *
  * It stands beside ckpt_adamw (ckpt_ops.h): matrices inside a model take this
- * step, its tables and vectors AdamW's.  A matrix's state is two fragments
- * fewer bytes than AdamW's: the fp32 master copy and one moment.  Like every
- * operator, the result depends on the inputs alone (no atomics, a fixed order
+ * step, its tables and vectors AdamW's.  A matrix has one fragment less to
+ * capture than with AdamW: parameter, fp32 master copy, one moment.  Like every
+ * operator's, the result depends on the inputs alone (no atomics, a fixed order
  * of every sum), matrix by matrix: the others of a call do not change it.
  *
  * Conventions are those of ckpt_ops.h.

@@ -4,7 +4,7 @@
 //   A = X X^T,  B = ca I + cb A + cc A A,  X <- B X
 // with X laid out so that its rows are the shorter side; two steps are made
 // from one A where that is worth it (ckpt_muon.cpp).  Large matrices are bound
-// by the matrix cores (7 of 4096 x 4096 to 11008: 36 ms, 1.15 PFLOP/s on the
+// by the matrix cores (7 of 4096 x 4096 to 11008: 36 ms, 1.1 PFLOP/s on the
 // planes over all launches), small ones by the launches' latencies.
 //
 // The operands are two planes of fp16, 22 bits, and three products of planes
