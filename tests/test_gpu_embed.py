@@ -43,7 +43,7 @@ def unit(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("n, dim, vocab", [(0, 64, 10), (1, 1, 1), (1, 4096, 300), (3, 7, 5), (64, 64, 256), (65, 513, 100),
+@pytest.mark.parametrize("n, dim, vocab", [(0, 64, 10), (1, 1, 1), (10, 2, 5), (10, 3, 5), (1, 4096, 300), (3, 7, 5), (64, 64, 256), (65, 513, 100),
                                            (300, 1000, 77), (5, 8191, 9), (9000, 320, 500), (2000, 2049, 1000)])
 def test_lookup(n, dim, vocab, dtype):
     table = torch.randn(vocab, dim, generator=gen(n), device="cuda").to(dtype)
@@ -105,7 +105,7 @@ def reference(d, ids, vocab, scale, old=None):
 
 @pytest.mark.parametrize("rows, table", [(BF, BF), (F32, F32), (BF, F32), (F32, BF)])
 @pytest.mark.parametrize("kind", ["even", "text", "one"])
-@pytest.mark.parametrize("n, dim, vocab", [(1, 1, 1), (1, 4096, 300), (3, 7, 5), (63, 64, 33), (64, 64, 256), (65, 513, 100),
+@pytest.mark.parametrize("n, dim, vocab", [(1, 1, 1), (10, 2, 5), (200, 3, 5), (1, 4096, 300), (3, 7, 5), (63, 64, 33), (64, 64, 256), (65, 513, 100),
                                            (128, 1030, 40), (129, 5000, 7), (1000, 1000, 77), (3000, 65, 1001),
                                            (5000, 320, 40000), (20000, 9, 3), (70000, 130, 2500)])
 def test_gradient(n, dim, vocab, kind, rows, table):

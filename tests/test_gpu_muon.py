@@ -237,6 +237,43 @@ def test_another_stream_and_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(y, want)), k
 
 
+def test_rows_of_4_million():
+    """The longest rows there may be: sums of 2^22 squares, and more tiles of the first launches than 2^16."""
+    x = matrix((66, 1 << 22))
+    for t in (x, x.t().contiguous()):
+        y, = P.ckpt_orthogonalize([t])
+        got = (y if t is x else y.t()).double()
+        g = x.double() @ x.double().t()
+        # X = F U with F of U's Gram matrix alone: 66 x 66 in 64 bits
+        n = float(g.diagonal().sum().sqrt()) + 1e-7
+        f, a = torch.eye(66, dtype=torch.float64, device="cuda") / n, g / n ** 2
+        for _ in range(5):
+            b = 3.4445 * torch.eye(66, dtype=torch.float64, device="cuda") - 4.7750 * a + 2.0315 * a @ a
+            f, a = b @ f, b @ a @ b
+        want = f @ x.double()
+        # 5 steps of 3 roundings of 2^-22 and sums of 2^-23 a square, grown by the steps' factors (at most 3.4 a step, 2 in all here)
+        assert float((got - want).norm()) < 2e-5 * float(want.norm())
+
+
+def test_calls_on_two_streams_at_once():
+    shapes = [(300, 500), (64, 64), (1, 900), (129, 130)]
+    lists, flat = state(shapes, BF, F32)
+    twin, same = state(shapes, BF, F32)
+    x = [matrix((600, 700)), matrix((40, 200))]
+    want = P.ckpt_orthogonalize(x)
+    for _ in range(3):
+        P.ckpt_muon(*twin, lr=1e-2)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        P.ckpt_muon(*lists, lr=1e-2, stream=streams[0])
+        got.append(P.ckpt_orthogonalize(x, stream=streams[1].cuda_stream))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(flat, same))
+    assert all(torch.equal(a, b) for y in got for a, b in zip(y, want))
+
+
 def test_refusals():
     lists, flat = state([(10, 20), (30, 5)], BF, F32)
     before = [t.clone() for t in flat]
