@@ -14,7 +14,7 @@
 namespace ckpt {
 namespace {
 
-constexpr uint64_t kSingly = 384; // up to this short side: step by step, which is fewer launches and twice as exact
+constexpr uint64_t kSingly = kMuonAll; // up to this short side: step by step, which is fewer launches and twice as exact
 constexpr uint64_t kDefaultPiece = 4ull << 30; // the matrices of a layer of 4096 x 11008, in one group
 
 // The largest that a singular value becomes, that a step multiplies one by, and that two steps do (NaN and infinity: as
@@ -199,6 +199,7 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
     const bool fits = fits_twos(ns);
     return grouped(jobs, ns.piece_bytes, &need, [&](size_t first, size_t last) {
         const bool twos = fits && jobs[first].s > kSingly;
+        a.all = jobs[first].s <= kMuonAll;
         a.count = (uint32_t)(last - first);
         for (size_t k = first; k < last; ++k) {
             a.m[k - first] = jobs[k].m;
@@ -213,6 +214,7 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
             if (err != hipSuccess) return;
             TriArgs t = {};
             t.count = a.count;
+            t.all = a.all;
             t.ca = (float)ns.a;
             t.cb = (float)ns.b;
             t.cc = poly ? (float)ns.c : 1.0f;

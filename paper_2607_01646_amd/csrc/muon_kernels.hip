@@ -635,6 +635,7 @@ __device__ inline f16x8 column_part(const uint16_t* m, uint32_t ld, uint32_t c0,
 // out[q][p]: q = lane % 16, p = 4 (lane / 16) + 0..3.
 __device__ inline void multiply2(f32x4& acc, const f16x8 (&p)[2], const f16x8 (&q)[2])
 {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[1], q[1], acc, 0, 0, 0);
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], q[1], acc, 0, 0, 0);
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[1], q[0], acc, 0, 0, 0);
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], q[0], acc, 0, 0, 0);
@@ -851,10 +852,10 @@ template <bool PA, bool QA>
 using Large = Shape<2, 2, PA, QA, 256, 256, 4, 2, 32, 2, true>;
 template <bool PA, bool QA>
 using Wide = Shape<2, 2, PA, QA, 128, 256, 2, 4, 32, 3, true, true>;
-template <bool PA, bool QA>
-using Middle = Shape<2, 2, PA, QA, 128, 128, 2, 4, 64, 2, true, true>;
-template <bool PA, bool QA>
-using Small = Shape<2, 2, PA, QA, 64, 64, 2, 2, 64, 3, true, true>;
+template <bool PA, bool QA, bool ALL>
+using Middle = Shape<2, 2, PA, QA, 128, 128, 2, 4, 64, 2, true, true, ALL>;
+template <bool PA, bool QA, bool ALL>
+using Small = Shape<2, 2, PA, QA, 64, 64, 2, 2, 64, 3, true, true, ALL>;
 
 uint64_t blocks(uint64_t x, uint32_t side) { return (x + side - 1) / side; }
 
@@ -878,7 +879,7 @@ Size size_of(const A& a, bool parts, T tiles, K steps)
     Size best = kSmall;
     double least = 1e30;
     for (int z = kSmall; z <= kLarge; ++z) {
-        if (z == kLarge && parts) continue;
+        if ((z == kLarge && parts) || (z > kMiddle && a.all)) continue;
         const auto& c = kTile[z];
         uint64_t all = 0, work = 0;
         for (uint32_t i = 0; i < a.count; ++i) {
@@ -921,14 +922,17 @@ hipError_t apply(MuonArgs& a, hipStream_t stream)
     const Size size = size_of(a, parts, tiles, steps);
     a.shares = steps(a.m[0]) != steps(a.m[a.count - 1]);
     const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const MuonMatrix& m) { return tiles(m, size); });
-    using LT = std::conditional_t<kNext, Large<true, false>, Large<false, true>>;
-    using WT = std::conditional_t<kNext, Wide<true, false>, Wide<false, true>>;
-    using MT = std::conditional_t<kNext, Middle<true, false>, Middle<false, true>>;
-    using ST = std::conditional_t<kNext, Small<true, false>, Small<false, true>>;
-    return size == kLarge    ? launch_tiles(apply_kernel<Large<true, false>, LT, End>, &a, all, LT::kThreads, stream)
-           : size == kWide   ? launch_tiles(apply_kernel<Wide<true, false>, WT, End>, &a, all, WT::kThreads, stream)
-           : size == kMiddle ? launch_tiles(apply_kernel<Middle<true, false>, MT, End>, &a, all, MT::kThreads, stream)
-                             : launch_tiles(apply_kernel<Small<true, false>, ST, End>, &a, all, ST::kThreads, stream);
+    const auto launch = [&](auto wide, auto turned) { // the shape of wide matrices, and of tall ones' last X
+        using W = decltype(wide);
+        using T = std::conditional_t<kNext, W, decltype(turned)>;
+        return launch_tiles(apply_kernel<W, T, End>, &a, all, W::kThreads, stream);
+    };
+    return size == kLarge    ? launch(Large<true, false>(), Large<false, true>())
+           : size == kWide   ? launch(Wide<true, false>(), Wide<false, true>())
+           : size == kMiddle ? (a.all ? launch(Middle<true, false, true>(), Middle<false, true, true>())
+                                      : launch(Middle<true, false, false>(), Middle<false, true, false>()))
+           : a.all           ? launch(Small<true, false, true>(), Small<false, true, true>())
+                             : launch(Small<true, false, false>(), Small<false, true, false>());
 }
 
 } // namespace
@@ -995,10 +999,15 @@ hipError_t launch_muon_tri(TriArgs& a, hipStream_t stream)
     const Size size = size_of(a, parts, tiles, steps);
     a.shares = steps(a.m[0]) != steps(a.m[a.count - 1]);
     const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const TriMatrix& m) { return tiles(m, size); });
-    return size == kLarge    ? launch_tiles(tri_kernel<Large<false, false>>, &a, all, Large<false, false>::kThreads, stream)
-           : size == kWide   ? launch_tiles(tri_kernel<Wide<false, false>>, &a, all, Wide<false, false>::kThreads, stream)
-           : size == kMiddle ? launch_tiles(tri_kernel<Middle<false, false>>, &a, all, Middle<false, false>::kThreads, stream)
-                             : launch_tiles(tri_kernel<Small<false, false>>, &a, all, Small<false, false>::kThreads, stream);
+    const auto launch = [&](auto shape) {
+        using S = decltype(shape);
+        return launch_tiles(tri_kernel<S>, &a, all, S::kThreads, stream);
+    };
+    return size == kLarge    ? launch(Large<false, false>())
+           : size == kWide   ? launch(Wide<false, false>())
+           : size == kMiddle ? (a.all ? launch(Middle<false, false, true>()) : launch(Middle<false, false, false>()))
+           : a.all           ? launch(Small<false, false, true>())
+                             : launch(Small<false, false, false>());
 }
 
 hipError_t launch_muon_apply(MuonArgs& a, bool last, hipStream_t stream)

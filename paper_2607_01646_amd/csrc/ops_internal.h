@@ -209,7 +209,11 @@ struct MuonArgs {
     double eps;
     const float* grad_scale;
     bool nesterov, in_f32, out_f32, shares;
+    bool all; // short sides up to kMuonAll
 };
+// Up to this short side the fourth product of planes is made, too: few terms do not average what it leaves out (2^-22 of a
+// square), and cc A A has three times the size of B, in which it is one of two that nearly cancel.
+constexpr uint32_t kMuonAll = 384;
 // Values of k whose products are added up together before they are added to the sum (0: all): of X X^T, which the norms of
 // rows are, and where there are few, whose rounding fp32 would not hide.  A matrix's own sides decide.
 inline
@@ -218,7 +222,7 @@ inline
 #endif
     uint32_t muon_chunk(uint32_t k, bool gram)
 {
-    return k <= 384 ? 128 : !gram ? 0 : k <= 1024 ? 256 : 512;
+    return k <= 384 ? 128 : k < 1024 ? 256 : gram ? 512 : 0;
 }
 // Symmetric products out = ca I + cb c + cc p q, p q^T of rows of k values; no c: cc p q alone.
 struct TriMatrix {
@@ -231,6 +235,7 @@ struct TriArgs {
     uint32_t count;
     float ca, cb, cc;
     bool shares;
+    bool all;
 };
 // Matrices of at most these sides: all of the step in one launch, which uses no workspace.
 constexpr uint32_t kTinyShort = 64, kTinyLong = 256;

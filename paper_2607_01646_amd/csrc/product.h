@@ -162,17 +162,17 @@ __device__ inline uint2 tile_of(uint32_t block, uint32_t np, uint32_t nq)
 // either sign (2^-23 within 2^-8 of fp32's largest value).
 //
 // 2 and 2 (HALF): planes of fp16, hi = x and lo = x - hi rounded to nearest, 22 bits together; hi hi, hi lo and lo hi are
-// made, and lo lo, 2^-22 of the value, is left out.
+// made, and lo lo, 2^-22 of the value, is left out unless ALL.
 //
 // PARTS: the sums of every `chunk` values of k are added up in registers of their own.  A sum that grows is rounded by more
 // and more (of squares, 8192 values of k: 9.5e-7 of it in one go), with two planes 3 times for every 16 values.
 template <int ZP_, int ZQ_, bool PA_, bool QA_, int BP_, int BQ_, int NWP_, int NWQ_, int BK_, int BUFS_, bool HALF_ = false,
-          bool PARTS_ = false>
+          bool PARTS_ = false, bool ALL_ = false>
 struct Shape {
     static constexpr int ZP = ZP_, ZQ = ZQ_, BP = BP_, BQ = BQ_, NWP = NWP_, NWQ = NWQ_, BK = BK_, BUFS = BUFS_;
     static constexpr bool PA = PA_, QA = QA_, HALF = HALF_, PARTS = PARTS_;
     // Products of planes whose indexes sum to more than this are left out.
-    static constexpr int kMostSum = ZP == 3 && ZQ == 3 ? 2 : HALF && ZP == 2 && ZQ == 2 ? 1 : ZP + ZQ - 2;
+    static constexpr int kMostSum = ZP == 3 && ZQ == 3 ? 2 : HALF && !ALL_ && ZP == 2 && ZQ == 2 ? 1 : ZP + ZQ - 2;
     static constexpr int kThreads = NWP * NWQ * 64;
     static constexpr int kBuffer = (ZP * BP + ZQ * BQ) * BK; // elements
     static_assert(BUFS >= 2 && BUFS <= 4, "");
