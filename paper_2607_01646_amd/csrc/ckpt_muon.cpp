@@ -57,6 +57,10 @@ ckpt_status check_ns(const ckpt_newton_schulz& ns)
     return CKPT_OK;
 }
 
+// Whether all steps may be made from one Gram matrix in 64 bits: what its roundings leave in the place of a singular value
+// of 0 grows by the square of a step's factor.
+bool fits_thin(const ckpt_newton_schulz& ns) { return std::pow(Iterates(ns).factor, 2.0 * (ns.steps - 1)) <= 1e7; }
+
 // Whether two steps are made from one Gram matrix: X's next is B A B (all are polynomials of A), and X is multiplied once,
 // by the product of both factors.  Of the products with the long side that leaves 9 for 5 steps instead of 15, in units of
 // s^2 l, and of those of the short side 11 instead of 5, in units of s^3.  It is as exact as step by step (a Gram matrix of
@@ -68,6 +72,7 @@ bool fits_twos(const ckpt_newton_schulz& ns) { return Iterates(ns).both <= 14; }
 struct Job {
     MuonMatrix m;
     uint64_t s, l;
+    bool thin;
     uint64_t x, y, a, b, c, part; // offsets in the workspace
 };
 
@@ -76,34 +81,38 @@ bool lay_out(Job& j, uint64_t rows, uint64_t cols, uint64_t& at)
 {
     j.s = std::min(rows, cols);
     j.l = std::max(rows, cols);
-    const bool vector = j.s == 1; // no products
-    const uint64_t x = vector ? 0 : up(4 * j.s * up(j.l, 64), 256), a = vector ? 0 : up(4 * j.s * up(j.s, 64), 256); // at most 2^46 each
+    const uint64_t x = j.thin ? 8 * kThin * kThin : up(4 * j.s * up(j.l, 64), 256); // at most 2^46
+    const uint64_t y = j.thin ? 0 : x, a = j.thin ? 0 : up(4 * j.s * up(j.s, 64), 256);
     const uint64_t tiles = ((rows + kMuonRows - 1) / kMuonRows) * ((cols + kMuonCols - 1) / kMuonCols);
+    const uint64_t parts = j.thin ? std::min<uint64_t>((j.l + 255) / 256, kThinParts) : tiles;
     j.x = at;
     j.y = j.x + x;
-    j.a = j.y + x;
+    j.a = j.y + y;
     j.b = j.a + a;
     j.c = j.b + a;
     j.part = j.c + a;
-    at = j.part + up(8 * tiles, 256);
+    at = j.part + up(8 * parts * (j.thin ? kThin * kThin : 1), 256);
     j.m.rows = (uint32_t)rows;
     j.m.cols = (uint32_t)cols;
-    j.m.part_n = (uint32_t)tiles;
+    j.m.part_n = (uint32_t)parts;
     return tiles <= (1u << 23);
 }
 
 // The matrices of a call by the way they go, which their own sides decide: a matrix's result does not depend on others.
 struct Jobs {
-    std::vector<Job> vectors; // one row or column
-    std::vector<Job> tiny;    // one launch, no workspace
+    std::vector<Job> thin;   // short sides up to 16
+    std::vector<Job> tiny;   // one launch, no workspace
     std::vector<Job> others;
 };
-Jobs sorted(const std::vector<Job>& jobs)
+Jobs sorted(const std::vector<Job>& jobs, const ckpt_newton_schulz& ns)
 {
     Jobs to;
+    const bool thin = fits_thin(ns);
     for (const Job& j : jobs) {
         const uint32_t s = std::min(j.m.rows, j.m.cols), l = std::max(j.m.rows, j.m.cols);
-        (s == 1 ? to.vectors : s <= kTinyShort && l <= kTinyLong ? to.tiny : to.others).push_back(j);
+        std::vector<Job>& list = s <= kThin && thin ? to.thin : s <= kTinyShort && l <= kTinyLong ? to.tiny : to.others;
+        list.push_back(j);
+        list.back().thin = &list == &to.thin;
     }
     std::stable_partition(to.others.begin(), to.others.end(),
                           [](const Job& j) { return std::min(j.m.rows, j.m.cols) > kSingly; });
@@ -142,10 +151,10 @@ ckpt_status nothing(size_t, size_t) { return CKPT_OK; }
 // The bytes that all of a call needs: its groups run one behind the other.
 ckpt_status needed(Jobs& jobs, uint64_t piece_bytes, uint64_t* bytes)
 {
-    uint64_t vectors = 0;
-    if (ckpt_status st = grouped(jobs.vectors, piece_bytes, &vectors, nothing)) return st;
+    uint64_t thin = 0;
+    if (ckpt_status st = grouped(jobs.thin, piece_bytes, &thin, nothing)) return st;
     if (ckpt_status st = grouped(jobs.others, piece_bytes, bytes, nothing)) return st;
-    *bytes = std::max(*bytes, vectors);
+    *bytes = std::max(*bytes, thin);
     return CKPT_OK;
 }
 
@@ -170,7 +179,7 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
                     uint64_t workspace_bytes, hipStream_t s)
 {
     uint64_t need = 0;
-    Jobs sides = sorted(all);
+    Jobs sides = sorted(all, ns);
     std::vector<Job>& jobs = sides.others;
     if (ckpt_status st = needed(sides, ns.piece_bytes, &need)) return st;
     if (need > workspace_bytes)
@@ -178,7 +187,7 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
                          (unsigned long long)need);
     a.eps = ns.eps;
     uint8_t* w = (uint8_t*)workspace;
-    const MuonPolynomial polynomial = {(float)ns.a, (float)ns.b, (float)ns.c, ns.steps};
+    const MuonPolynomial polynomial = {ns.a, ns.b, ns.c, ns.steps};
     const auto done = [](hipError_t err) {
         return err == hipSuccess ? CKPT_OK : fail_free(CKPT_EHIP, "orthogonalisation: %s", hipGetErrorString(err));
     };
@@ -187,15 +196,16 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
         for (uint32_t k = 0; k < a.count; ++k) a.m[k] = sides.tiny[i + k].m;
         if (ckpt_status st = done(launch_muon_tiny(a, polynomial, s))) return st;
     }
-    const ckpt_status vectors = grouped(sides.vectors, ns.piece_bytes, &need, [&](size_t first, size_t last) {
+    const ckpt_status thin = grouped(sides.thin, ns.piece_bytes, &need, [&](size_t first, size_t last) {
         a.count = (uint32_t)(last - first);
         for (size_t k = first; k < last; ++k) {
-            a.m[k - first] = sides.vectors[k].m;
-            a.m[k - first].part = (double*)(w + sides.vectors[k].part);
+            a.m[k - first] = sides.thin[k].m;
+            a.m[k - first].part = (double*)(w + sides.thin[k].part);
+            a.m[k - first].x = (uint16_t*)(w + sides.thin[k].x);
         }
-        return done(launch_muon_vectors(a, polynomial, s));
+        return done(launch_muon_thin(a, polynomial, s));
     });
-    if (vectors) return vectors;
+    if (thin) return thin;
     const bool fits = fits_twos(ns);
     return grouped(jobs, ns.piece_bytes, &need, [&](size_t first, size_t last) {
         const bool twos = fits && jobs[first].s > kSingly;
@@ -333,7 +343,7 @@ extern "C" ckpt_status ckpt_orthogonalize_workspace(const ckpt_matrix* m, uint32
         std::vector<Job> jobs;
         if (!bytes) return fail_free(CKPT_EINVAL, "null argument");
         if (ckpt_status st = orthogonalize_jobs(m, n, ns, jobs)) return st;
-        Jobs sides = sorted(jobs);
+        Jobs sides = sorted(jobs, *ns);
         return needed(sides, ns->piece_bytes, bytes);
     });
 }
@@ -387,7 +397,7 @@ extern "C" ckpt_status ckpt_muon_workspace(const ckpt_muon_matrix* m, uint32_t n
         std::vector<Job> jobs;
         if (!bytes) return fail_free(CKPT_EINVAL, "null argument");
         if (ckpt_status st = muon_jobs(m, n, args, jobs)) return st;
-        Jobs sides = sorted(jobs);
+        Jobs sides = sorted(jobs, args->ns);
         return needed(sides, args->ns.piece_bytes, bytes);
     });
 }

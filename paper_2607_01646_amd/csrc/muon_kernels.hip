@@ -191,43 +191,6 @@ __global__ __launch_bounds__(1024) void norm_kernel(const MuonArgs a)
     if (threadIdx.x == 0) m.part[0] = sum; // every part was read before the workgroup met
 }
 
-// Matrices of one row or one column: X stays a multiple of the update, and A is a number.  All of it behind first_kernel, in
-// the same tiles.
-template <class G>
-__global__ __launch_bounds__(kThreads) void vector_kernel(const MuonArgs a, const MuonPolynomial n)
-{
-    __shared__ double s_wave[kThreads / 64];
-    const uint32_t f = matrix_of(a, blockIdx.x), t = blockIdx.x - a.m[f].first;
-    const MuonMatrix& m = a.m[f];
-    const uint32_t rows = m.rows, cols = m.cols, nc = (cols + kMuonCols - 1) / kMuonCols;
-    double sum = 0;
-    const uint32_t parts = m.part_n <= kMuonParts ? m.part_n : 1;
-    for (uint32_t k = threadIdx.x; k < parts; k += kThreads) sum += m.part[k];
-    const double norm = sqrt(block_sum(sum, s_wave));
-    double x = norm / (norm + a.eps), factor = 1 / (norm + a.eps);
-    for (uint32_t step = 0; step < n.steps; ++step) {
-        const double s = x * x, by = n.ca + s * (n.cb + s * n.cc);
-        x *= by;
-        factor *= by;
-    }
-    const float cs = a.grad_scale ? *a.grad_scale : 1.0f;
-    const uint32_t r0 = t / nc * kMuonRows, c0 = t % nc * kMuonCols;
-    const uint32_t r = rows == 1 ? 0 : r0 + threadIdx.x, c = rows == 1 ? c0 + threadIdx.x : 0;
-    if (r >= rows || c >= cols || (rows != 1 && threadIdx.x >= kMuonRows)) return;
-    float u = load1((const G*)m.in + r * m.in_ld + c);
-    const uint64_t at = (uint64_t)r * cols + c;
-    if (m.momentum) u = update(a, m.momentum[at], cs * u);
-    float y = (float)((double)u * factor);
-    if (m.master) {
-        y = m.master[at] * a.keep - y * m.scale;
-        m.master[at] = y;
-    }
-    if (a.out_f32)
-        ((float*)m.out)[r * m.out_ld + c] = y;
-    else
-        ((uint16_t*)m.out)[r * m.out_ld + c] = bf16_of(y);
-}
-
 template <class G>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const MuonArgs a)
 {
@@ -604,6 +567,155 @@ __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply
     }
 }
 
+// ---- thin matrices ----
+//
+// Short sides up to 16: all steps are polynomials of one Gram matrix, G = U U^T, which is so small that it is kept in 64
+// bits: a launch makes it, one goes through the steps (A <- B A B, F <- B F) and the last makes X = F U.  Few terms do not
+// average the roundings of 22 bits (2 x 1033: 1.6e-6 off with planes, 5e-7 with products in fp32), and five steps from one
+// Gram matrix, which in fewer bits are not stable, are so in 64 (fits_thin in ckpt_muon.cpp).  Bound by HBM for long
+// rows, by the launches' latencies for others.
+constexpr uint32_t kThinLd = kThreads + 4; // of LDS rows: 16 bytes further apart than a power of two
+
+// The update's s values at `at` of the long side; KEEP: the momentum's new ones are stored, else they are.
+template <class G, bool KEEP>
+__device__ inline void thin_values(const MuonArgs& a, const MuonMatrix& m, bool wide, uint32_t s, uint32_t at, float (&u)[kThin])
+{
+    const float cs = a.grad_scale ? *a.grad_scale : 1.0f;
+    float old[kThin];
+    const uint64_t in_step = wide ? m.in_ld : 1, step = wide ? m.cols : 1;
+    const G* in = (const G*)m.in + (wide ? at : at * m.in_ld);
+    float* momentum = m.momentum + (wide ? at : (uint64_t)at * m.cols);
+#pragma unroll
+    for (uint32_t i = 0; i < kThin; ++i) u[i] = load1(in + min(i, s - 1) * in_step);
+    if (m.momentum) {
+#pragma unroll
+        for (uint32_t i = 0; i < kThin; ++i) old[i] = momentum[min(i, s - 1) * step];
+#pragma unroll
+        for (uint32_t i = 0; i < kThin; ++i) {
+            const float cg = cs * u[i];
+            if (KEEP) {
+                old[i] = a.beta * old[i] + a.one_beta * cg;
+                if (i < s) momentum[i * step] = old[i];
+            }
+            u[i] = update(a, old[i], cg);
+        }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kThin; ++i) u[i] = i < s ? u[i] : 0.0f;
+}
+
+// Momentum, and a workgroup's share of G: part_n shares of runs of 256 places of the long side.  A thread sums one element of
+// G over as many of a run's places as G's side, to a power of two, has elements.
+template <class G>
+__global__ __launch_bounds__(kThreads) void thin_gram_kernel(const MuonArgs a)
+{
+    __shared__ __attribute__((aligned(16))) float s_u[kThin][kThinLd];
+    const uint32_t f = matrix_of(a, blockIdx.x), t = blockIdx.x - a.m[f].first;
+    const MuonMatrix& m = a.m[f];
+    const bool wide = m.rows <= m.cols;
+    const uint32_t s = min(m.rows, m.cols), l = max(m.rows, m.cols), runs = (l + kThreads - 1) / kThreads;
+    const uint32_t log2 = s > 1 ? 32 - __clz(s - 1) : 0, pair = threadIdx.x & ((1u << 2 * log2) - 1);
+    const uint32_t i = pair >> log2, j = pair & ((1u << log2) - 1), k0 = threadIdx.x - pair, span = 1u << 2 * log2;
+    double sum = 0;
+    for (uint32_t run = t; run < runs; run += m.part_n) {
+        const uint32_t at = run * kThreads + threadIdx.x;
+        float u[kThin];
+        if (at < l) thin_values<G, true>(a, m, wide, s, at, u);
+#pragma unroll
+        for (uint32_t k = 0; k < kThin; ++k) s_u[k][threadIdx.x] = at < l ? u[k] : 0.0f;
+        __syncthreads();
+        if (s == 1) {
+            sum += (double)s_u[0][threadIdx.x] * (double)s_u[0][threadIdx.x];
+        } else if (i < s && j <= i) {
+            for (uint32_t k = k0; k < k0 + span; k += 4) {
+                const f32x4 x = *(const f32x4*)&s_u[i][k], y = *(const f32x4*)&s_u[j][k];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sum += (double)x[v] * (double)y[v];
+            }
+        }
+        __syncthreads();
+    }
+    double* s_sum = (double*)s_u;
+    s_sum[threadIdx.x] = sum;
+    __syncthreads();
+    for (uint32_t n = kThreads / 2; n >= span; n /= 2) {
+        if (threadIdx.x < n) s_sum[threadIdx.x] += s_sum[threadIdx.x + n];
+        __syncthreads();
+    }
+    // Elements behind the s-th, and above the diagonal, are not read (thin_steps_kernel).
+    if (threadIdx.x < span && i < s) m.part[(uint64_t)t * kThreads + i * kThin + j] = s_sum[threadIdx.x];
+}
+
+// All steps of a matrix by one workgroup, an element a thread: F over the norm, where X would be.
+__global__ __launch_bounds__(kThreads) void thin_steps_kernel(const MuonArgs a, const MuonPolynomial n)
+{
+    __shared__ double s_a[kThin][kThin + 1], s_b[kThin][kThin + 1], s_f[kThin][kThin + 1], s_t[kThin][kThin + 1];
+    const MuonMatrix& m = a.m[blockIdx.x];
+    const uint32_t s = min(m.rows, m.cols);
+    const uint32_t i = threadIdx.x / kThin, j = threadIdx.x % kThin;
+    double g = 0;
+    if (max(i, j) < s) {
+#pragma unroll 8
+        for (uint32_t t = 0; t < m.part_n; ++t) g += m.part[(uint64_t)t * kThreads + max(i, j) * kThin + min(i, j)];
+    }
+    s_a[i][j] = g;
+    __syncthreads();
+    double squares = 0;
+    for (uint32_t k = 0; k < s; ++k) squares += s_a[k][k];
+    __syncthreads();
+    const double norm = sqrt(squares) + a.eps;
+    double x = s_a[i][j] = g / norm / norm, f = i == j ? 1 / norm : 0;
+    s_f[i][j] = f;
+    __syncthreads();
+    const auto product = [&](const double (&p)[kThin][kThin + 1], const double (&q)[kThin][kThin + 1]) {
+        double sum = 0;
+        for (uint32_t k = 0; k < s; ++k) sum += p[i][k] * q[k][j];
+        return sum;
+    };
+    for (uint32_t step = 0; step < n.steps; ++step) {
+        s_b[i][j] = (i == j ? n.ca : 0.0) + n.cb * x + n.cc * product(s_a, s_a);
+        __syncthreads();
+        f = product(s_b, s_f);
+        s_t[i][j] = product(s_b, s_a);
+        __syncthreads();
+        s_f[i][j] = f;
+        x = s_a[i][j] = product(s_t, s_b);
+        __syncthreads();
+    }
+    ((double*)m.x)[threadIdx.x] = f;
+}
+
+template <class G>
+__global__ __launch_bounds__(kThreads) void thin_apply_kernel(const MuonArgs a)
+{
+    __shared__ double s_f[kThin][kThin];
+    const uint32_t index = matrix_of(a, blockIdx.x), t = blockIdx.x - a.m[index].first;
+    const MuonMatrix& m = a.m[index];
+    const bool wide = m.rows <= m.cols;
+    const uint32_t s = min(m.rows, m.cols), l = max(m.rows, m.cols), at = t * kThreads + threadIdx.x;
+    s_f[threadIdx.x / kThin][threadIdx.x % kThin] = ((const double*)m.x)[threadIdx.x];
+    __syncthreads();
+    if (at >= l) return;
+    float u[kThin];
+    thin_values<G, false>(a, m, wide, s, at, u);
+    for (uint32_t i = 0; i < s; ++i) {
+        double sum = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kThin; ++k) sum += s_f[i][k] * (double)u[k];
+        const uint64_t row = wide ? i : at, col = wide ? at : i;
+        float y = (float)sum;
+        if (m.master) {
+            float* w = m.master + row * m.cols + col;
+            y = *w * a.keep - y * m.scale;
+            *w = y;
+        }
+        if (a.out_f32)
+            ((float*)m.out)[row * m.out_ld + col] = y;
+        else
+            ((uint16_t*)m.out)[row * m.out_ld + col] = bf16_of(y);
+    }
+}
+
 // ---- small matrices ----
 //
 // Up to 64 x 256: a workgroup makes all of a matrix's step, X, A and B in LDS, in the time that the launches' latencies
@@ -718,6 +830,7 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
     }
     __syncthreads();
 
+    const float ca = (float)n.ca, cb = (float)n.cb, cc = (float)n.cc;
     // P P^T: two tiles a wave, of the same q.
     auto square = [&](const uint16_t* p, uint32_t ld, uint32_t plane, uint32_t k, const uint16_t* c, uint16_t* out) {
         const uint32_t q0 = 16 * (wave >> 1), p0 = 32 * (wave & 1), q = q0 + (lane & 15), p1 = p0 + 4 * (lane >> 4);
@@ -746,7 +859,7 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
                 Planes old;
                 old.load(c + at, kAPlane);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = n.cc * v[j] + n.cb * old.at(j) + (p1 + 16 * t + j == q ? n.ca * kUp : 0.0f);
+                for (int j = 0; j < 4; ++j) v[j] = cc * v[j] + cb * old.at(j) + (p1 + 16 * t + j == q ? ca * kUp : 0.0f);
             }
             uint2 hi, lo;
             split2(v, hi, lo);
@@ -963,16 +1076,17 @@ static hipError_t launch_norms(const MuonArgs& a, hipStream_t stream)
     return hipGetLastError();
 }
 
-hipError_t launch_muon_vectors(MuonArgs& a, const MuonPolynomial& n, hipStream_t stream)
+hipError_t launch_muon_thin(MuonArgs& a, const MuonPolynomial& n, hipStream_t stream)
 {
-    if (const hipError_t e = launch_muon_first(a, stream)) return e;
-    if (const hipError_t e = launch_norms(a, stream)) return e;
-    const uint64_t tiles = number(a, 1, [](const MuonMatrix& m) { return (uint64_t)m.part_n; });
-    if (a.in_f32)
-        vector_kernel<float><<<(uint32_t)tiles, kThreads, 0, stream>>>(a, n);
-    else
-        vector_kernel<uint16_t><<<(uint32_t)tiles, kThreads, 0, stream>>>(a, n);
-    return hipGetLastError();
+    const uint64_t parts = number(a, 1, [](const MuonMatrix& m) { return (uint64_t)m.part_n; });
+    hipError_t e = a.in_f32 ? launch_tiles(thin_gram_kernel<float>, &a, parts, kThreads, stream)
+                            : launch_tiles(thin_gram_kernel<uint16_t>, &a, parts, kThreads, stream);
+    if (e != hipSuccess) return e;
+    thin_steps_kernel<<<a.count, kThreads, 0, stream>>>(a, n);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const uint64_t runs = number(a, 1, [](const MuonMatrix& m) { return blocks(std::max(m.rows, m.cols), kThreads); });
+    return a.in_f32 ? launch_tiles(thin_apply_kernel<float>, &a, runs, kThreads, stream)
+                    : launch_tiles(thin_apply_kernel<uint16_t>, &a, runs, kThreads, stream);
 }
 
 hipError_t launch_muon_pack(MuonArgs& a, hipStream_t stream)

@@ -213,7 +213,7 @@ struct MuonArgs {
 };
 // Up to this short side the fourth product of planes is made, too: few terms do not average what it leaves out (2^-22 of a
 // square), and cc A A has three times the size of B, in which it is one of two that nearly cancel.
-constexpr uint32_t kMuonAll = 384;
+constexpr uint32_t kMuonAll = 448;
 // Values of k whose products are added up together before they are added to the sum (0: all): of X X^T, which the norms of
 // rows are, and where there are few, whose rounding fp32 would not hide.  A matrix's own sides decide.
 inline
@@ -222,7 +222,7 @@ inline
 #endif
     uint32_t muon_chunk(uint32_t k, bool gram)
 {
-    return k <= 384 ? 128 : k < 1024 ? 256 : gram ? 512 : 0;
+    return k <= 640 ? 128 : k < 1024 ? 256 : gram ? 512 : 0;
 }
 // Symmetric products out = ca I + cb c + cc p q, p q^T of rows of k values; no c: cc p q alone.
 struct TriMatrix {
@@ -240,11 +240,12 @@ struct TriArgs {
 // Matrices of at most these sides: all of the step in one launch, which uses no workspace.
 constexpr uint32_t kTinyShort = 64, kTinyLong = 256;
 struct MuonPolynomial {
-    float ca, cb, cc;
+    double ca, cb, cc;
     uint32_t steps;
 };
-// Matrices of one row or column: `part` is all that they need of the workspace.
-hipError_t launch_muon_vectors(MuonArgs& a, const MuonPolynomial& n, hipStream_t stream);
+// Short sides up to kThin: `part` holds part_n shares of 256 sums (at most kThinParts), x 256 doubles.
+constexpr uint32_t kThin = 16, kThinParts = 512;
+hipError_t launch_muon_thin(MuonArgs& a, const MuonPolynomial& n, hipStream_t stream);
 hipError_t launch_muon_tiny(const MuonArgs& a, const MuonPolynomial& n, hipStream_t stream);
 // Elements of the tiles of the launches that are not products.
 constexpr uint32_t kMuonRows = 16, kMuonCols = 256, kMuonTurn = 64, kMuonParts = 1024;

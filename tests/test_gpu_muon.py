@@ -14,7 +14,7 @@ if torch.cuda.is_available():
     import paper_2607_01646_amd as P
 
 BF, F32 = torch.bfloat16, torch.float32
-SHAPES = [(1, 1), (1, 7), (7, 1), (1, 5000), (3000, 1), (2, 3), (31, 33), (63, 65), (64, 64), (65, 64), (64, 256), (130, 70), (127, 513),
+SHAPES = [(1, 1), (1, 7), (7, 1), (1, 5000), (3000, 1), (2, 1033), (16, 16), (5000, 16), (15, 257), (200000, 3), (2, 3), (31, 33), (63, 65), (64, 64), (65, 64), (64, 256), (130, 70), (127, 513),
           (300, 1000), (1000, 300), (512, 512), (257, 2049)]
 
 
@@ -57,6 +57,30 @@ def test_one_element_beside_zeros():
     check_orthogonal(y, x)
     y[17, 131] = 0
     assert not y.any()
+
+
+def test_thin_matrices_are_as_exact_as_64_bits_let_them():
+    """Short sides up to 16 are rounded once, at the end.  What 64 bits leave grows by a step's factor, 3.45, twice for every
+    step but one: 16 * 2^-53 * 3.45^8, 4e-11."""
+    for shape in ((1, 300), (3, 5), (16, 700), (900, 11)):
+        for few in (False, True):
+            x = matrix(shape, few=few)
+            y, = P.ckpt_orthogonalize([x])
+            want = orthogonal(x)
+            assert bool(((y.double() - want).abs() <= 2 * U32 * want.abs() + 1e-9).all()), shape
+    # with so many steps that the Gram matrix of U would not do
+    x = matrix((5, 400))
+    y, = P.ckpt_orthogonalize([x], steps=64, coefficients=(1.5, -0.5, 0.0))
+    check_orthogonal(y, x, steps=64, coefficients=(1.5, -0.5, 0.0))
+
+
+def test_thin_zeros_and_what_is_no_number():
+    good, zero = matrix((7, 300)), torch.zeros(300, 9, device="cuda")
+    bad = [matrix((4, 600)), matrix((600, 4)), matrix((1, 5))]
+    bad[0][2, 599], bad[1][0, 0], bad[2][0, 4] = math.nan, math.inf, -math.inf
+    out = P.ckpt_orthogonalize([bad[0], good, zero, bad[1], bad[2]])
+    assert all(bool(out[k].isnan().all()) for k in (0, 3, 4)) and not out[2].any()
+    assert torch.equal(out[1], P.ckpt_orthogonalize([good])[0])
 
 
 def test_zeros_and_what_is_no_number():

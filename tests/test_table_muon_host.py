@@ -136,8 +136,8 @@ def up(x, a):
 def bytes_of(r, c):
     s, l = min(r, c), max(r, c)
     tiles = -(-r // 16) * -(-c // 256)
-    if s == 1:
-        return up(8 * tiles, 256)
+    if s <= 16:  # sums of 16 x 16 products for runs of 256 places, and what comes of them, in 64 bits
+        return 2048 + 2048 * min(-(-l // 256), 512)
     return 2 * up(4 * s * up(l, 64), 256) + 3 * up(4 * s * up(s, 64), 256) + up(8 * tiles, 256)
 
 
@@ -148,8 +148,9 @@ def test_the_workspace_is_bounded_by_the_piece(piece):
     rc, n = need_orth(shapes, piece_bytes=piece)
     largest = max(bytes_of(*s) for s in shapes)
     assert rc == P.CKPT_OK and largest <= n <= max(piece or 4 << 30, largest)
-    assert need_orth([(64, 256), (2, 2), (200, 64), (5, 0)]) == (P.CKPT_OK, 0)
-    assert need_orth([(1, 5), (70000, 1), (64, 64)]) == (P.CKPT_OK, up(bytes_of(1, 5), 256) + bytes_of(70000, 1))
+    assert need_orth([(64, 256), (17, 17), (200, 64), (5, 0)]) == (P.CKPT_OK, 0)
+    assert need_orth([(1, 5), (700000, 16), (64, 64)]) == (P.CKPT_OK, bytes_of(1, 5) + bytes_of(700000, 16))
+    assert need_orth([(16, 900)], a=1.5, b=-0.5, c=0.0, steps=64) == (P.CKPT_OK, 2 * 4 * 16 * 960 + 3 * 4 * 16 * 64 + 256)
     assert need_orth([]) == (P.CKPT_OK, 0)
     assert need_orth([(300, 200)]) == (P.CKPT_OK, bytes_of(300, 200))
 
