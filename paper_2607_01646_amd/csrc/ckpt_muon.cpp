@@ -231,8 +231,12 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
             for (size_t k = first; k < last; ++k) {
                 const Job& j = jobs[k];
                 const auto at = [&](uint64_t Job::*o) { return (uint16_t*)(w + j.*o); };
-                t.m[k - first] = {at(p), at(q), poly ? at(p) : nullptr, at(out), (uint32_t)j.s,
-                                  k_of(p, j), 0, muon_chunk(k_of(p, j), p == &Job::x || p == &Job::y)};
+                const bool gram = p == &Job::x || p == &Job::y;
+                const uint32_t k_all = k_of(p, j), chunk = muon_chunk(k_all, gram), s4 = (uint32_t)up(j.s, 4);
+                // While the Gram matrix is made the other X holds nothing, and is as large as this one.
+                const uint32_t slices = gram && (uint64_t)s4 * up(k_all, chunk) / chunk <= k_all ? (uint32_t)(up(k_all, chunk) / chunk) : 1;
+                t.m[k - first] = {at(p), at(q), poly ? at(p) : nullptr, at(out), (uint32_t)j.s, k_all, 0, chunk,
+                                  gram ? (float*)at(p == &Job::x ? &Job::y : &Job::x) : nullptr, slices};
             }
             err = launch_muon_tri(t, s);
         };

@@ -537,6 +537,87 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads >= 512 ? 2 : 1) void tri_k
                t, 0, s0, s1, s2, s3, m.chunk);
 }
 
+// Few rows that are long have few tiles, and a tile's workgroup goes through all of k (X X^T of 64 x 8192: 60 us).  Here each
+// chunk of k has a workgroup, and join_kernel adds up what they leave in the order of tri_kernel's own sums: the bits are the
+// same, whichever way a call goes.  All five steps of 64 x 8192 356 -> 120 us, of 448 x 8192 439 -> 251, of 17 x 100000 3310 ->
+// 238; launch_muon_tri estimates both ways.
+struct PartEnd {
+    float* out;
+    uint32_t s, ld;
+};
+template <int TP, int TQ>
+struct Finish<PartEnd, TP, TQ> {
+    static __device__ inline void run(const PartEnd& e, const Early<PartEnd, TQ>&, f32x16 (&acc)[TP][TQ], uint32_t p0,
+                                      uint32_t q0, uint32_t, uint16_t*)
+    {
+        const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
+#pragma unroll
+        for (int tq = 0; tq < TQ; ++tq)
+#pragma unroll
+            for (int tp = 0; tp < TP; ++tp)
+#pragma unroll
+                for (uint32_t r = 0; r < 4; ++r) {
+                    const uint32_t p = p0 + 32 * tp + 8 * r + 4 * half, q = q0 + 32 * tq + (lane & 31);
+                    if (p > q || q >= e.s) continue;
+                    f32x4 v;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = acc[tp][tq][4 * r + j];
+                    *(f32x4*)(e.out + (uint64_t)q * e.ld + p) = v;
+                }
+    }
+};
+
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void slices_kernel(const TriArgs a)
+{
+    CKPT_BUFFERS(S, S);
+    static_assert(S::BQ == S::BP, "");
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t before = __ballot(lane < a.count && a.m[lane < kMuonMats ? lane : 0].first <= blockIdx.x);
+    const TriMatrix m = a.m[__builtin_amdgcn_readfirstlane(63 - __builtin_clzll(before))];
+    const uint32_t at = blockIdx.x - m.first, slice = at % m.slices, t = at / m.slices;
+    uint32_t i = (uint32_t)((__builtin_sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+    while (i * (i + 1) / 2 > t) --i;
+    while ((i + 1) * (i + 2) / 2 <= t) ++i;
+    const uint32_t j = t - i * (i + 1) / 2, k0 = slice * m.chunk, k = m.slices > 1 ? min(m.chunk, m.k - k0) : m.k;
+    const Operand X = {m.p + k0, (uint64_t)m.s * m.k, m.k, m.s, k};
+    const uint32_t ld = (m.s + 3) / 4 * 4;
+    const PartEnd end = {m.part + (uint64_t)slice * m.s * ld, m.s, ld};
+    product<S>(X, X, {m.s, m.s, k, 1, false}, end, make_uint2(__builtin_amdgcn_readfirstlane(j), __builtin_amdgcn_readfirstlane(i)),
+               t, 0, s0, s1, s2, s3, m.chunk);
+}
+
+__global__ __launch_bounds__(kThreads) void join_kernel(const TriArgs a)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t before = __ballot(lane < a.count && a.m[lane < kMuonMats ? lane : 0].first <= blockIdx.x);
+    const TriMatrix m = a.m[__builtin_amdgcn_readfirstlane(63 - __builtin_clzll(before))];
+    const uint32_t s = m.s, ld = up64(s), part_ld = (s + 3) / 4 * 4, at = (blockIdx.x - m.first) * kThreads + threadIdx.x;
+    const uint32_t q = at / (ld / 4), p = at % (ld / 4) * 4; // 4 values of p, up to the diagonal
+    if (q >= s || (p > q && p + 4 <= s)) return;
+    f32x4 v = {0, 0, 0, 0};
+    if (p <= q) {
+        const float* part = m.part + (uint64_t)q * part_ld + p;
+#pragma unroll 8
+        for (uint32_t k = 0; k < m.slices; ++k) v += *(const f32x4*)(part + (uint64_t)k * s * part_ld);
+    }
+    v = a.cc * (v * kDown);
+    uint2 hi, lo;
+    split2(v, hi, lo);
+    const uint64_t plane = (uint64_t)s * ld;
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+        const u16x4 u = __builtin_bit_cast(u16x4, z ? lo : hi);
+        uint16_t* out = m.out + z * plane;
+        if (p + 3 <= q || p >= s) *(u16x4*)(out + (uint64_t)q * ld + p) = u;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            if (p + j <= q) out[(uint64_t)q * ld + p + j] = out[(uint64_t)(p + j) * ld + q] = u[j];
+            else if (p + j >= s) out[(uint64_t)q * ld + p + j] = 0;
+        }
+    }
+}
+
 // [q][p] is [short][long]; for the last X of a tall matrix [long][short], as it lies.  W: the shape of the one, T: of the other.
 template <class W, class T, class End>
 __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply_kernel(const MuonArgs a)
@@ -572,8 +653,9 @@ __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply
 // Short sides up to 16: all steps are polynomials of one Gram matrix, G = U U^T, which is so small that it is kept in 64
 // bits: a launch makes it, one goes through the steps (A <- B A B, F <- B F) and the last makes X = F U.  Few terms do not
 // average the roundings of 22 bits (2 x 1033: 1.6e-6 off with planes, 5e-7 with products in fp32), and five steps from one
-// Gram matrix, which in fewer bits are not stable, are so in 64 (fits_thin in ckpt_muon.cpp).  Bound by HBM for long
-// rows, by the launches' latencies for others.
+// Gram matrix, which in fewer bits are not stable, are so in 64 (fits_thin in ckpt_muon.cpp).  Bound by the launches'
+// latencies (2 x 1033: 14 us, by planes 114), of long rows by the sums from LDS (16 x 1048576: 136 us for 192 MB read and
+// written; its transpose, whose lanes read rows of their own, 213).
 constexpr uint32_t kThinLd = kThreads + 4; // of LDS rows: 16 bytes further apart than a power of two
 
 // The update's s values at `at` of the long side; KEEP: the momentum's new ones are stored, else they are.
@@ -961,6 +1043,8 @@ constexpr struct {
     double few, many, end; // us a step with up to 128 tiles, and with 256 and more; us a tile
 } kTile[] = {{64, 64, 0.48, 0.56, 4}, {128, 128, 1.05, 1.75, 6}, {128, 256, 1.9, 2.75, 8}, {256, 256, 3.4, 4.9, 10}};
 
+constexpr double kJoin = 6; // us of join_kernel
+
 template <bool PA, bool QA>
 using Large = Shape<2, 2, PA, QA, 256, 256, 4, 2, 32, 2, true>;
 template <bool PA, bool QA>
@@ -987,7 +1071,7 @@ uint64_t number(A& a, uint32_t round, F tiles)
 // The size of tiles that is done first, of products that have `tiles(m, size)` with `steps(m)` of 64 values of k each, the
 // longest first; `parts`: some have sums in parts.
 template <class A, class T, class K>
-Size size_of(const A& a, bool parts, T tiles, K steps)
+Size size_of(const A& a, bool parts, T tiles, K steps, double* time = nullptr)
 {
     Size best = kSmall;
     double least = 1e30;
@@ -1008,6 +1092,7 @@ Size size_of(const A& a, bool parts, T tiles, K steps)
         t = std::max(t, most * step(all) + c.end);
         if (t < least) least = t, best = (Size)z;
     }
+    if (time) *time = least;
     return best;
 }
 
@@ -1110,7 +1195,26 @@ hipError_t launch_muon_tri(TriArgs& a, hipStream_t stream)
     std::stable_sort(a.m, a.m + a.count, [&](const TriMatrix& x, const TriMatrix& y) { return x.k > y.k; });
     bool parts = false;
     for (uint32_t i = 0; i < a.count; ++i) parts |= a.m[i].chunk != 0;
-    const Size size = size_of(a, parts, tiles, steps);
+    double whole;
+    const Size size = size_of(a, parts, tiles, steps, &whole);
+    if (a.m[0].part) {
+        uint64_t most = 0, work = 0;
+        for (uint32_t i = 0; i < a.count; ++i) {
+            const uint64_t each = a.m[i].slices > 1 ? a.m[i].chunk / 64 : steps(a.m[i]);
+            most = std::max(most, each);
+            work += tiles(a.m[i], kSmall) * a.m[i].slices * each;
+        }
+        const uint64_t runs = number(a, 1, [&](const TriMatrix& m) { return tiles(m, kSmall) * m.slices; });
+        const auto& c = kTile[kSmall];
+        const double mean = (double)work / (double)runs, rounds = (double)blocks(runs, 256);
+        if (std::max(rounds * (mean * c.many + c.end), (double)most * c.few + c.end) + kJoin < whole) {
+            const hipError_t e = a.all ? launch_tiles(slices_kernel<Small<false, false, true>>, &a, runs, kThreads, stream)
+                                       : launch_tiles(slices_kernel<Small<false, false, false>>, &a, runs, kThreads, stream);
+            if (e != hipSuccess) return e;
+            const uint64_t joins = number(a, 1, [](const TriMatrix& m) { return blocks((uint64_t)m.s * (blocks(m.s, 64) * 16), kThreads); });
+            return launch_tiles(join_kernel, &a, joins, kThreads, stream);
+        }
+    }
     a.shares = steps(a.m[0]) != steps(a.m[a.count - 1]);
     const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const TriMatrix& m) { return tiles(m, size); });
     const auto launch = [&](auto shape) {

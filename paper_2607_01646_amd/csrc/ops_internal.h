@@ -229,6 +229,8 @@ struct TriMatrix {
     const uint16_t *p, *q, *c;
     uint16_t* out;
     uint32_t s, k, first, chunk; // chunk: muon_chunk
+    float* part;                 // nullptr, or where sums of `slices` runs of a chunk each may go ([slices][s][up(s, 4)])
+    uint32_t slices;
 };
 struct TriArgs {
     TriMatrix m[kMuonMats];

@@ -83,6 +83,16 @@ def test_thin_zeros_and_what_is_no_number():
     assert torch.equal(out[1], P.ckpt_orthogonalize([good])[0])
 
 
+def test_long_rows_alone_and_among_others():
+    """Gram matrices of few long rows are summed by many workgroups, and by fewer in a call of many: to the same bits."""
+    for shape, n in (((448, 4096), 32), ((65, 5001), 40), ((3000, 130), 64), ((509, 2600), 20)):
+        x = [matrix(shape, scale=k + 1) for k in range(2)]
+        alone = [P.ckpt_orthogonalize([y])[0] for y in x]
+        check_orthogonal(alone[1], x[1])
+        among = P.ckpt_orthogonalize([x[k % 2] for k in range(n)] + [matrix((300, 300))])
+        assert all(torch.equal(among[k], alone[k % 2]) for k in range(n)), shape
+
+
 def test_zeros_and_what_is_no_number():
     """In one call: each matrix goes by itself."""
     good = matrix((80, 200))
