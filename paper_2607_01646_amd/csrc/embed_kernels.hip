@@ -106,6 +106,30 @@ __device__ inline void store(O* row, uint32_t c, uint32_t dim, const float (&x)[
     }
 }
 
+// A wave's share of a row of zeros, the `run`-th of `runs` of N elements each: cut at addresses that are multiples of 128
+// bytes, wherever the row begins, so that a line is written at once (7 tokens of 43667 x 7381 fp32: 396 -> 251 us).  PAST the
+// caches where rows are read meanwhile (a table of 32000 x 4096 takes 71 us with its gradient, 75 through them); few tokens
+// have none to keep (100 of 32000 x 4096 bf16, which the last cache holds: 47 us past it, 39 through it).
+template <uint32_t N, bool PAST, class O>
+__device__ inline void clear(O* row, uint32_t dim, uint32_t run, uint32_t runs)
+{
+    constexpr int kEach = 16 / sizeof(O);
+    const int skip = (int)((uintptr_t)row % 128 / sizeof(O)), lane = threadIdx.x & 63;
+    const int end = run + 1 < runs ? (int)((run + 1) * N) - skip : (int)dim;
+    for (int c = (int)(run * N) - skip + lane * kEach; c < end; c += 64 * kEach) {
+        if (c >= 0 && c + kEach <= (int)dim) {
+            if constexpr (PAST)
+                __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, (u32x4*)(row + c));
+            else
+                *(u32x4*)(row + c) = u32x4{0, 0, 0, 0};
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (c + j >= 0 && c + j < (int)dim) row[c + j] = 0;
+        }
+    }
+}
+
 // ---- the lookup ----
 //
 // A wave takes `UNROLL` KiB of a token's row, all of its loads ahead of its stores.
@@ -144,8 +168,9 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const EmbedArgs a, uin
 // tokens for each of the words, and those below all of them, which is where the workgroup's tokens begin, and lists the
 // ones that are the workgroup's in LDS.  Then each wave puts its tokens in their places.  A wave's places of a word follow
 // those of the waves before it, a lane's those of the lanes before it: the order is the tokens' own.  A wave whose tokens
-// its list does not hold goes over the ids again.  Bound by the instructions of the first pass.
-constexpr uint32_t kList = 256;
+// its list does not hold goes over the ids again and puts 64 in their places at a time (56265 tokens of 64, 3890 of them one
+// word: 77 us with lists of 256 and at most the tokens among 64 ids at a time, so 50).  Bound by the instructions of the first pass.
+constexpr uint32_t kList = 768;
 __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const EmbedArgs a)
 {
     extern __shared__ uint32_t s_place[]; // [kSortWaves][range]
@@ -246,13 +271,35 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const EmbedArgs a
         }
         return;
     }
+    uint32_t* list = s_list[wave];
+    uint32_t have = 0;
+    auto put_listed = [&] { // the first 64
+        const uint32_t token = list[min(lane, have - 1)];
+        put(lane < have, token, ((const uint2*)a.ids)[token].x);
+    };
     for (uint64_t t = begin; t < end; t += 64 * kAhead) {
         uint32_t w[kAhead];
         load(t, w);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (__ballot(w[u] - first < words)) put(w[u] - first < words, (uint32_t)(t + 64 * u + lane), w[u]);
+        for (int u = 0; u < kAhead; ++u) {
+            const bool in = w[u] - first < words;
+            const uint64_t which = __ballot(in);
+            if (in) list[have + __builtin_popcountll(which & ((1ull << lane) - 1))] = (uint32_t)(t + 64 * u + lane);
+            have += __builtin_popcountll(which);
+            if (have < 64) continue;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            put_listed();
+            const uint32_t rest = list[64 + lane];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            have -= 64;
+            if (lane < have) list[lane] = rest;
+        }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (have) put_listed();
 }
 
 // ---- the sums ----
@@ -290,15 +337,7 @@ __global__ __launch_bounds__(kThreads) void sums_kernel(const EmbedArgs a, uint3
         const bool none = lane < kZeroRows / 4 && v0 + lane < a.vocab && a.start[mine] == a.start[mine + 1];
         for (uint64_t left = __ballot(none); left; left &= left - 1) {
             O* row = (O*)a.table + (uint64_t)(v0 + __builtin_ctzll(left)) * a.table_ld;
-            constexpr int kEach = 16 / sizeof(O);
-            const float zero[kEach] = {};
-            // Past the caches: a table of 32000 x 4096 takes 71 us with its gradient, 75 through them.
-            for (uint32_t c = lane * kEach; c < a.dim; c += 64 * kEach) {
-                if (c + kEach <= a.dim)
-                    __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, (u32x4_any*)(row + c));
-                else
-                    store(row, c, a.dim, zero);
-            }
+            clear<64 * 16 / sizeof(O), true>(row, a.dim, 0, 1);
         }
         return;
     }
@@ -445,12 +484,13 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const EmbedArgs a)
                     for (int j = 0; j < kValues; ++j) sum[j] += there[u] ? p[u].at(j) : 0.0f;
             }
         }
-        if (c >= a.dim || (a.add && !any)) continue;
+        if (!any) {
+            if (!a.add) clear<64 * kValues, false>((O*)a.table + (uint64_t)v * a.table_ld, a.dim, blockIdx.y, gridDim.y);
+            continue;
+        }
+        if (c >= a.dim) continue;
         if (c + kValues > a.dim) Piece<T>::settle(sum, c, a.dim);
-        if (any)
-            write_row<O>(a, v, c, sum);
-        else
-            store((O*)a.table + (uint64_t)v * a.table_ld, c, a.dim, sum);
+        write_row<O>(a, v, c, sum);
     }
 }
 

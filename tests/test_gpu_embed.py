@@ -336,3 +336,39 @@ def test_refusals():
         P.ckpt_embedding_grad(d, ids, 10, dtype=torch.float16)
     with pytest.raises(ValueError):
         P.ckpt_embedding_grad(d, ids, 10, dtype=BF, add_to=table)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n, dim, vocab", [(5, 7, 300), (100, 513, 333), (300, 1, 1000), (1000, 259, 500)])
+def test_what_lies_beside_the_gradient_s_rows(n, dim, vocab, dtype):
+    """Rows of the C call's table at any place and any distance: all of each is written, and nothing else."""
+    import ctypes as C
+    from paper_2607_01646_amd import embed
+    d = torch.randn(n, dim, generator=gen(n), device="cuda").to(dtype)
+    ids = masked(words(n, vocab, "text"))
+    want = P.ckpt_embedding_grad(d, ids, vocab)
+    for begin, more in ((0, 1), (1, 0), (3, 8), (5, 129), (64, 3)):
+        whole = torch.full((begin + vocab * (dim + more) + 100,), 7.0, device="cuda").to(dtype)
+        a = embed.ckpt_embed_args(dtype=P.CKPT_TYPE_BF16 if dtype == BF else P.CKPT_TYPE_F32, tokens=n, dim=dim, vocab=vocab,
+                                  ids=ids.data_ptr(), ignore_index=IGNORE, scale=1.0, rows=d.data_ptr(), rows_stride=dim,
+                                  table=whole.data_ptr() + begin * whole.element_size(), table_stride=dim + more)
+        a.table_dtype = a.dtype
+        need = C.c_uint64()
+        assert embed._ops().ckpt_embedding_grad_workspace(C.byref(a), C.byref(need)) == P.CKPT_OK
+        work = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+        assert embed._ops().ckpt_embedding_grad(C.byref(a), 0, work.data_ptr(), need.value,
+                                                torch.cuda.current_stream().cuda_stream) == P.CKPT_OK
+        rows = whole[begin:begin + vocab * (dim + more)].view(vocab, dim + more)
+        assert torch.equal(rows[:, :dim], want)
+        assert bool((rows[:, dim:] == 7).all()) and bool((whole[:begin] == 7).all()) and bool((whole[begin + vocab * (dim + more):] == 7).all())
+
+
+@pytest.mark.parametrize("kind", ["text", "one"])
+def test_more_tokens_of_a_word_than_its_sorting_waves_list(kind):
+    n, dim, vocab = 150000, 17, 300000
+    d = torch.randn(n, dim, generator=gen(n), device="cuda")
+    ids = masked(words(n, vocab, kind))
+    want, bound, count = reference(d, ids, vocab, 1.0)
+    got = P.ckpt_embedding_grad(d, ids, vocab)
+    within(got, want, bound + U32 * want.abs(), "table")
+    assert torch.equal(got, P.ckpt_embedding_grad(d, ids, vocab))
