@@ -8,7 +8,8 @@
 // planes over all launches), small ones by the launches' latencies.
 //
 // The operands are two planes of fp16, 22 bits, and three products of planes
-// are made for each product: what is left out is 2^-22 of it.  The result is
+// are made for each product: what is left out is 2^-22 of it (four for short
+// sides up to kMuonAll, which leave nothing out).  The result is
 // as far from 64 bits as with products in fp32 (1e-6 to 5e-6).  One plane
 // would take a third of the time and leave it 1.3e-3 off for gradients without
 // structure, 6e-3 for those of few directions (one of bf16 1e-2 and 5e-2): the
@@ -801,7 +802,7 @@ __global__ __launch_bounds__(kThreads) void thin_apply_kernel(const MuonArgs a)
 // ---- small matrices ----
 //
 // Up to 64 x 256: a workgroup makes all of a matrix's step, X, A and B in LDS, in the time that the launches' latencies
-// would take many times over (4 matrices of 64 x 64 to 256: 33 us, 112 by the kernels above).  The same sums of the same
+// would take many times over (4 matrices of 64 x 64 to 256: 36 us, 112 by the kernels above).  The same sums of the same
 // operands, but step by step.  X is padded with zeros to 64 rows and 256 columns; rows lie 16 bytes further
 // apart than they are long, which spreads the 16 rows that a quarter of a wave reads over the banks.
 constexpr int kTinyThreads = 512, kTinyX = kTinyLong + 8, kTinyA = kTinyShort + 8;

@@ -69,9 +69,10 @@ def test_thin_matrices_are_as_exact_as_64_bits_let_them():
             want = orthogonal(x)
             assert bool(((y.double() - want).abs() <= 2 * U32 * want.abs() + 1e-9).all()), shape
     # with so many steps that the Gram matrix of U would not do
-    x = matrix((5, 400))
-    y, = P.ckpt_orthogonalize([x], steps=64, coefficients=(1.5, -0.5, 0.0))
-    check_orthogonal(y, x, steps=64, coefficients=(1.5, -0.5, 0.0))
+    for shape in ((5, 400), (1, 700), (900, 1), (3000, 16)):
+        x = matrix(shape)
+        y, = P.ckpt_orthogonalize([x], steps=64, coefficients=(1.5, -0.5, 0.0))
+        check_orthogonal(y, x, steps=64, coefficients=(1.5, -0.5, 0.0))
 
 
 def test_thin_zeros_and_what_is_no_number():
