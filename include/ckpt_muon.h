@@ -28,7 +28,8 @@ extern "C" {
  * Operands of the products are held in 22 bits (two planes of fp16), sums in
  * fp32, the norm in fp64: an fp32 result is as exact as with products in fp32
  * (1e-6 to 5e-6), others nearly.  With a side of up to 16 all is held in fp64,
- * and rounded once (unless the polynomial's a^(2 (steps - 1)) exceeds 1e7).
+ * and rounded once (unless the most that a step multiplies a value by, to the
+ * power of 2 (steps - 1), exceeds 1e7).
  */
 typedef struct {
     uint32_t steps;       /* 1 to 64 */

@@ -64,7 +64,7 @@ GradPlan plan_grad(const ckpt_embed_args* a)
     return l;
 }
 
-ckpt_status check_pointers(const ckpt_embed_args* a, int device, Known& known)
+ckpt_status check_pointers(const ckpt_embed_args* a, bool grad, int device, Known& known)
 {
     const uint64_t e = a->dtype == CKPT_TYPE_F32 ? 4 : 2, te = a->table_dtype == CKPT_TYPE_F32 ? 4 : 2;
     const Given given[] = {{a->ids, a->tokens, 1, 1, 8, "ids"},
@@ -78,6 +78,8 @@ ckpt_status check_pointers(const ckpt_embed_args* a, int device, Known& known)
     extent(a->vocab, a->dim, a->table_stride, te, &table);
     const uint64_t r = (uint64_t)(uintptr_t)a->rows, t = (uint64_t)(uintptr_t)a->table;
     if (rows && r < t + table && t < r + rows) return fail_free(CKPT_EINVAL, "rows and table overlap");
+    const uint64_t i = (uint64_t)(uintptr_t)a->ids, to = grad ? t : r, bytes = grad ? table : rows;
+    if (a->tokens && i < to + bytes && to < i + 8 * a->tokens) return fail_free(CKPT_EINVAL, "ids overlap %s", grad ? "the table" : "rows");
     return CKPT_OK;
 }
 
@@ -112,7 +114,7 @@ extern "C" ckpt_status ckpt_embedding(const ckpt_embed_args* a, int32_t device, 
     DeviceGuard dg;
     if (ckpt_status st = enter_device(device, dg)) return st;
     Known known;
-    if (ckpt_status st = check_pointers(a, device, known)) return st;
+    if (ckpt_status st = check_pointers(a, false, device, known)) return st;
     const hipError_t err = launch_lookup(embed_args(a), (hipStream_t)stream);
     if (err != hipSuccess) return fail_free(CKPT_EHIP, "lookup: %s", hipGetErrorString(err));
     return CKPT_OK;
@@ -140,7 +142,7 @@ extern "C" ckpt_status ckpt_embedding_grad(const ckpt_embed_args* a, int32_t dev
     DeviceGuard dg;
     if (ckpt_status st = enter_device(device, dg)) return st;
     Known known;
-    if (ckpt_status st = check_pointers(a, device, known)) return st;
+    if (ckpt_status st = check_pointers(a, true, device, known)) return st;
     if (l.bytes)
         if (ckpt_status st = check_given({workspace, 1, l.bytes, l.bytes, 1, "workspace"}, device, known)) return st;
     uint8_t* w = (uint8_t*)workspace;

@@ -372,3 +372,13 @@ def test_more_tokens_of_a_word_than_its_sorting_waves_list(kind):
     got = P.ckpt_embedding_grad(d, ids, vocab)
     within(got, want, bound + U32 * want.abs(), "table")
     assert torch.equal(got, P.ckpt_embedding_grad(d, ids, vocab))
+
+
+def test_ids_that_lie_in_what_is_written():
+    table = torch.zeros(10, 8, device="cuda")
+    ids = table.view(torch.int64)[3, :2]
+    with pytest.raises(P.CkptError, match="overlap"):
+        P.ckpt_embedding_grad(torch.ones(2, 8, device="cuda"), ids, 10, add_to=table)
+    assert not table.any()
+    d = torch.zeros(2, 8, device="cuda")  # ids beside the rows that are only read
+    assert not P.ckpt_embedding_grad(d, d.view(torch.int64)[0, :2], 10).any()
