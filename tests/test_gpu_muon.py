@@ -248,8 +248,8 @@ def test_a_parameter_that_is_its_master_copy_and_flat_lists():
         assert all(torch.equal(a, b) for a, b in zip(lists[k], twin[k]))
 
 
-def test_another_stream_and_a_graph():
-    shapes = [(64, 64), (33, 200), (200, 33), (300, 300)]
+@pytest.mark.parametrize("shapes", [[(64, 64), (33, 200), (200, 33), (300, 300)], [(5, 300), (80, 6000), (3000, 16), (4096, 500), (1, 1000)]])
+def test_another_stream_and_a_graph(shapes):
     lists, flat = state(shapes, BF, BF, gap=1)
     twin, same = state(shapes, BF, BF, gap=1)
     s = torch.cuda.Stream()
