@@ -26,10 +26,10 @@ extern "C" {
  * `steps` times and leaves the singular vectors as they are.  A matrix of
  * zeros stays zero; one with a NaN or an infinity becomes NaN altogether.
  * Operands of the products are held in 22 bits (two planes of fp16), sums in
- * fp32, the norm in fp64: an fp32 result is as exact as with products in fp32
- * (1e-6 to 5e-6), others nearly.  With a side of up to 16 all is held in fp64,
- * and rounded once (unless the most that a step multiplies a value by, to the
- * power of 2 (steps - 1), exceeds 1e7).
+ * fp32, the norm in fp64: X is as exact as with products in fp32 (1e-6 to
+ * 5e-6), of any type, and in a step as well.  With a side of up to 16 all is
+ * held in fp64, and rounded once (unless the most that a step multiplies a
+ * value by, to the power of 2 (steps - 1), exceeds 1e7).
  */
 typedef struct {
     uint32_t steps;       /* 1 to 64 */

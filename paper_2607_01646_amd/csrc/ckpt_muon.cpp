@@ -186,7 +186,6 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
         return fail_free(CKPT_EINVAL, "workspace of %llu bytes needs %llu", (unsigned long long)workspace_bytes,
                          (unsigned long long)need);
     a.eps = ns.eps;
-    a.exact = a.out_f32 && !all.front().m.master; // of a call all or none have master copies
     uint8_t* w = (uint8_t*)workspace;
     const MuonPolynomial polynomial = {ns.a, ns.b, ns.c, ns.steps};
     const auto done = [](hipError_t err) {
@@ -210,7 +209,7 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
     const bool fits = fits_twos(ns);
     return grouped(jobs, ns.piece_bytes, &need, [&](size_t first, size_t last) {
         const bool twos = fits && jobs[first].s > kSingly;
-        a.all = a.exact && jobs[first].s <= kMuonAll;
+        a.all = jobs[first].s <= kMuonAll;
         a.count = (uint32_t)(last - first);
         for (size_t k = first; k < last; ++k) {
             a.m[k - first] = jobs[k].m;
@@ -233,7 +232,7 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
                 const Job& j = jobs[k];
                 const auto at = [&](uint64_t Job::*o) { return (uint16_t*)(w + j.*o); };
                 const bool gram = p == &Job::x || p == &Job::y;
-                const uint32_t k_all = k_of(p, j), chunk = muon_chunk(k_all, gram, a.exact), s4 = (uint32_t)up(j.s, 4);
+                const uint32_t k_all = k_of(p, j), chunk = muon_chunk(k_all, gram), s4 = (uint32_t)up(j.s, 4);
                 // While the Gram matrix is made the other X holds nothing, and is as large as this one.
                 const uint32_t slices = gram && (uint64_t)s4 * up(k_all, chunk) / chunk <= k_all ? (uint32_t)(up(k_all, chunk) / chunk) : 1;
                 t.m[k - first] = {at(p), at(q), poly ? at(p) : nullptr, at(out), (uint32_t)j.s, k_all, 0, chunk,

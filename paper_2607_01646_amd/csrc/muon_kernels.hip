@@ -9,7 +9,7 @@
 //
 // The operands are two planes of fp16, 22 bits, and three products of planes
 // are made for each product: what is left out is 2^-22 of it (four for short
-// sides up to kMuonAll of exact results, which leave nothing out).  The result is
+// sides up to kMuonAll, which leave nothing out).  The result is
 // as far from 64 bits as with products in fp32 (1e-6 to 5e-6).  One plane
 // would take a third of the time and leave it 1.3e-3 off for gradients without
 // structure, 6e-3 for those of few directions (one of bf16 1e-2 and 5e-2): the
@@ -632,7 +632,7 @@ __global__ __launch_bounds__(W::kThreads, W::kThreads >= 512 ? 2 : 1) void apply
     const uint32_t p = wide ? l : s, q = wide ? s : l, np = (p + W::BP - 1) / W::BP, nq = (q + W::BQ - 1) / W::BQ;
     uint32_t t;
     if (!tile_in(a.shares, at - m.first, np * nq, t)) return;
-    const uint32_t chunk = muon_chunk(lda, false, a.exact);
+    const uint32_t chunk = muon_chunk(lda, false);
     const uint32_t band = t / (kBand * np), in = t % (kBand * np), width = min(kBand, nq - band * kBand);
     const uint2 tile = make_uint2(in / width, band * kBand + in % width);
     const Operand X = {m.x, (uint64_t)s * ldx, ldx, s, ldx};
@@ -802,7 +802,7 @@ __global__ __launch_bounds__(kThreads) void thin_apply_kernel(const MuonArgs a)
 // ---- small matrices ----
 //
 // Up to 64 x 256: a workgroup makes all of a matrix's step, X, A and B in LDS, in the time that the launches' latencies
-// would take many times over (4 matrices of 64 x 64 to 256: 34 us, 112 by the kernels above).  The same sums of the same
+// would take many times over (4 matrices of 64 x 64 to 256: 36 us, 112 by the kernels above).  The same sums of the same
 // operands, but step by step.  X is padded with zeros to 64 rows and 256 columns; rows lie 16 bytes further
 // apart than they are long, which spreads the 16 rows that a quarter of a wave reads over the banks.
 constexpr int kTinyThreads = 512, kTinyX = kTinyLong + 8, kTinyA = kTinyShort + 8;
@@ -828,16 +828,15 @@ __device__ inline f16x8 column_part(const uint16_t* m, uint32_t ld, uint32_t c0,
     return __builtin_bit_cast(f16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
 }
 // out[q][p]: q = lane % 16, p = 4 (lane / 16) + 0..3.
-template <bool ALL>
 __device__ inline void multiply2(f32x4& acc, const f16x8 (&p)[2], const f16x8 (&q)[2])
 {
-    if constexpr (ALL) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[1], q[1], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[1], q[1], acc, 0, 0, 0);
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], q[1], acc, 0, 0, 0);
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[1], q[0], acc, 0, 0, 0);
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], q[0], acc, 0, 0, 0);
 }
 
-template <class G, bool ALL>
+template <class G>
 __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, const MuonPolynomial n)
 {
     constexpr uint32_t kXPlane = kTinyShort * kTinyX, kAPlane = kTinyShort * kTinyA;
@@ -931,8 +930,8 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
                 }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                multiply2<ALL>(acc[0], x[h][0], y[h]);
-                multiply2<ALL>(acc[1], x[h][1], y[h]);
+                multiply2(acc[0], x[h][0], y[h]);
+                multiply2(acc[1], x[h][1], y[h]);
             }
         }
 #pragma unroll
@@ -974,9 +973,9 @@ __global__ __launch_bounds__(kTinyThreads) void tiny_kernel(const MuonArgs a, co
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 if constexpr (turned)
-                    multiply2<ALL>(acc[t], b[t & 3], x[t >> 2]);
+                    multiply2(acc[t], b[t & 3], x[t >> 2]);
                 else
-                    multiply2<ALL>(acc[t], x[t >> 2], b[t & 3]);
+                    multiply2(acc[t], x[t >> 2], b[t & 3]);
             }
         }
     };
@@ -1118,7 +1117,7 @@ hipError_t apply(MuonArgs& a, hipStream_t stream)
     const auto steps = [](const MuonMatrix& m) { return blocks(std::min(m.rows, m.cols), 64); };
     std::stable_sort(a.m, a.m + a.count, [&](const MuonMatrix& x, const MuonMatrix& y) { return steps(x) > steps(y); });
     bool parts = false;
-    for (uint32_t i = 0; i < a.count; ++i) parts |= muon_chunk((uint32_t)steps(a.m[i]) * 64, false, a.exact) != 0;
+    for (uint32_t i = 0; i < a.count; ++i) parts |= muon_chunk((uint32_t)steps(a.m[i]) * 64, false) != 0;
     const Size size = size_of(a, parts, tiles, steps);
     a.shares = steps(a.m[0]) != steps(a.m[a.count - 1]);
     const uint64_t all = number(a, a.shares ? kXcds : 1, [&](const MuonMatrix& m) { return tiles(m, size); });
@@ -1148,9 +1147,9 @@ hipError_t launch_muon_tiny(const MuonArgs& a, const MuonPolynomial& n, hipStrea
 {
     if (a.count == 0 || a.count > kMuonMats) return hipErrorInvalidValue;
     if (a.in_f32)
-        (a.exact ? tiny_kernel<float, true> : tiny_kernel<float, false>)<<<a.count, kTinyThreads, 0, stream>>>(a, n);
-    else // results of bf16, or of a step
-        tiny_kernel<uint16_t, false><<<a.count, kTinyThreads, 0, stream>>>(a, n);
+        tiny_kernel<float><<<a.count, kTinyThreads, 0, stream>>>(a, n);
+    else
+        tiny_kernel<uint16_t><<<a.count, kTinyThreads, 0, stream>>>(a, n);
     return hipGetLastError();
 }
 

@@ -209,23 +209,22 @@ struct MuonArgs {
     double eps;
     const float* grad_scale;
     bool nesterov, in_f32, out_f32, shares;
-    bool exact; // fp32 results: a step's X, times lr, and one in bf16 are rounded by more than the products leave
-    bool all;   // exact, short sides up to kMuonAll
+    bool all; // short sides up to kMuonAll
 };
-// Up to this short side exact results have the fourth product of planes made, too: few terms do not average what it leaves
-// out (2^-22 of a square), and cc A A has three times the size of B, in which it is one of two that nearly cancel (21 x 153:
-// 1.8 times as far off as by products in fp32; with it at most 1.48 times over 13867 shapes; 4 small matrices 34 -> 36 us).
+// Up to this short side the fourth product of planes is made, too: few terms do not average what it leaves out (2^-22 of a
+// square), and cc A A has three times the size of B, in which it is one of two that nearly cancel (21 x 153: 1.8 times as far
+// off as by products in fp32; with it at most 1.48 times over 13867 shapes; 4 small matrices 34 -> 36 us).  For a step's X and
+// a result in bf16 as well: a master copy that begins at zero, or a large lr, shows them.
 constexpr uint32_t kMuonAll = 448;
 // Values of k whose products are added up together before they are added to the sum (0: all): of X X^T, which the norms of
-// rows are, and where there are few, whose rounding fp32 would not hide (16 matrices with short sides of 512: 4% of the time,
-// so for exact results alone).  A matrix's own sides decide, and the call's type.
+// rows are, and where there are few, whose rounding fp32 would not hide (16 matrices with short sides of 512: 4% of the time).
+// A matrix's own sides decide.
 inline
 #ifdef __HIPCC__
     __host__ __device__
 #endif
-    uint32_t muon_chunk(uint32_t k, bool gram, bool exact)
+    uint32_t muon_chunk(uint32_t k, bool gram)
 {
-    if (!gram && !exact) return k <= 384 ? 128 : 0;
     return k <= 640 ? 128 : k < 1024 ? 256 : gram ? 512 : 0;
 }
 // Symmetric products out = ca I + cb c + cc p q, p q^T of rows of k values; no c: cc p q alone.

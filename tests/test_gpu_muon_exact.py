@@ -1,0 +1,67 @@
+"""How exact the orthogonalised step is: one arithmetic for every type and both
+entry points, as near to 64 bits as products in fp32, and the step's own
+outputs on all sizes of tiles (needs an MI355X; through the C ABI)."""
+import pytest
+import torch
+
+from muon_util import A, B, C, EPS, orthogonal
+from test_gpu_muon import BF, F32, matrix
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    import paper_2607_01646_amd as P
+
+# On both sides of every way that a matrix's own sides choose (16, 64 x 256, 448) and of the lengths of its sums in parts
+# (384, 640, 1024).
+SHAPES = [(9, 300), (33, 33), (64, 256), (21, 153), (40, 300), (300, 70), (96, 5000), (384, 390), (300, 700), (448, 448),
+          (450, 449), (512, 700), (640, 700), (700, 641), (777, 1003), (1003, 900), (1100, 1024), (1025, 1030)]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_the_step_takes_the_orthogonalisation_s_own_bits(shape):
+    """From masters and momentum of zero, without decay and with lr scale 1, the master copy is -X and nothing is rounded: X
+    is that of ckpt_orthogonalize in fp32, whatever the types of gradient and parameter."""
+    for grad_type in (F32, BF):
+        grad = matrix(shape, grad_type)
+        x, = P.ckpt_orthogonalize([grad.float()])
+        for param_type in (F32, BF):
+            master, momentum = torch.zeros_like(x), torch.zeros_like(x)
+            param = torch.ones_like(x).to(param_type)
+            P.ckpt_muon([param], [master], [momentum], [grad], lr=1.0, momentum=0.0, nesterov=False, scale=1.0)
+            assert torch.equal(master, -x), (grad_type, param_type)
+            assert torch.equal(param, (-x).to(param_type)) and torch.equal(momentum, grad.float())
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_a_bf16_result_is_the_fp32_one_rounded(shape):
+    x = matrix(shape, BF)
+    assert torch.equal(P.ckpt_orthogonalize([x])[0], P.ckpt_orthogonalize([x.float()])[0].to(BF))
+
+
+def in_fp32(u):
+    """The definition with torch's products in fp32."""
+    x = u / (u.square().sum(dtype=torch.float64).sqrt() + EPS).float()
+    x = x if x.shape[0] <= x.shape[1] else x.t().contiguous()
+    for _ in range(5):
+        g = x @ x.t().contiguous()
+        x = A * x + (B * g + C * (g @ g)) @ x
+    return x if u.shape[0] <= u.shape[1] else x.t()
+
+
+@pytest.mark.parametrize("few", [False, True])
+@pytest.mark.parametrize("shape", [(17, 40), (21, 153), (33, 33), (40, 300), (64, 256), (65, 300), (96, 160), (300, 130),
+                                   (257, 2049), (384, 400), (448, 448), (449, 600), (520, 1100), (777, 1003), (1100, 1024)])
+def test_as_exact_as_products_in_fp32(shape, few):
+    """Both against 64 bits, over eight matrices.  Each rounds its operands once: a value in fp32 by 0.29 steps of 2^-23 in the
+    mean square, one in two planes of fp16 by that and 0.24 of 2^-22 more (the first leaves half a step of 2^-10 at most,
+    evenly, of which the second's half step is 2^-22 in half of the cases, 2^-23 in a quarter, ..): 1.9 times as much
+    together.  The sums are rounded by no more than in fp32: once for 16 values of k and product of planes, 3 or 4 of those,
+    where fp32 products round at least once for 4 values, and in parts of 128 besides."""
+    off = [0.0, 0.0]
+    for seed in range(8):
+        u = matrix(shape, few=few, seed=seed)
+        want = orthogonal(u)
+        for k, x in enumerate((P.ckpt_orthogonalize([u])[0], in_fp32(u))):
+            off[k] += float((x.double() - want).square().sum())
+    assert off[0] ** 0.5 <= 2 * off[1] ** 0.5, "%.3g, in fp32 %.3g" % (off[0] ** 0.5, off[1] ** 0.5)
