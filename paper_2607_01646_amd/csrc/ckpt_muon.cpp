@@ -15,6 +15,8 @@ namespace ckpt {
 namespace {
 
 constexpr uint64_t kSingly = 448; // up to this short side: step by step, which is fewer launches and twice as exact
+// What a short side decides for all matrices of a launch: groups hold matrices of one way alone.
+uint32_t way(uint64_t s) { return (s > kSingly) + (s > kMuonAll); }
 constexpr uint64_t kDefaultPiece = 4ull << 30; // the matrices of a layer of 4096 x 11008, in one group
 
 // The largest that a singular value becomes, that a step multiplies one by, and that two steps do (NaN and infinity: as
@@ -114,8 +116,8 @@ Jobs sorted(const std::vector<Job>& jobs, const ckpt_newton_schulz& ns)
         list.push_back(j);
         list.back().thin = &list == &to.thin;
     }
-    std::stable_partition(to.others.begin(), to.others.end(),
-                          [](const Job& j) { return std::min(j.m.rows, j.m.cols) > kSingly; });
+    const auto of = [](const Job& j) { return way(std::min(j.m.rows, j.m.cols)); };
+    std::stable_sort(to.others.begin(), to.others.end(), [&](const Job& x, const Job& y) { return of(x) > of(y); });
     return to;
 }
 
@@ -134,7 +136,7 @@ ckpt_status grouped(std::vector<Job>& jobs, uint64_t piece_bytes, uint64_t* most
             if (!lay_out(j, j.m.rows, j.m.cols, next))
                 return fail_free(CKPT_EINVAL, "matrix of %u x %u: too many elements", j.m.rows, j.m.cols);
             tiles += std::max<uint64_t>(j.m.part_n, (j.s + 63) / 64 * ((j.l + 63) / 64)); // of any launch, at most
-            if (k > i && (next > budget || tiles > (1u << 23) || (j.s > kSingly) != (jobs[i].s > kSingly))) break;
+            if (k > i && (next > budget || tiles > (1u << 23) || way(j.s) != way(jobs[i].s))) break;
             if (tiles > (1u << 23)) return fail_free(CKPT_EINVAL, "matrix of %u x %u: too many elements", j.m.rows, j.m.cols);
             jobs[k] = j;
             at = next;

@@ -65,3 +65,17 @@ def test_as_exact_as_products_in_fp32(shape, few):
         for k, x in enumerate((P.ckpt_orthogonalize([u])[0], in_fp32(u))):
             off[k] += float((x.double() - want).square().sum())
     assert off[0] ** 0.5 <= 2 * off[1] ** 0.5, "%.3g, in fp32 %.3g" % (off[0] ** 0.5, off[1] ** 0.5)
+
+
+def test_short_sides_beside_the_ways_limits_in_one_call():
+    """A launch's matrices go one way: those on either side of a limit keep the bits of their own calls, in any order."""
+    shapes = [(449, 600), (447, 600), (600, 448), (385, 500), (450, 449), (383, 500), (500, 384), (640, 641), (17, 600),
+              (1025, 1026), (65, 449), (448, 449), (1024, 1023)]
+    x = [matrix(s, BF if k % 3 == 0 else F32) for k, s in enumerate(shapes)]
+    for kind in (BF, F32):
+        mine = [t for t in x if t.dtype == kind]
+        alone = [P.ckpt_orthogonalize([t])[0] for t in mine]
+        for order in (1, -1):
+            for piece in (0, 8 << 20):
+                out = P.ckpt_orthogonalize(mine[::order], piece_bytes=piece)
+                assert all(torch.equal(a, b) for a, b in zip(out[::order], alone))
