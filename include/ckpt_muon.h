@@ -51,8 +51,8 @@ typedef struct {
 /* Orthogonalises n matrices of one type (CKPT_TYPE_*).  `workspace`: 256-byte
  * aligned device memory of at least the bytes that _workspace says, the call's
  * own until its work on `stream` has run (NULL where that is 0).
- * Results do not overlap each other or other matrices; contiguous ones are
- * checked.  Errors: EINVAL (sizes, numbers, pointers, overlaps), EHIP. */
+ * Results lie in no element of each other or of other matrices (whose rows may
+ * lie between theirs).  Errors: EINVAL (sizes, numbers, pointers, overlaps), EHIP. */
 ckpt_status ckpt_orthogonalize_workspace(const ckpt_matrix* m, uint32_t n, const ckpt_newton_schulz* ns,
                                          uint64_t* bytes);
 ckpt_status ckpt_orthogonalize(const ckpt_matrix* m, uint32_t n, uint32_t dtype, const ckpt_newton_schulz* ns,

@@ -270,20 +270,46 @@ ckpt_status run_all(const std::vector<Job>& all, MuonArgs& a, const ckpt_newton_
     });
 }
 
+// Bytes [lo, hi): rows of `width`, `pitch` apart.
 struct Span {
-    uint64_t lo, hi;
+    uint64_t lo, hi, rows, width, pitch;
     bool written;
+    Span(const void* p, uint64_t n, uint64_t cols, uint64_t ld, uint64_t e, bool w)
+        : lo((uint64_t)(uintptr_t)p), rows(n), width(cols * e), pitch(ld * e), written(w)
+    {
+        if (n == 1 || ld == cols) rows = 1, width = pitch = n * cols * e;
+        hi = lo + (rows - 1) * pitch + width;
+    }
 };
+
+// Whether a row of x lies where one of y does; x begins first, and y within it.
+bool meet(const Span& x, const Span& y)
+{
+    if (x.rows == 1 && y.rows == 1) return true;
+    if (x.pitch == y.pitch) { // y's rows begin `in` bytes behind those of x from the `skip`-th on
+        const uint64_t skip = (y.lo - x.lo) / x.pitch, in = (y.lo - x.lo) % x.pitch;
+        return (in < x.width && skip < x.rows) || (in + y.width > x.pitch && skip + 1 < x.rows);
+    }
+    const Span &few = x.rows < y.rows ? x : y, &many = x.rows < y.rows ? y : x;
+    for (uint64_t i = 0; i < few.rows; ++i) {
+        const uint64_t lo = few.lo + i * few.pitch, hi = lo + few.width;
+        // The first of the others' rows that ends behind lo.
+        const uint64_t j = lo < many.lo + many.width ? 0 : (lo - many.lo - many.width) / many.pitch + 1;
+        if (j < many.rows && many.lo + j * many.pitch < hi) return true;
+    }
+    return false;
+}
 
 // Whether something written lies where something else does.
 bool overlap(std::vector<Span>& spans)
 {
     std::sort(spans.begin(), spans.end(), [](const Span& x, const Span& y) { return x.lo < y.lo; });
-    uint64_t any = 0, written = 0;
-    for (const Span& x : spans) {
-        if (x.lo < (x.written ? any : written)) return true;
-        any = std::max(any, x.hi);
-        if (x.written) written = std::max(written, x.hi);
+    std::vector<const Span*> open; // that end behind the beginning of the next
+    for (const Span& y : spans) {
+        open.erase(std::remove_if(open.begin(), open.end(), [&](const Span* x) { return x->hi <= y.lo; }), open.end());
+        for (const Span* x : open)
+            if ((x->written || y.written) && meet(*x, y)) return true;
+        open.push_back(&y);
     }
     return false;
 }
@@ -375,12 +401,9 @@ extern "C" ckpt_status ckpt_orthogonalize(const ckpt_matrix* m, uint32_t n, uint
             if (ckpt_status st = check_given({m[i].in, rows, cols, m[i].in_stride, e, what}, device, known)) return st;
             snprintf(what, sizeof what, "matrix %u, its result", i);
             if (ckpt_status st = check_given({m[i].out, rows, cols, m[i].out_stride, e, what}, device, known)) return st;
-            const auto span = [&](const void* p, uint64_t ld, bool written) {
-                if (rows > 1 && ld != cols) return; // rows of others may lie between them
-                spans.push_back({(uint64_t)(uintptr_t)p, (uint64_t)(uintptr_t)p + rows * cols * e, written});
-            };
-            span(m[i].out, m[i].out_stride, true);
-            if (m[i].in != m[i].out || (rows > 1 && m[i].in_stride != m[i].out_stride)) span(m[i].in, m[i].in_stride, false);
+            spans.emplace_back(m[i].out, rows, cols, m[i].out_stride, e, true);
+            if (m[i].in != m[i].out || (rows > 1 && m[i].in_stride != m[i].out_stride))
+                spans.emplace_back(m[i].in, rows, cols, m[i].in_stride, e, false);
             MuonMatrix& to = jobs[at++].m;
             to.in = m[i].in;
             to.in_ld = m[i].in_stride;
@@ -443,7 +466,7 @@ extern "C" ckpt_status ckpt_muon(const ckpt_muon_matrix* m, uint32_t n, const ck
                 }
                 // A parameter in full precision may be its own master copy.
                 if (&x == part && m[i].param == (void*)m[i].master && pe == 4) continue;
-                spans.push_back({p, p + all * x.e, x.written});
+                spans.emplace_back(x.p, 1, all, all, x.e, x.written);
             }
             MuonMatrix& to = jobs[at++].m;
             to.in = m[i].grad;

@@ -79,3 +79,28 @@ def test_short_sides_beside_the_ways_limits_in_one_call():
             for piece in (0, 8 << 20):
                 out = P.ckpt_orthogonalize(mine[::order], piece_bytes=piece)
                 assert all(torch.equal(a, b) for a, b in zip(out[::order], alone))
+
+
+def test_matrices_that_overlap_row_by_row_are_refused():
+    wide = matrix((150, 1000))
+    old = wide.clone()
+    a, b = wide[:, :300], wide[:, 299:500]
+    new = [torch.empty_like(t) for t in (a, b)]
+    for x, out in (([a, b], [a, b]),  # a column of both is written
+                   ([a, a], [a, a]),  # one matrix twice
+                   ([a, b], [new[0], a[:, :201]]),  # over the other's input
+                   ([a], [wide.view(-1)[:75000].view(150, 500)[:, :300]]),  # in place, but with other rows
+                   ([a], [wide.view(-1)[100:45100].view(150, 300)]),  # contiguous, over the strided ones
+                   ([a, new[0]], [wide[:, 500:800], wide[:, 700:]])):
+        with pytest.raises(P.CkptError, match="overlap"):
+            P.ckpt_orthogonalize(x, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(wide, old)
+    # what reads the same, and what lies between the rows of others, does not
+    want = P.ckpt_orthogonalize([a.contiguous(), wide[:, 300:600].contiguous(), wide[1::2, 600:].contiguous()])
+    twice = P.ckpt_orthogonalize([a, a, b])
+    assert torch.equal(twice[0], want[0]) and torch.equal(twice[1], want[0])
+    parts = [a, wide[:, 300:600], wide[1::2, 600:]]
+    for x, y in zip(P.ckpt_orthogonalize(parts, out=parts), want):
+        assert torch.equal(x, y)
+    assert torch.equal(wide[::2, 600:], old[::2, 600:])
