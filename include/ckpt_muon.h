@@ -84,7 +84,7 @@ typedef struct {
  *   param = master rounded to nearest even.
  * Call it behind ckpt_wait(CKPT_WAIT_CAPTURED) on the same stream where a
  * snapshot of these fragments may be in flight.
- * Errors: EINVAL (also fragments that overlap), EHIP. */
+ * Errors: EINVAL (also fragments that overlap, or have grad_scale in them), EHIP. */
 ckpt_status ckpt_muon_workspace(const ckpt_muon_matrix* m, uint32_t n, const ckpt_muon_args* args, uint64_t* bytes);
 ckpt_status ckpt_muon(const ckpt_muon_matrix* m, uint32_t n, const ckpt_muon_args* args, int32_t device,
                       void* workspace, uint64_t workspace_bytes, void* stream);

@@ -446,6 +446,7 @@ extern "C" ckpt_status ckpt_muon(const ckpt_muon_matrix* m, uint32_t n, const ck
         if (args->grad_scale)
             if (ckpt_status st = check_given({args->grad_scale, 1, 1, 1, 4, "grad_scale"}, device, known)) return st;
         std::vector<Span> spans;
+        if (args->grad_scale) spans.emplace_back(args->grad_scale, 1, 1, 1, 4, false); // launches behind the first read it again
         size_t at = 0;
         for (uint32_t i = 0; i < n; ++i) {
             const uint64_t all = m[i].rows * m[i].cols;

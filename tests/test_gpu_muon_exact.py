@@ -104,3 +104,13 @@ def test_matrices_that_overlap_row_by_row_are_refused():
     for x, y in zip(P.ckpt_orthogonalize(parts, out=parts), want):
         assert torch.equal(x, y)
     assert torch.equal(wide[::2, 600:], old[::2, 600:])
+
+
+def test_a_scale_that_lies_in_what_is_written_is_refused():
+    p, w, m, g = (torch.ones(40, 300, device="cuda") for _ in range(4))
+    for t in (p, w, m):
+        with pytest.raises(P.CkptError, match="overlap"):
+            P.ckpt_muon([p], [w], [m], [g], lr=1e-2, grad_scale=t.view(-1)[-1:])
+    torch.cuda.synchronize()
+    assert all(bool((t == 1).all()) for t in (p, w, m))
+    P.ckpt_muon([p], [w], [m], [g], lr=1e-2, grad_scale=g.view(-1)[:1])  # beside what is only read
