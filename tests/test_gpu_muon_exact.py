@@ -4,8 +4,9 @@ outputs on all sizes of tiles (needs an MI355X; through the C ABI)."""
 import pytest
 import torch
 
-from muon_util import A, B, C, EPS, orthogonal
-from test_gpu_muon import BF, F32, matrix
+from muon_util import A, B, C, EPS, check_orthogonal, orthogonal, step
+from ops_util import within
+from test_gpu_muon import BF, F32, matrix, state
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +115,53 @@ def test_a_scale_that_lies_in_what_is_written_is_refused():
     torch.cuda.synchronize()
     assert all(bool((t == 1).all()) for t in (p, w, m))
     P.ckpt_muon([p], [w], [m], [g], lr=1e-2, grad_scale=g.view(-1)[:1])  # beside what is only read
+
+
+def check_step(lists, before, i, lr, wd, scale, what):
+    want = step(*[x[i] for x in before], lr, 0.9, True, wd, scale)
+    for k, name in enumerate(("param", "master", "momentum")):
+        value, bound = getattr(want, name)
+        within(lists[k][i], value, bound, "%s of %s" % (name, what))
+
+
+@pytest.mark.parametrize("param, grad", [(BF, BF), (F32, F32), (BF, F32)])
+@pytest.mark.parametrize("shape", [(390, 500), (448, 900), (900, 448), (520, 1100), (1100, 520), (777, 1003), (1003, 777),
+                                   (1100, 1200)])
+def test_the_step_of_larger_matrices_against_64_bits(shape, param, grad):
+    """With decay, and from masters of zero with a large lr, where X is all that there is."""
+    for lr, wd, scale, zero in ((2e-2, 0.1, 0.2 * max(shape) ** 0.5, False), (1.0, 0.0, 0.7, True)):
+        lists, _ = state([shape], param, grad, gap=1)
+        if zero:
+            lists[0][0].zero_()
+            lists[1][0].zero_()
+        before = [[t.clone() for t in x] for x in lists]
+        P.ckpt_muon(*lists, lr=lr, momentum=0.9, weight_decay=wd, scale=scale)
+        check_step(lists, before, 0, lr, wd, scale, shape)
+        assert torch.equal(lists[0][0], lists[1][0].to(param))
+
+
+@pytest.mark.parametrize("shape, count", [((1000, 1100), 4), ((1000, 1100), 24), ((1088, 1152), 8), ((2176, 2200), 2)])
+def test_the_step_on_larger_tiles_against_64_bits(shape, count):
+    """So many matrices, every other one tall, that tiles of 128 x 256 and 256 x 256 are the quickest for their products."""
+    shapes = [shape if k % 2 else shape[::-1] for k in range(count)]
+    lists, _ = state(shapes, BF, BF)
+    before = [[t.clone() for t in x] for x in lists]
+    P.ckpt_muon(*lists, lr=2e-2, momentum=0.9, weight_decay=0.1, scale=5.0)
+    for i in (0, count - 1):
+        check_step(lists, before, i, 2e-2, 0.1, 5.0, shapes[i])
+    for i in range(count):
+        one = [[x[i]] for x in before]
+        P.ckpt_muon(*one, lr=2e-2, momentum=0.9, weight_decay=0.1, scale=5.0)
+        assert all(torch.equal(a[0], b[i]) for a, b in zip(one, lists)), i
+
+
+@pytest.mark.parametrize("count", [1, 2, 3, 5, 6, 7, 8])
+@pytest.mark.parametrize("side", [1025, 1088, 1152, 1153])
+def test_tiles_past_the_last_row_of_a_symmetric_product(side, count):
+    """Short sides of up to half a tile of 256 more than whole ones: of the last row's two tiles of 128 x 256 one begins past
+    the matrix.  With 5 to 8 matrices those tiles are the quickest for X X^T and its polynomials."""
+    x = [matrix((side, side + 64) if k % 2 else (side + 64, side), seed=k) for k in range(count)]
+    out = P.ckpt_orthogonalize(x)
+    check_orthogonal(out[-1], x[-1])
+    for a, b in zip(out, x):
+        assert torch.equal(a, P.ckpt_orthogonalize([b])[0])
