@@ -27,9 +27,12 @@ extern "C" {
  * zeros stays zero; one with a NaN or an infinity becomes NaN altogether.
  * Operands of the products are held in 22 bits (two planes of fp16), sums in
  * fp32, the norm in fp64: X is as exact as with products in fp32 (1e-6 to
- * 5e-6), of any type, and in a step as well.  With a side of up to 16 all is
- * held in fp64, and rounded once (unless the most that a step multiplies a
- * value by, to the power of 2 (steps - 1), exceeds 1e7).
+ * 5e-6), of any type, and in a step as well.  No value is held to less than
+ * 2^-37, though: where eps is far above |U|, so that X begins small, it is off
+ * by up to 2^-37 sqrt(rows cols) eps / |U| of itself (777 x 1003 with 1e4 |U|
+ * for eps: 4e-5).  With a side of up to 16 all is held in fp64, and rounded
+ * once (unless the most that a step multiplies a value by, to the power of
+ * 2 (steps - 1), exceeds 1e7).
  */
 typedef struct {
     uint32_t steps;       /* 1 to 64 */

@@ -165,3 +165,17 @@ def test_tiles_past_the_last_row_of_a_symmetric_product(side, count):
     check_orthogonal(out[-1], x[-1])
     for a, b in zip(out, x):
         assert torch.equal(a, P.ckpt_orthogonalize([b])[0])
+
+
+@pytest.mark.parametrize("share", [1e-2, 1e-4, 1e-7, 1e-12])
+@pytest.mark.parametrize("shape", [(9, 300), (64, 256), (70, 130), (777, 1003), (2100, 1300)])
+def test_norms_far_below_eps(shape, share):
+    """X is small then.  A value of X in planes is off by 2^-37 at most where they hold no 22 bits of it (half of fp16's
+    smallest step, of 2^12 times the value), and what was rounded grows by 3.4445 a step: 2^-37 (3.4445 + .. + 3.4445^5) for
+    each value, beside the roundings that any X has.  Short sides up to 16 have none of that."""
+    u = matrix(shape, scale=1.0)
+    u = u / u.norm() * (EPS * share)
+    x, = P.ckpt_orthogonalize([u])
+    want = orthogonal(u)
+    grown = 0.0 if min(shape) <= 16 else 2.0 ** -37 * sum(A ** k for k in range(1, 6)) * (shape[0] * shape[1]) ** 0.5
+    assert float((x.double() - want).norm()) <= grown + 5e-6 * float(want.norm())
