@@ -4,8 +4,10 @@
  * it may share the table.
  *
  * Every result depends on the inputs alone: a row's tokens are summed in their
- * order, in runs whose lengths the number of tokens decides.  Conventions are
- * those of ckpt_ops.h.
+ * order, in runs whose length the call's sizes decide (the number of tokens,
+ * the rows' width and type, for few tokens also the number of words): columns
+ * of a table by themselves need not have the bits of the whole table's.
+ * Conventions are those of ckpt_ops.h.
  */
 #ifndef CKPT_EMBED_H
 #define CKPT_EMBED_H

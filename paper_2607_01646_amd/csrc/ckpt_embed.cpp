@@ -43,8 +43,9 @@ GradPlan plan_grad(const ckpt_embed_args* a)
     if (l.few) return l;
     // Sorting workgroups: each reads all ids, so no more than the GPU has units, unless LDS holds no more words.
     l.range = (uint32_t)std::min<uint64_t>(std::max<uint64_t>((a->vocab + 255) / 256, 32), kSortRange);
-    // Sorted tokens that a wave sums: 64 ids at a time, as long as that leaves each SIMD two waves (8192 tokens of 4096: 61 us with the table, with four waves 70); and no more than 1024
-    // chunks, which bounds what is joined for a word that most tokens have.
+    // Sorted tokens that a wave sums: 64, or fewer down to 8 until each SIMD has two waves (8192 tokens of 4096: 61 us with the
+    // table, with four waves 70), or as many as make 1024 chunks of a long batch.  Narrow rows have up to 4096 chunks
+    // then (halved until there are 2048 or more), which bounds what is joined for a word that most tokens have.
     uint64_t chunk = std::max<uint64_t>(64, up((n + 1023) / 1024, 64));
     while (chunk > 8 && (n + chunk - 1) / chunk * runs < 2048) chunk /= 2;
     l.chunk = (uint32_t)chunk;
