@@ -14,7 +14,12 @@
 namespace ckpt {
 namespace {
 
-constexpr uint64_t kSingly = 448; // up to this short side: step by step, which is fewer launches and twice as exact
+// Up to this short side it goes step by step, which is 17 launches for 5 steps, by twos (fits_twos) 19, and half the error.
+// Above it what is quicker depends on the long side and on how many matrices a launch has (us step by step, by twos: one of
+// 512 x 700 153, 167; one of 777 x 1003 177, 209; 32 of 512 x 512 544, 611; 16 of 512 x 1024 424, 419; a GPT's 16 of 512 x 512
+// to 2048 693, 606; 2048 x 8192 1757, 1409).  A matrix's own short side decides: its bits may not depend on the others of the
+// call, and matrices of two ways in one call would have the launches of both.
+constexpr uint64_t kSingly = 448;
 // What a short side decides for all matrices of a launch: groups hold matrices of one way alone.
 uint32_t way(uint64_t s) { return (s > kSingly) + (s > kMuonAll); }
 constexpr uint64_t kDefaultPiece = 4ull << 30; // the matrices of a layer of 4096 x 11008, in one group
@@ -65,9 +70,10 @@ bool fits_thin(const ckpt_newton_schulz& ns) { return std::pow(Iterates(ns).fact
 
 // Whether two steps are made from one Gram matrix: X's next is B A B (all are polynomials of A), and X is multiplied once,
 // by the product of both factors.  Of the products with the long side that leaves 9 for 5 steps instead of 15, in units of
-// s^2 l, and of those of the short side 11 instead of 5, in units of s^3.  It is as exact as step by step (a Gram matrix of
-// X itself sets every other step right; with three from one, what is rounded off beside the large singular values grows in
-// the small ones' place until it is all there is).  The product of both factors has to fit the operands' scale.
+// s^2 l, and of those of the short side 11 instead of 5, in units of s^3.  A Gram matrix of X itself sets every other step
+// right: 777 x 1003 is 3.1e-6 off, step by step 1.4e-6, by products in fp32 2.7e-6.  (With three from one, what is rounded off
+// beside the large singular values grows in the small ones' place until it is all there is.)  The product of both factors has
+// to fit the operands' scale.
 bool fits_twos(const ckpt_newton_schulz& ns) { return Iterates(ns).both <= 14; }
 
 // A matrix of the call, whichever entry point it is of.
